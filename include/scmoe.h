@@ -1,5 +1,6 @@
 /*
- * scmoe.h — C ABI of the MI355X (gfx950) ScMoE forward-pass library.
+ * scmoe.h — C ABI of the MI355X (gfx950) ScMoE library: the forward pass of a block, and what
+ * trains its routing part (layer norm, balance loss, gradients of gate, encode and decode).
  *
  * One shortcut-connected MoE block (ScMoE paper, Sec. 3.1, Eq. (7)):
  *
@@ -27,7 +28,7 @@
  *  - bf16 buffers must be 16-byte aligned with row strides that are multiples of 8
  *    elements; fp32 buffers 16-byte aligned with strides that are multiples of 4.
  *    d and F must be multiples of 8.  Violations give SCMOE_ERR_SHAPE.
- *  - T == 0 is legal everywhere (no-op, SCMOE_OK).
+ *  - T == 0 is legal everywhere (no-op, SCMOE_OK; sums over the tokens are written: zeros).
  */
 #ifndef SCMOE_H
 #define SCMOE_H
@@ -63,6 +64,8 @@ enum { SCMOE_CG_NONE = 0, SCMOE_CG_1 = 1, SCMOE_CG_2 = 2 };
 #define SCMOE_MAX_EXPERTS 64
 /* Upper limit on k, the routed experts per token (the paper's layers use 1, 2 and 3). */
 #define SCMOE_MAX_TOPK 4
+/* Upper limit on the width of a normed row. */
+#define SCMOE_MAX_NORM_WIDTH 16384
 
 /* Shape and options of one layer.  Plain data, host memory, read during the call only. */
 typedef struct scmoe_desc {
@@ -441,6 +444,119 @@ int moe_top2_layer_forward(const scmoe_desc* desc, const void* x, int64_t ldx,
                            const scmoe_weights* w, void* y, int64_t ldy,
                            const scmoe_routing_out* routing, void* workspace,
                            size_t ws_bytes, void* stream);
+
+/*
+ * Layer norm over the model width, in front of a block of a pre-norm model (the paper leaves the norms
+ * of its blocks out of the formulas, Sec. 3.1):
+ *
+ *   h[t,:]   = x[t,:] + residual[t,:]                        (rounded to dtype and stored in `sum`)
+ *   mean[t]  = sum_i h[t,i] / d,   rstd[t] = 1 / sqrt(sum_i (h[t,i] - mean[t])^2 / d + eps)
+ *   y[t,:]   = (h[t,:] - mean[t]) * rstd[t] * gamma + beta
+ *
+ * residual NULL: h = x, and sum must be NULL; with a residual both are needed.  What is normed is the
+ * rounded sum, so the backward pass, which reads it, differentiates what was computed.
+ * gamma, beta: [d] fp32, 16-byte aligned, NULL = 1 and 0.  mean, rstd: [T] fp32 or NULL (serving).
+ * eps > 0, else SCMOE_ERR_ARG; d <= SCMOE_MAX_NORM_WIDTH.  fp32 arithmetic, the squares summed about
+ * the mean.  sum and y may each be the buffer of x or residual (same pointer and stride; not both the
+ * same one).  One launch, no workspace; a row's result does not depend on the other rows.
+ */
+int scmoe_layer_norm(const void* x, int64_t ldx, int32_t dtype, const void* residual, int64_t ldres,
+                     const float* gamma, const float* beta, float eps, int32_t T, int32_t d,
+                     void* sum, int64_t ldsum, void* y, int64_t ldy, float* mean, float* rstd,
+                     void* stream);
+
+/* Bytes of workspace scmoe_layer_norm_backward needs for dgamma and dbeta (at most 4 KiB per
+ * column).  `out` is a host pointer. */
+int scmoe_layer_norm_backward_workspace_bytes(int32_t T, int32_t d, size_t* out);
+
+/*
+ * Gradient of scmoe_layer_norm.  x: what was normed (`sum` where there was a residual); mean, rstd as
+ * the forward call kept them; dy: [T, d], the gradient of y.  With xh = (x - mean) rstd, g = dy gamma:
+ *
+ *   dx[t,:]  = rstd[t] * (g - sum_i g_i / d - xh * sum_i (g_i xh_i) / d) + dsum[t,:]
+ *   dgamma   = sum_t dy[t,:] * xh[t,:],   dbeta = sum_t dy[t,:]
+ *
+ * dsum (NULL: none): the gradient that reaches the sum beside the norm (the residual stream's); dx is
+ * then the gradient of both x and residual.  dgamma, dbeta: [d] fp32, overwritten, each may be NULL;
+ * with both NULL the workspace may be NULL.  dx may be the buffer of dy, x or dsum (same pointer and
+ * stride).  fp32 sums in an order that does not depend on scheduling.
+ */
+int scmoe_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int32_t dtype,
+                              const float* gamma, const float* mean, const float* rstd,
+                              const void* dsum, int64_t lddsum, int32_t T, int32_t d, void* dx,
+                              int64_t lddx, float* dgamma, float* dbeta, void* workspace,
+                              size_t ws_bytes, void* stream);
+
+/* Bytes of workspace scmoe_balance_loss needs.  `out` is a host pointer. */
+int scmoe_balance_loss_workspace_bytes(int32_t T, int32_t E, size_t* out);
+
+/*
+ * The load-balancing loss of the gate (the "MoE loss" of Tables 8-9, coefficient 0.01; the paper gives
+ * no formula: the reading here is the product of each expert's share of the items and its mean
+ * probability).  Over the N tokens with mask[t] != 0 (mask NULL: all T):
+ *
+ *   load[e]      = items (t, j) with expert_idx[t,j] == e      (before any capacity; int32)
+ *   mean_prob[e] = sum_t probs[t,e] / N
+ *   loss         = coef * E * sum_e load[e] / (k N) * mean_prob[e]
+ *   slope[e]     = dloss / dprobs[t,e] = coef * E * load[e] / (k N) / N, the same for every counted
+ *                  token (the counts have no gradient); scmoe_gate_backward takes it
+ *
+ * probs: [T, E] fp32 as the gate calls write it; expert_idx: [T, k], values outside [0, E) are not
+ * counted; mask: [T] bytes, nothing of a token with mask 0 is read.  N == 0: all results are 0.
+ */
+int scmoe_balance_loss(const float* probs, const int32_t* expert_idx, const uint8_t* mask, int32_t T,
+                       int32_t E, int32_t k, float coef, int32_t* load, float* mean_prob,
+                       float* slope, float* loss, void* workspace, size_t ws_bytes, void* stream);
+
+/* Bytes of workspace scmoe_gate_backward needs.  `out` is a host pointer. */
+int scmoe_gate_backward_workspace_bytes(int32_t T, int32_t d, int32_t E, size_t* out);
+
+/*
+ * Gradient of the gate (Eq. (2)-(4)) and of the input encode, in one pass over x.
+ *
+ *   g[t,e]  = dloss * slope[e] + sum over j with expert_idx[t,j] == e of dgate_w[t,j]   (normalize 0)
+ *   dl[t,e] = probs[t,e] * (g[t,e] - sum_e' probs[t,e'] g[t,e'])
+ *   normalize 1: the gate weights are no part of g; instead dl[t,e] += sum over those j of
+ *             gate_w[t,j] * (dgate_w[t,j] - sum_i gate_w[t,i] dgate_w[t,i])
+ *   dW_g    = sum_t x[t,:]^T dl[t,:],   dbias = sum_t dl[t,:]
+ *   dx[t,:] = dl[t,:] W_g^T + sum over j with dst_row[t,j] >= 0 of dx_perm[dst_row[t,j], :]
+ *
+ * x, W_g, normalize: as in the gate call, probs, expert_idx, gate_w: what it wrote (probs is needed).
+ * dgate_w: [T, k] or NULL (no gradient reaches the weights); slope: [E] of scmoe_balance_loss or NULL
+ * (no loss), at least one of the two; dloss: one fp32 on the device, NULL = 1; gate_w is read with
+ * normalize 1 only.  Items with expert_idx outside [0, E) take no part.
+ * mask: [T] bytes or NULL.  A token with mask 0 has dl = 0 and adds nothing to dW_g and dbias whatever
+ * its x, probs and weights hold; the encode's gradient reaches its dx all the same.
+ * dx_perm, dst_row: the gradient of the packed rows (stride ld_perm) and where scmoe_dispatch put each
+ * item; both NULL: dx is the gate's gradient alone.
+ * dW_g: [d, E] fp32, dbias: [E] or NULL; both overwritten.  dx must not overlap any input.
+ * bf16: the products that make dW_g keep fp32 accuracy; dx is rounded once on store.  Sums in an order that
+ * does not depend on scheduling.
+ */
+int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, const float* W_g, const float* probs,
+                        const int32_t* expert_idx, const float* gate_w, const float* dgate_w,
+                        const float* slope, const float* dloss, const uint8_t* mask, int32_t T,
+                        int32_t d, int32_t E, int32_t k, int32_t normalize, const void* dx_perm,
+                        int64_t ld_perm, const int32_t* dst_row, void* dx, int64_t lddx, float* dW_g,
+                        float* dbias, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Gradient of scmoe_combine; arguments named there mean the same.  dy: [T, d], the gradient of y (and,
+ * as it is, of residual).  With r = dst_row[t*k+j] >= 0 and (c0, c1) = coef[t] (1, 1 without):
+ *
+ *   dy_perm[r, :]  = c1 * gate_w[t*k+j] * dy[t,:]          dbase[t,:] = c0 * dy[t,:]
+ *   dgate_w[t*k+j] = c1 * <dy[t,:], y_perm[r,:]>           (0 for a dropped item)
+ *   dcoef[t]       = (<dy[t,:], base[t,:]>, sum_j gate_w[t*k+j] <dy[t,:], y_perm[r,:]>)
+ *
+ * Each result may be NULL.  y_perm is needed for dgate_w and dcoef, base for dcoef.  Rows of dy_perm
+ * that no item names are left untouched.  dy_perm may be the buffer of y_perm, dbase the one of base
+ * (same pointer and stride).  Every value of dst_row must be unique or -1, as scmoe_dispatch gives them.
+ */
+int scmoe_combine_backward(const void* dy, int64_t lddy, int32_t dtype, const void* y_perm,
+                           int64_t ldyp, const int32_t* dst_row, const float* gate_w, int32_t T,
+                           int32_t d, int32_t k, const void* base, int64_t ldbase, const float* coef,
+                           void* dy_perm, int64_t lddyp, float* dgate_w, void* dbase, int64_t lddbase,
+                           float* dcoef, void* stream);
 
 #ifdef __cplusplus
 }

@@ -24,7 +24,10 @@ EXPORTS = ["scmoe_status_string", "scmoe_last_hip_error", "scmoe_set_gemm_varian
            "scmoe_expert_ffn_workspace_bytes",
            "scmoe_combine", "scmoe_coef_gate", "scmoe_workspace_bytes", "scmoe_layer_forward",
            "scmoe_offload_pool_bytes", "scmoe_layer_forward_offload", "scmoe_offload_begin", "scmoe_offload_finish", "moe_topk_layer_forward",
-           "moe_top2_layer_forward"]
+           "moe_top2_layer_forward",
+           "scmoe_layer_norm", "scmoe_layer_norm_backward_workspace_bytes", "scmoe_layer_norm_backward",
+           "scmoe_balance_loss_workspace_bytes", "scmoe_balance_loss", "scmoe_gate_backward_workspace_bytes",
+           "scmoe_gate_backward", "scmoe_combine_backward"]
 
 
 class Desc(C.Structure):
@@ -93,6 +96,17 @@ def lib():
         _lib.moe_topk_layer_forward.argtypes = [C.POINTER(Desc), vp, i64, C.POINTER(Weights), vp, i64,
                                                 C.POINTER(RoutingOut), vp, sz, vp]
         _lib.moe_top2_layer_forward.argtypes = _lib.moe_topk_layer_forward.argtypes
+        f32 = C.c_float
+        _lib.scmoe_layer_norm.argtypes = [vp, i64, i32, vp, i64, vp, vp, f32, i32, i32, vp, i64, vp, i64, vp, vp, vp]
+        _lib.scmoe_layer_norm_backward_workspace_bytes.argtypes = [i32, i32, C.POINTER(sz)]
+        _lib.scmoe_layer_norm_backward.argtypes = [vp, i64, vp, i64, i32, vp, vp, vp, vp, i64, i32, i32, vp, i64, vp, vp, vp, sz, vp]
+        _lib.scmoe_balance_loss_workspace_bytes.argtypes = [i32, i32, C.POINTER(sz)]
+        _lib.scmoe_balance_loss.argtypes = [vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, vp, vp, sz, vp]
+        _lib.scmoe_gate_backward_workspace_bytes.argtypes = [i32, i32, i32, C.POINTER(sz)]
+        _lib.scmoe_gate_backward.argtypes = [vp, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i64, vp, vp,
+                                             i64, vp, vp, vp, sz, vp]
+        _lib.scmoe_combine_backward.argtypes = [vp, i64, i32, vp, i64, vp, vp, i32, i32, i32, vp, i64, vp, vp, i64, vp, vp, i64, vp,
+                                                vp]
     return _lib
 
 
@@ -321,3 +335,112 @@ def moe_top2_layer_forward(desc, x, weights, y, workspace, routing=None, stream=
         C.byref(desc), _ptr(x), _ld(x), C.byref(weights), _ptr(y), _ld(y),
         None if routing is None else C.byref(routing), _ptr(workspace),
         workspace.numel() * workspace.element_size(), _stream(stream)), "moe_top2_layer_forward")
+
+
+def _rows_like(x, *others):
+    """Activations of one call: the same shape and type as x (None: not given)."""
+    for t in others:
+        if t is not None and (t.dtype != x.dtype or t.shape != x.shape):
+            raise TypeError("expected %s of %s, got %s of %s" % (tuple(x.shape), x.dtype, tuple(t.shape), t.dtype))
+
+
+def _packed_like(x, *others):
+    """Packed rows: the width and the type of x."""
+    for t in others:
+        if t is not None and (t.dtype != x.dtype or t.dim() != 2 or t.shape[1] != x.shape[1]):
+            raise TypeError("expected rows of %d %s, got %s of %s" % (x.shape[1], x.dtype, tuple(t.shape), t.dtype))
+
+
+def _dense(dtype, *pairs):
+    """Pairs of a tensor (or None) and the number of elements it must have: dense and of that type."""
+    for t, n in pairs:
+        if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
+            raise TypeError("expected %d contiguous %s, got %s of %s" % (n, dtype, tuple(t.shape), t.dtype))
+
+
+def _mask(mask, T):
+    """One byte per token: torch.bool or torch.uint8."""
+    if mask is not None:
+        _dense(torch.bool if mask.dtype == torch.bool else torch.uint8, (mask, T))
+
+
+def _nbytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def scmoe_layer_norm(x, gamma, beta, eps, y, residual=None, sum_out=None, mean=None, rstd=None, stream=None):
+    """y = norm(x + residual) * gamma + beta; sum_out takes x + residual, mean and rstd what the backward pass needs."""
+    T, d = x.shape
+    _rows_like(x, y, residual, sum_out)
+    _dense(torch.float32, (gamma, d), (beta, d), (mean, T), (rstd, T))
+    _check(lib().scmoe_layer_norm(_ptr(x), _ld(x), dtype_code(x), _ptr(residual), _ld(residual), _ptr(gamma), _ptr(beta), eps, T, d,
+                                  _ptr(sum_out), _ld(sum_out), _ptr(y), _ld(y), _ptr(mean), _ptr(rstd), _stream(stream)),
+           "scmoe_layer_norm")
+
+
+def scmoe_layer_norm_backward_workspace_bytes(T, d):
+    out = C.c_size_t(0)
+    _check(lib().scmoe_layer_norm_backward_workspace_bytes(T, d, C.byref(out)), "scmoe_layer_norm_backward_workspace_bytes")
+    return out.value
+
+
+def scmoe_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, workspace=None, dsum=None, stream=None):
+    """dx, dgamma and dbeta of scmoe_layer_norm; x is what was normed, dsum the gradient that reaches it beside the norm."""
+    T, d = x.shape
+    _rows_like(x, dy, dx, dsum)
+    _dense(torch.float32, (gamma, d), (mean, T), (rstd, T), (dgamma, d), (dbeta, d))
+    _check(lib().scmoe_layer_norm_backward(_ptr(dy), _ld(dy), _ptr(x), _ld(x), dtype_code(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
+                                           _ptr(dsum), _ld(dsum), T, d, _ptr(dx), _ld(dx), _ptr(dgamma), _ptr(dbeta),
+                                           _ptr(workspace), _nbytes(workspace), _stream(stream)), "scmoe_layer_norm_backward")
+
+
+def scmoe_balance_loss_workspace_bytes(T, E):
+    out = C.c_size_t(0)
+    _check(lib().scmoe_balance_loss_workspace_bytes(T, E, C.byref(out)), "scmoe_balance_loss_workspace_bytes")
+    return out.value
+
+
+def scmoe_balance_loss(probs, expert_idx, k, coef, load, mean_prob, slope, loss, workspace, mask=None, stream=None):
+    """Loss, items per expert and the loss's slope in every counted token's probabilities."""
+    T, E = probs.shape
+    _dense(torch.float32, (probs, T * E), (mean_prob, E), (slope, E), (loss, 1))
+    _dense(torch.int32, (expert_idx, T * k), (load, E))
+    _mask(mask, T)
+    _check(lib().scmoe_balance_loss(_ptr(probs), _ptr(expert_idx), _ptr(mask), T, E, k, coef, _ptr(load), _ptr(mean_prob), _ptr(slope),
+                                    _ptr(loss), _ptr(workspace), _nbytes(workspace), _stream(stream)), "scmoe_balance_loss")
+
+
+def scmoe_gate_backward_workspace_bytes(T, d, E):
+    out = C.c_size_t(0)
+    _check(lib().scmoe_gate_backward_workspace_bytes(T, d, E, C.byref(out)), "scmoe_gate_backward_workspace_bytes")
+    return out.value
+
+
+def scmoe_gate_backward(x, W_g, probs, expert_idx, gate_w, dgate_w, dx, dW_g, dbias, workspace, k=1, normalize=0, slope=None, dloss=None,
+                        mask=None, dx_perm=None, dst_row=None, stream=None):
+    """dx, dW_g and dbias from the gradient of the gate weights, the balance loss's slope (times dloss) and the gradient of
+    the packed rows."""
+    T, d = x.shape
+    E = W_g.shape[1]
+    _rows_like(x, dx)
+    _packed_like(x, dx_perm)
+    _dense(torch.float32, (W_g, d * E), (probs, T * E), (gate_w, T * k), (dgate_w, T * k), (dW_g, d * E), (dbias, E), (slope, E), (dloss, 1))
+    _dense(torch.int32, (expert_idx, T * k), (dst_row, T * k))
+    _mask(mask, T)
+    _check(lib().scmoe_gate_backward(_ptr(x), _ld(x), dtype_code(x), _ptr(W_g), _ptr(probs), _ptr(expert_idx), _ptr(gate_w), _ptr(dgate_w),
+                                     _ptr(slope), _ptr(dloss), _ptr(mask), T, d, E, k, normalize, _ptr(dx_perm), _ld(dx_perm),
+                                     _ptr(dst_row), _ptr(dx), _ld(dx), _ptr(dW_g), _ptr(dbias), _ptr(workspace), _nbytes(workspace),
+                                     _stream(stream)), "scmoe_gate_backward")
+
+
+def scmoe_combine_backward(dy, y_perm, dst_row, gate_w, k, dy_perm=None, dgate_w=None, base=None, coef=None, dbase=None, dcoef=None,
+                           stream=None):
+    """What reaches the packed rows, the gate weights, the shared expert's rows and the coefficients (each may be None)."""
+    T, d = dy.shape
+    _rows_like(dy, base, dbase)
+    _packed_like(dy, y_perm, dy_perm)
+    _dense(torch.float32, (gate_w, T * k), (dgate_w, T * k), (coef, 2 * T), (dcoef, 2 * T))
+    _dense(torch.int32, (dst_row, T * k))
+    _check(lib().scmoe_combine_backward(_ptr(dy), _ld(dy), dtype_code(dy), _ptr(y_perm), _ld(y_perm), _ptr(dst_row), _ptr(gate_w), T, d, k,
+                                        _ptr(base), _ld(base), _ptr(coef), _ptr(dy_perm), _ld(dy_perm), _ptr(dgate_w), _ptr(dbase),
+                                        _ld(dbase), _ptr(dcoef), _stream(stream)), "scmoe_combine_backward")

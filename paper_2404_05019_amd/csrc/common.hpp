@@ -166,6 +166,10 @@ inline int64_t padded_ld(int64_t width, int dtype) {
   const int64_t eb = elem_bytes(dtype);
   return ((width * eb) % 512 == 0) ? width + 128 / eb : width;
 }
+// a[0, na), b[0, nb) = sums over n parts of `stride` floats (a multiple of 4) that hold them one behind the other, in an
+// order that does not depend on scheduling; a or b may be nullptr, n may be 0.
+int sum_parts(const float* parts, int n, int64_t stride, float* a, int64_t na, float* b, int64_t nb, hipStream_t stream);
+
 bool ffn_mfma_supported(int d, int F);
 bool ffn_joint_second_fits(int T, int rows, int d, int F, int E, int64_t ldh, int64_t ldw2);   // sizes that the joint second GEMM takes
 bool ffn_second_in_one_launch(int T, int rows, int d, int F, int E);   // top-1 layer: both second GEMMs as one launch and the combine kernel

@@ -1,0 +1,350 @@
+// Layer norm over the model width and its gradient.
+//
+//   mean = sum(h) / d,  rstd = (sum((h - mean)^2) / d + eps)^(-1/2),  xh = (h - mean) rstd,  y = xh gamma + beta
+//   g = dy gamma:  dh = rstd (g - sum(g) / d - xh sum(g xh) / d);  dgamma = sum over rows of dy xh;  dbeta = sum of dy
+//
+// Bound by HBM: a row is read once, kept in registers (the squares are summed about the mean in a second walk over
+// them, so that a large mean costs no digits) and written once.  All arithmetic in fp32.
+#include "rows.hpp"
+
+namespace scmoe {
+
+struct NormArgs {
+  const unsigned char* x; int64_t ldx;           // strides in bytes
+  const unsigned char* residual; int64_t ldres;  // added to x; nullptr: none
+  unsigned char* sum; int64_t ldsum;
+  const float* gamma; const float* beta;         // nullptr: 1, 0
+  float eps;
+  int T, d;
+  unsigned char* y; int64_t ldy;
+  float* mean; float* rstd;                      // nullptr: not kept
+};
+
+struct NormGradArgs {
+  const unsigned char* dy; int64_t lddy;         // strides in bytes
+  const unsigned char* x; int64_t ldx;
+  const float* gamma; const float* mean; const float* rstd;
+  const unsigned char* dsum; int64_t lddsum;     // added to the gradient; nullptr: none
+  int T, d;
+  unsigned char* dx; int64_t lddx;
+  float* parts; int64_t stride;                  // one part per workgroup: dgamma [d], dbeta [d]; nullptr: neither is wanted
+};
+
+// A row belongs to W waves, a lane to V of its values (V / 8 or V / 4 pieces of 16 bytes, 64 W pieces apart).
+// W = 1: four rows per workgroup and no barrier.
+constexpr int norm_threads(int W) { return W == 1 ? 256 : 64 * W; }
+
+// Sums of two values over the waves of a row.  `turn` alternates between calls: one barrier each is enough.
+template <int W>
+__device__ __forceinline__ void row_sums(float& a, float& b, float2 (*s)[W], int turn) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  if (W > 1) {
+    if ((threadIdx.x & 63) == 0) s[turn][threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float2 p = s[turn][w];
+      a += p.x;
+      b += p.y;
+    }
+  }
+}
+
+template <bool BF16, int V, int W>
+__global__ __launch_bounds__(norm_threads(W)) void layer_norm_kernel(NormArgs a) {
+  constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = 64 * W;
+  __shared__ float2 s[2][W];
+  const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int pieces = a.d / NV;
+  for (int64_t row = W == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6) : blockIdx.x; row < a.T;
+       row += static_cast<int64_t>(gridDim.x) * (W == 1 ? 4 : 1)) {
+    uint4 q[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) q[p] = load16(a.x + row * a.ldx + static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16);
+    if (a.residual != nullptr) {
+      uint4 r[P];
+#pragma unroll
+      for (int p = 0; p < P; ++p) r[p] = load16(a.residual + row * a.ldres + static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16);
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        float v[NV], u[NV];
+        unpack16<BF16>(q[p], v);
+        unpack16<BF16>(r[p], u);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] += u[i];
+        q[p] = pack16<BF16>(v);       // what is normed is what is stored: the backward pass reads the stored sum
+        if (lane + p * STEP < pieces) store16(a.sum + row * a.ldsum + static_cast<int64_t>(lane + p * STEP) * 16, q[p]);
+      }
+    }
+    float v[V];
+    float sum = 0.0f, none = 0.0f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      unpack16<BF16>(zero_unless(lane + p * STEP < pieces, q[p]), v + p * NV);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) sum += v[p * NV + i];
+    }
+    row_sums<W>(sum, none, s, 0);
+    const float inv = 1.0f / static_cast<float>(a.d);
+    const float mean = sum * inv;
+    float sq = 0.0f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const bool in = lane + p * STEP < pieces;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const float c = v[p * NV + i] - mean;
+        v[p * NV + i] = c;
+        sq += in ? c * c : 0.0f;
+      }
+    }
+    row_sums<W>(sq, none, s, 1);
+    const float rstd = 1.0f / sqrtf(sq * inv + a.eps);
+    if (lane == 0) {
+      if (a.mean != nullptr) a.mean[row] = mean;
+      if (a.rstd != nullptr) a.rstd[row] = rstd;
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = lane + p * STEP;
+      if (c >= pieces) continue;
+      float o[NV];
+#pragma unroll
+      for (int i = 0; i < NV; i += 4) {
+        const float4 g = a.gamma == nullptr ? make_float4(1.0f, 1.0f, 1.0f, 1.0f) : *reinterpret_cast<const float4*>(a.gamma + c * NV + i);
+        const float4 b = a.beta == nullptr ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : *reinterpret_cast<const float4*>(a.beta + c * NV + i);
+        const float* t = v + p * NV + i;
+        o[i] = fmaf(t[0] * rstd, g.x, b.x);
+        o[i + 1] = fmaf(t[1] * rstd, g.y, b.y);
+        o[i + 2] = fmaf(t[2] * rstd, g.z, b.z);
+        o[i + 3] = fmaf(t[3] * rstd, g.w, b.w);
+      }
+      store16(a.y + row * a.ldy + static_cast<int64_t>(c) * 16, pack16<BF16>(o));
+    }
+  }
+}
+
+// Every workgroup takes every gridDim.x-th row (group of four rows); a lane's columns are the same in all of them, so
+// dgamma and dbeta are summed in registers and leave as one part per workgroup.
+template <bool BF16, int V, int W>
+__global__ __launch_bounds__(norm_threads(W)) void layer_norm_backward_kernel(NormGradArgs a) {
+  constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = 64 * W, ROWS = W == 1 ? 4 : 1;
+  __shared__ float2 s[2][W];
+  extern __shared__ __attribute__((aligned(16))) float cols[];   // W == 1: [2][d]
+  const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int pieces = a.d / NV;
+  const float inv = 1.0f / static_cast<float>(a.d);
+  float g[V], ag[V], ab[V];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int c = min(lane + p * STEP, pieces - 1);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      g[p * NV + i] = a.gamma == nullptr ? 1.0f : a.gamma[c * NV + i];
+      ag[p * NV + i] = ab[p * NV + i] = 0.0f;
+    }
+  }
+  int turn = 0;
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + (W == 1 ? threadIdx.x >> 6 : 0); row < a.T;
+       row += static_cast<int64_t>(gridDim.x) * ROWS) {
+    uint4 qx[P], qy[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int64_t c = static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16;
+      qx[p] = load16(a.x + row * a.ldx + c);
+      qy[p] = load16(a.dy + row * a.lddy + c);
+    }
+    uint4 qs[P];
+    if (a.dsum != nullptr) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) qs[p] = load16(a.dsum + row * a.lddsum + static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16);
+    }
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const bool in = lane + p * STEP < pieces;
+      float x[NV], y[NV];
+      unpack16<BF16>(zero_unless(in, qx[p]), x);
+      unpack16<BF16>(zero_unless(in, qy[p]), y);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const float xh = (x[i] - mean) * rstd, gy = y[i] * g[p * NV + i];
+        s1 += gy;
+        s2 = fmaf(gy, xh, s2);
+        ag[p * NV + i] = fmaf(y[i], xh, ag[p * NV + i]);
+        ab[p * NV + i] += y[i];
+      }
+    }
+    row_sums<W>(s1, s2, s, turn);
+    turn ^= 1;
+    s1 *= inv;
+    s2 *= inv;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = lane + p * STEP;
+      if (c >= pieces) continue;
+      float x[NV], y[NV], r[NV];
+      unpack16<BF16>(qx[p], x);
+      unpack16<BF16>(qy[p], y);
+      if (a.dsum != nullptr) {
+        unpack16<BF16>(qs[p], r);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) r[i] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const float xh = (x[i] - mean) * rstd;
+        r[i] = fmaf(rstd, (y[i] * g[p * NV + i] - s1) - xh * s2, r[i]);
+      }
+      store16(a.dx + row * a.lddx + static_cast<int64_t>(c) * 16, pack16<BF16>(r));
+    }
+  }
+  if (a.parts == nullptr) return;
+  float* part = a.parts + blockIdx.x * a.stride;
+  if (W == 1) {
+    // the four waves hold sums of the same columns: added in the waves' order
+    for (int w = 0; w < 4; ++w) {
+      if (static_cast<int>(threadIdx.x >> 6) == w) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const int c = lane + p * STEP;
+          if (c >= pieces) continue;
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            cols[c * NV + i] = ag[p * NV + i] + (w == 0 ? 0.0f : cols[c * NV + i]);
+            cols[a.d + c * NV + i] = ab[p * NV + i] + (w == 0 ? 0.0f : cols[a.d + c * NV + i]);
+          }
+        }
+      }
+      __syncthreads();
+    }
+    for (int i = threadIdx.x; i < a.d / 2; i += 256) reinterpret_cast<float4*>(part)[i] = reinterpret_cast<const float4*>(cols)[i];
+  } else {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int c = lane + p * STEP;
+      if (c >= pieces) continue;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        part[c * NV + i] = ag[p * NV + i];
+        part[a.d + c * NV + i] = ab[p * NV + i];
+      }
+    }
+  }
+}
+
+// Workgroups of the backward kernel: two per compute unit, each with a part of 8 d bytes to leave.
+static int norm_grad_groups(int T, int d) {
+  const int rows = d <= 2048 ? 4 : 1;
+  const int64_t most = (static_cast<int64_t>(T) + rows - 1) / rows;
+  const int cap = 2 * num_cus();
+  return static_cast<int>(most < cap ? most : cap);
+}
+
+constexpr int64_t NORM_MAX_GROUPS = 1 << 20;   // keeps the threads of a launch under 2^32; more rows than that take turns
+
+#define SCMOE_NORM_SIZES(LAUNCH)                    \
+  if (d <= 512) LAUNCH(8, 1);                       \
+  else if (d <= 1024) LAUNCH(16, 1);                \
+  else if (d <= 2048) LAUNCH(32, 1);                \
+  else if (d <= 4096) LAUNCH(16, 4);                \
+  else if (d <= 8192) LAUNCH(32, 4);                \
+  else LAUNCH(32, 8)
+
+static int layer_norm(const NormArgs& a, int dtype, hipStream_t stream) {
+  const int d = a.d;
+#define SCMOE_NORM(V, W)                                                                                                  \
+  do {                                                                                                                    \
+    const int64_t groups = W == 1 ? (static_cast<int64_t>(a.T) + 3) / 4 : a.T;                                            \
+    dim3 grid(static_cast<unsigned>(groups < NORM_MAX_GROUPS ? groups : NORM_MAX_GROUPS)), block(norm_threads(W));        \
+    if (dtype == SCMOE_BF16) hipLaunchKernelGGL((layer_norm_kernel<true, V, W>), grid, block, 0, stream, a);             \
+    else hipLaunchKernelGGL((layer_norm_kernel<false, V, W>), grid, block, 0, stream, a);                                \
+  } while (0)
+  SCMOE_NORM_SIZES(SCMOE_NORM);
+#undef SCMOE_NORM
+  return launch_status();
+}
+
+static int layer_norm_backward(const NormGradArgs& a, int dtype, int groups, hipStream_t stream) {
+  const int d = a.d;
+#define SCMOE_NORM(V, W)                                                                                                  \
+  do {                                                                                                                    \
+    const size_t lds = W == 1 && a.parts != nullptr ? static_cast<size_t>(d) * 8 : 0;                                    \
+    dim3 grid(groups), block(norm_threads(W));                                                                            \
+    if (dtype == SCMOE_BF16) hipLaunchKernelGGL((layer_norm_backward_kernel<true, V, W>), grid, block, lds, stream, a);  \
+    else hipLaunchKernelGGL((layer_norm_backward_kernel<false, V, W>), grid, block, lds, stream, a);                     \
+  } while (0)
+  SCMOE_NORM_SIZES(SCMOE_NORM);
+#undef SCMOE_NORM
+  return launch_status();
+}
+
+static int norm_shape(int dtype, int T, int d) {
+  if (!dtype_ok(dtype)) return SCMOE_ERR_DTYPE;
+  if (T < 0 || d <= 0 || d % 8 != 0 || d > SCMOE_MAX_NORM_WIDTH) return SCMOE_ERR_SHAPE;
+  return SCMOE_OK;
+}
+
+}  // namespace scmoe
+
+extern "C" int scmoe_layer_norm(const void* x, int64_t ldx, int32_t dtype, const void* residual, int64_t ldres, const float* gamma,
+                                const float* beta, float eps, int32_t T, int32_t d, void* sum, int64_t ldsum, void* y, int64_t ldy,
+                                float* mean, float* rstd, void* stream) {
+  using namespace scmoe;
+  if (const int st = norm_shape(dtype, T, d)) return st;
+  if (!(eps > 0.0f) || isinf(eps)) return SCMOE_ERR_ARG;
+  if (T == 0) return SCMOE_OK;
+  if (!x || !y || (residual != nullptr) != (sum != nullptr)) return SCMOE_ERR_NULL;
+  if (!view_ok(x, ldx, d, dtype) || !view_ok(y, ldy, d, dtype) || !aligned16(gamma) || !aligned16(beta)) return SCMOE_ERR_SHAPE;
+  if (residual && (!view_ok(residual, ldres, d, dtype) || !view_ok(sum, ldsum, d, dtype))) return SCMOE_ERR_SHAPE;
+  const int eb = elem_bytes(dtype);
+  NormArgs a = {};
+  a.x = static_cast<const unsigned char*>(x); a.ldx = ldx * eb;
+  a.residual = static_cast<const unsigned char*>(residual); a.ldres = ldres * eb;
+  a.sum = static_cast<unsigned char*>(sum); a.ldsum = ldsum * eb;
+  a.gamma = gamma; a.beta = beta; a.eps = eps; a.T = T; a.d = d;
+  a.y = static_cast<unsigned char*>(y); a.ldy = ldy * eb;
+  a.mean = mean; a.rstd = rstd;
+  return layer_norm(a, dtype, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int scmoe_layer_norm_backward_workspace_bytes(int32_t T, int32_t d, size_t* out) {
+  using namespace scmoe;
+  if (!out) return SCMOE_ERR_NULL;
+  if (const int st = norm_shape(SCMOE_F32, T, d)) return st;
+  *out = static_cast<size_t>(norm_grad_groups(T, d)) * d * 8;
+  return SCMOE_OK;
+}
+
+extern "C" int scmoe_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int32_t dtype, const float* gamma,
+                                         const float* mean, const float* rstd, const void* dsum, int64_t lddsum, int32_t T, int32_t d,
+                                         void* dx, int64_t lddx, float* dgamma, float* dbeta, void* workspace, size_t ws_bytes,
+                                         void* stream) {
+  using namespace scmoe;
+  if (const int st = norm_shape(dtype, T, d)) return st;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  const bool sums = dgamma != nullptr || dbeta != nullptr;
+  if (T == 0) return sums ? sum_parts(nullptr, 0, 0, dgamma, d, dbeta, d, hs) : SCMOE_OK;
+  if (!dy || !x || !mean || !rstd || !dx || (sums && !workspace)) return SCMOE_ERR_NULL;
+  if (!view_ok(dy, lddy, d, dtype) || !view_ok(x, ldx, d, dtype) || !view_ok(dx, lddx, d, dtype) || !aligned16(gamma)) return SCMOE_ERR_SHAPE;
+  if (dsum && !view_ok(dsum, lddsum, d, dtype)) return SCMOE_ERR_SHAPE;
+  const int groups = norm_grad_groups(T, d);
+  if (sums && !aligned16(workspace)) return SCMOE_ERR_SHAPE;
+  if (sums && ws_bytes < static_cast<size_t>(groups) * d * 8) return SCMOE_ERR_WORKSPACE;
+  const int eb = elem_bytes(dtype);
+  NormGradArgs a = {};
+  a.dy = static_cast<const unsigned char*>(dy); a.lddy = lddy * eb;
+  a.x = static_cast<const unsigned char*>(x); a.ldx = ldx * eb;
+  a.gamma = gamma; a.mean = mean; a.rstd = rstd;
+  a.dsum = static_cast<const unsigned char*>(dsum); a.lddsum = lddsum * eb;
+  a.T = T; a.d = d;
+  a.dx = static_cast<unsigned char*>(dx); a.lddx = lddx * eb;
+  a.parts = sums ? static_cast<float*>(workspace) : nullptr;
+  a.stride = 2 * static_cast<int64_t>(d);
+  if (const int st = layer_norm_backward(a, dtype, groups, hs)) return st;
+  return sums ? sum_parts(a.parts, groups, a.stride, dgamma, d, dbeta, d, hs) : SCMOE_OK;
+}

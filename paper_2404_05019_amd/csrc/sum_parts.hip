@@ -1,0 +1,57 @@
+// Adds up the partial sums that the workgroups of a gradient kernel leave in the workspace.  A second launch in
+// place of floating-point atomics: the order of the sum is fixed, so the gradient has the same bits in every run.
+#include "common.hpp"
+
+namespace scmoe {
+
+constexpr int SUM_SLICES = 64;   // threads that share a column group, each with every 64th part
+constexpr int SUM_QUADS = 4;     // 16-byte column groups per workgroup: 64 bytes of every part
+
+// parts: [n][stride] fp32, stride a multiple of 4.  Columns [0, na) go to a, columns [na, na + nb) to b.
+__global__ __launch_bounds__(SUM_SLICES * SUM_QUADS) void sum_parts_kernel(const float* __restrict__ parts, int n, int64_t stride,
+                                                                           float* __restrict__ a, int64_t na, float* __restrict__ b,
+                                                                           int64_t nb) {
+  __shared__ float4 s[SUM_SLICES][SUM_QUADS];
+  const int quad = threadIdx.x % SUM_QUADS, slice = threadIdx.x / SUM_QUADS;
+  const int64_t col = (static_cast<int64_t>(blockIdx.x) * SUM_QUADS + quad) * 4;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (col < stride) {
+#pragma unroll 4
+    for (int i = slice; i < n; i += SUM_SLICES) {
+      const float4 q = *reinterpret_cast<const float4*>(parts + i * stride + col);
+      v.x += q.x;
+      v.y += q.y;
+      v.z += q.z;
+      v.w += q.w;
+    }
+  }
+  s[slice][quad] = v;
+  __syncthreads();
+#pragma unroll
+  for (int half = SUM_SLICES / 2; half > 0; half >>= 1) {
+    if (slice < half) {
+      const float4 p = s[slice][quad], q = s[slice + half][quad];
+      s[slice][quad] = make_float4(p.x + q.x, p.y + q.y, p.z + q.z, p.w + q.w);
+    }
+    __syncthreads();
+  }
+  if (slice < 4) {
+    const int64_t c = col + slice;
+    const float4 q = s[0][quad];
+    const float r = slice == 0 ? q.x : slice == 1 ? q.y : slice == 2 ? q.z : q.w;
+    if (c < na) {
+      if (a != nullptr) a[c] = r;
+    } else if (c < na + nb) {
+      if (b != nullptr) b[c - na] = r;
+    }
+  }
+}
+
+int sum_parts(const float* parts, int n, int64_t stride, float* a, int64_t na, float* b, int64_t nb, hipStream_t stream) {
+  const int64_t quads = (na + nb + 3) / 4;
+  dim3 grid(static_cast<unsigned>((quads + SUM_QUADS - 1) / SUM_QUADS)), block(SUM_SLICES * SUM_QUADS);
+  hipLaunchKernelGGL(sum_parts_kernel, grid, block, 0, stream, parts, n, stride, a, na, b, nb);
+  return launch_status();
+}
+
+}  // namespace scmoe
