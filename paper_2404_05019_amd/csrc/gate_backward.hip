@@ -125,14 +125,15 @@ static size_t loss_bytes(int T, int E) {
 
 // ---- gradient of the gate -------------------------------------------------------------------------
 
-constexpr int GG_COLS = 128;     // columns of a workgroup: 8 per lane, 16 lanes
-constexpr int GG_TOKENS = 16;    // tokens of a wave's step
+constexpr int GG_TOK = 16;       // tokens of a wave's step
+static_assert(GG_TOK * SCMOE_MAX_TOPK <= 64, "one register holds a step's items");
 
 struct GateGradArgs {
   const unsigned char* x; int64_t ldx;          // strides in bytes
   const float* Wg; const float* probs; const int32_t* idx; const float* gate_w; const float* dgate_w;
   const float* slope; const float* dloss; const uint8_t* mask;
   int T, d, E, k, normalize;
+  int probs16;                                  // rows of probs are 16-byte aligned
   const unsigned char* dxp; int64_t lddxp; const int32_t* dst_row;
   unsigned char* dx; int64_t lddx;
   float* parts; int64_t stride;                 // [splits][d E + E, padded to 4]; one split: dW_g and dbias themselves
@@ -140,187 +141,362 @@ struct GateGradArgs {
   int splits;
 };
 
-// A workgroup has 128 columns and every `splits`-th group of 64 tokens, a wave 16 tokens of it.  Both products run on
-// the fp32 matrix instruction (16 x 16 outputs, k = 4):
-//   dx:   rows = tokens,  k = experts: lane (m, q) holds dl[token m, expert 4 s + q], which it computed
-//   dW_g: rows = columns, k = tokens:  lane (m, q) holds x[token 4 q + s, columns 8 m + j] as it was loaded, and
-//         dl[token 4 q + s, expert m] through LDS
-// Column tile j of a lane's eight is column 8 m + j, so rows of x and dx are moved in 16-byte pieces and nothing is
-// shuffled.  EC: groups of 16 experts.
+// A workgroup has COLS columns and every `splits`-th group of 64 tokens, a wave 16 tokens of it at a time.  Outputs of both
+// products are 16 x 16 tiles of the matrix instructions:
+//   dx:   rows = tokens,  k = experts: lane (m, q) computes dl[token m, S consecutive experts] and holds it as operand
+//   dW_g: rows = columns, k = tokens:  lane (m, q) holds x[tokens 4 q + i, columns NV m + j] as it was loaded (16 bytes), and
+//         dl[tokens 4 q + i, expert m] through LDS
+// Column tile j of a lane's NV is column NV m + j, so rows of x and dx are moved in 16-byte pieces and nothing is
+// shuffled.  fp32: the fp32 instruction (k = 4).  bf16: the bf16 ones (k = 16 and 32, 8 and 16 times the rate):
+//   dx:   dl and W_g each as two bf16 parts, rounded, 2^-16 of the value; the product of the low parts is left out
+//   dW_g: x is bf16; dl in three truncated parts, which hold its 24 bits exactly
+// What the next step reads is loaded ahead of this step's dx, the encode's rows ahead of this step's dW_g.
 template <bool BF16, int EC>
-__global__ __launch_bounds__(256) void gate_backward_kernel(GateGradArgs a) {
-  constexpr int EP = 16 * EC, S = 4 * EC, NV = BF16 ? 8 : 4, PP = 8 / NV, LD = EP + 4;
-  __shared__ __attribute__((aligned(16))) float ws[EP * GG_COLS];        // W_g transposed: [expert][column]; later sums of dW_g
-  __shared__ __attribute__((aligned(16))) float dls[4][GG_TOKENS * LD];  // dl of each wave's tokens
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, q = lane >> 4;
-  const int split = blockIdx.x % a.splits, c0 = (blockIdx.x / a.splits) * GG_COLS;
-  const int cols = min(GG_COLS, a.d - c0);
-  for (int i = tid; i < EP * GG_COLS; i += 256) {
-    const int c = i / EP, e = i % EP;
-    ws[e * GG_COLS + c] = c < cols && e < a.E ? a.Wg[static_cast<int64_t>(c0 + c) * a.E + e] : 0.0f;
+struct GateGradCfg {
+  static constexpr int EP = 16 * EC;                                 // experts, padded
+  static constexpr int S = EP / 4;                                   // experts of a lane
+  static constexpr int NV = BF16 ? 8 : 4, COLS = 16 * NV;
+  static constexpr int KB = EC == 4 ? 2 : 1;                         // bf16: k blocks of dx
+  static constexpr int KS = EC == 1 ? 4 : 8;                         // and values of a lane in one
+  static constexpr int LD = GG_TOK + 4;                              // floats per expert of the dl buffer
+  static constexpr int W_BYTES = EP * COLS * 4;
+  static constexpr int SUM_BYTES = 4 * COLS * 16 * 4;                // dW_g of four waves, 16 experts
+  static constexpr int LDS = W_BYTES + 16 * EP * LD > SUM_BYTES ? W_BYTES + 16 * EP * LD : SUM_BYTES;
+};
+
+// What a step reads.
+template <bool BF16, int EC>
+struct GateGradStep {
+  uint4 x[4];                          // tokens 4 q + i
+  float p[GateGradCfg<BF16, EC>::S];   // token m
+  int idx, dst;                        // item `lane` of the step's 16 k
+  float add, w;                        // its dgate_w, its gate_w
+  uint32_t use;                        // tokens that count, one bit each
+};
+
+template <bool BF16, int EC, int K, bool DISPATCH>
+__device__ __forceinline__ void gate_grad_load(const GateGradArgs& a, int64_t t0, int64_t col_byte, int lane, GateGradStep<BF16, EC>& n) {
+  using C = GateGradCfg<BF16, EC>;
+  const int m = lane & 15, q = lane >> 4;
+  const int left = a.T - t0 < GG_TOK ? static_cast<int>(a.T - t0) : GG_TOK;   // tokens of this step
+  const int mine = min(m, left - 1);
+  const bool on = m < left && (a.mask == nullptr || a.mask[t0 + mine] != 0);
+  n.use = static_cast<uint32_t>(__ballot(on)) & 0xffffu;
+  // items of this step in the order of memory: the expert and what it adds to g (to dl itself with normalize)
+  const int at = min(lane, left * K - 1);
+  n.idx = n.dst = -1;
+  n.add = 0.0f;
+  if (DISPATCH) {
+    const int r = a.dst_row[t0 * K + at];
+    n.dst = lane < left * K ? r : -1;
   }
-  __syncthreads();
-  const int col = c0 + min(8 * m, cols - 8);          // this lane's columns (lanes past the end move what they do not use)
-  const bool in = 8 * m < cols;
+  if (a.dgate_w != nullptr) {
+    const int e = a.idx[t0 * K + at];
+    n.idx = lane < left * K && e < a.E ? e : -1;
+    n.add = a.dgate_w[t0 * K + at];
+    if (a.normalize) n.w = a.gate_w[t0 * K + at];
+  }
+  const float* row = a.probs + (t0 + mine) * a.E;
+  if (a.probs16) {
+#pragma unroll
+    for (int s = 0; s < C::S; s += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(row + min(C::S * q + s, a.E - 4));
+      n.p[s] = v.x;
+      n.p[s + 1] = v.y;
+      n.p[s + 2] = v.z;
+      n.p[s + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int s = 0; s < C::S; ++s) n.p[s] = row[min(C::S * q + s, a.E - 1)];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) n.x[i] = load16(a.x + (t0 + min(4 * q + i, left - 1)) * a.ldx + col_byte);
+}
+
+template <int N>
+union Bf16Parts {
+  uint32_t w[N / 2];
+  __bf16 __attribute__((ext_vector_type(N))) v;
+  short __attribute__((ext_vector_type(N))) s;
+};
+
+template <int N>
+__device__ __forceinline__ f32x4_t mfma_bf16(const Bf16Parts<N>& a, const Bf16Parts<N>& b, f32x4_t c) {
+  if constexpr (N == 4) return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a.s, b.s, c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+
+// Two parts, rounded.
+template <int N>
+__device__ __forceinline__ void split2(const float* v, Bf16Parts<N>& hi, Bf16Parts<N>& lo) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    hi.w[i] = cvt_pk_bf16(v[2 * i], v[2 * i + 1]);
+    lo.w[i] = cvt_pk_bf16(v[2 * i] - __uint_as_float(hi.w[i] << 16), v[2 * i + 1] - __uint_as_float(hi.w[i] & 0xffff0000u));
+  }
+}
+
+// The high (low) halves of two words, the first one's in the low half.
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+
+// Three parts, truncated: their sum is the value.
+__device__ __forceinline__ void split3(const float* v, Bf16Parts<4> (&part)[3]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float a = v[2 * i], b = v[2 * i + 1];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      part[p].w[i] = high_halves(__float_as_uint(a), __float_as_uint(b));
+      a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+      b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+    }
+  }
+}
+
+// Rows of the encode's gradient for choice j of tokens 4 q + i, as far as they were kept.
+template <int K>
+__device__ __forceinline__ uint32_t gate_grad_rows(const GateGradArgs& a, int64_t t0, int64_t col_byte, int q, int dst, int j, uint4 (&dp)[4]) {
+  uint32_t have = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = __shfl(dst, (4 * q + i) * K + j, 64);
+    have |= r >= 0 ? 1u << i : 0u;
+    // (no row: the x of the step's first token, which is there)
+    const unsigned char* row = r >= 0 ? a.dxp + r * a.lddxp : a.x + t0 * a.ldx;
+    dp[i] = load16(row + col_byte);
+  }
+  return have;
+}
+
+template <bool BF16, int EC, int K, bool DISPATCH>
+__global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(GateGradArgs a) {
+  using C = GateGradCfg<BF16, EC>;
+  constexpr int EP = C::EP, S = C::S, LD = C::LD, NV = C::NV, COLS = C::COLS, KB = C::KB, KS = C::KS;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[C::LDS];
+  __shared__ float dbs[4][EP];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, q = lane >> 4;
+  float* const dls = reinterpret_cast<float*>(lds + C::W_BYTES) + wave * EP * LD;   // dl of this wave's tokens: [expert][token]
+  const int split = blockIdx.x % a.splits, c0 = (blockIdx.x / a.splits) * COLS;
+  const int cols = min(COLS, a.d - c0);
+  const bool in = NV * m < cols;                      // (lanes past the end move what they do not use)
+  const int64_t col_byte = static_cast<int64_t>(c0 + min(NV * m, cols - NV)) * (16 / NV);
+  const int64_t step = static_cast<int64_t>(a.splits) * 4 * GG_TOK;
+  int64_t t0 = (static_cast<int64_t>(split) * 4 + wave) * GG_TOK;
+  GateGradStep<BF16, EC> n;
+  if (t0 < a.T) gate_grad_load<BF16, EC, K, DISPATCH>(a, t0, col_byte, lane, n);
+
+  // W_g as operands of dx, in the order in which the lanes read them
+  const float* const wg = a.Wg + static_cast<int64_t>(c0) * a.E;
+  if (BF16) {
+    Bf16Parts<KS>* const wl = reinterpret_cast<Bf16Parts<KS>*>(lds);   // [column tile][part][k block][lane]
+    for (int i = tid; i < NV * KB * 64; i += 256) {
+      const int l = i % 64, kb = i / 64 % KB, j = i / (64 * KB);
+      const int c = NV * (l & 15) + j, e = S * (l >> 4) + KS * kb;
+      float v[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) v[s] = c < cols && e + s < a.E ? wg[c * a.E + e + s] : 0.0f;
+      split2<KS>(v, wl[(j * 2 * KB + kb) * 64 + l], wl[((j * 2 + 1) * KB + kb) * 64 + l]);
+    }
+  } else {
+    float* const wl = reinterpret_cast<float*>(lds);                 // [expert][column]
+    for (int i = tid; i < EP * COLS; i += 256) {
+      const int c = i / EP, e = i % EP;
+      wl[e * COLS + c] = c < cols && e < a.E ? wg[c * a.E + e] : 0.0f;
+    }
+  }
   float slope[S];
 #pragma unroll
-  for (int s = 0; s < S; ++s) {
-    const int e = 4 * s + q;
-    slope[s] = a.slope != nullptr && e < a.E ? a.slope[e] * (a.dloss != nullptr ? a.dloss[0] : 1.0f) : 0.0f;
-  }
-  f32x4_t acc[EC][8];
-  float db[S];
-#pragma unroll
-  for (int c = 0; c < EC; ++c)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[c][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-  for (int s = 0; s < S; ++s) db[s] = 0.0f;
+  for (int s = 0; s < S; ++s) slope[s] = a.slope != nullptr && S * q + s < a.E ? a.slope[S * q + s] * (a.dloss != nullptr ? a.dloss[0] : 1.0f) : 0.0f;
+  __syncthreads();
 
-  for (int64_t t0 = (static_cast<int64_t>(split) * 4 + wave) * GG_TOKENS; t0 < a.T; t0 += static_cast<int64_t>(a.splits) * 4 * GG_TOKENS) {
-    // x of tokens 4 q + s
-    uint4 xq[4][PP];
-    bool use[4];
+  f32x4_t acc[EC][NV];
+  float db[EC];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int64_t t = t0 + 4 * q + s;
-      const int64_t tc = t < a.T ? t : a.T - 1;
+  for (int c = 0; c < EC; ++c) {
+    db[c] = 0.0f;
 #pragma unroll
-      for (int p = 0; p < PP; ++p) xq[s][p] = load16(a.x + tc * a.ldx + static_cast<int64_t>(col) * (BF16 ? 2 : 4) + 16 * p);
-      use[s] = t < a.T && (a.mask == nullptr || a.mask[tc] != 0);
-    }
-    // dl of token m, experts 4 s + q
+    for (int j = 0; j < NV; ++j) acc[c][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  for (; t0 < a.T; t0 += step) {
+    const uint32_t use = n.use;
+    const int dst = n.dst;
+    uint4 dp[4];
+    uint32_t have = 0;
+    if (DISPATCH) have = gate_grad_rows<K>(a, t0, col_byte, q, dst, 0, dp);
+    // dl of token m, experts S q + s
     float dl[S];
     {
-      const int64_t t = t0 + m;
-      const bool on = t < a.T && (a.mask == nullptr || a.mask[t] != 0);
-      float p[S], g[S], own[S];
+      const bool on = (use >> m & 1u) != 0;
+      if (a.normalize) {
+        // in the lanes of the items: dot over their token's items
+        const int first = lane / K * K;
+        const float mine = n.idx >= 0 ? n.w * n.add : 0.0f;
+        float dot = 0.0f;
+#pragma unroll
+        for (int j = 0; j < K; ++j) dot += __shfl(mine, first + j, 64);
+        n.add = n.w * (n.add - dot);
+      }
+      float g[S], own[S];
+#pragma unroll
+      for (int s = 0; s < S; ++s) own[s] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        const int e = __shfl(n.idx, m * K + j, 64);
+        const float v = __shfl(n.add, m * K + j, 64);
+#pragma unroll
+        for (int s = 0; s < S; ++s) own[s] += e >= 0 && e == S * q + s ? v : 0.0f;
+      }
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        g[s] = a.normalize ? slope[s] : slope[s] + own[s];
+        own[s] = a.normalize ? own[s] : 0.0f;
+      }
       float total = 0.0f;
 #pragma unroll
       for (int s = 0; s < S; ++s) {
-        p[s] = on && 4 * s + q < a.E ? a.probs[t * a.E + 4 * s + q] : 0.0f;
-        g[s] = slope[s];
-        own[s] = 0.0f;
+        n.p[s] = on && S * q + s < a.E ? n.p[s] : 0.0f;
+        total = fmaf(n.p[s], g[s], total);
       }
-      if (on && a.dgate_w != nullptr) {
-        float dot = 0.0f;
-        if (a.normalize)
-          for (int j = 0; j < a.k; ++j) {
-            const int e = a.idx[t * a.k + j];
-            if (e >= 0 && e < a.E) dot = fmaf(a.gate_w[t * a.k + j], a.dgate_w[t * a.k + j], dot);
-          }
-        for (int j = 0; j < a.k; ++j) {
-          const int e = a.idx[t * a.k + j];
-          const float dw = a.dgate_w[t * a.k + j];
-          const float v = a.normalize ? a.gate_w[t * a.k + j] * (dw - dot) : dw;
-#pragma unroll
-          for (int s = 0; s < S; ++s)
-            if (e == 4 * s + q) {
-              if (a.normalize) own[s] += v;
-              else g[s] += v;
-            }
-        }
-      }
-#pragma unroll
-      for (int s = 0; s < S; ++s) total = fmaf(p[s], g[s], total);
       total += __shfl_xor(total, 16, 64);
       total += __shfl_xor(total, 32, 64);
 #pragma unroll
       for (int s = 0; s < S; ++s) {
-        dl[s] = on ? fmaf(p[s], g[s] - total, own[s]) : 0.0f;
-        db[s] += dl[s];
-        dls[wave][m * LD + 4 * s + q] = dl[s];
+        dl[s] = on ? fmaf(n.p[s], g[s] - total, own[s]) : 0.0f;
+        dls[(S * q + s) * LD + m] = dl[s];
       }
-    }
-    // dx
-    f32x4_t o[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const float4 w0 = *reinterpret_cast<const float4*>(&ws[(4 * s + q) * GG_COLS + 8 * m]);
-      const float4 w1 = *reinterpret_cast<const float4*>(&ws[(4 * s + q) * GG_COLS + 8 * m + 4]);
-      const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(dl[s], w[j], o[j], 0, 0, 0);
     }
     // dW_g
+    if (use != 0xffffu) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) n.x[i] = zero_unless((use >> (4 * q + i) & 1u) != 0, n.x[i]);
+    }
     wave_lds_order();
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      float v[8];
+    for (int c = 0; c < EC; ++c) {
+      const float4 t = *reinterpret_cast<const float4*>(&dls[(c * 16 + m) * LD + 4 * q]);
+      const float v[4] = {t.x, t.y, t.z, t.w};
+      db[c] += (v[0] + v[1]) + (v[2] + v[3]);
+      if constexpr (BF16) {
+        Bf16Parts<4> part[3];
+        split3(v, part);
 #pragma unroll
-      for (int p = 0; p < PP; ++p) unpack16<BF16>(zero_unless(use[s], xq[s][p]), v + p * NV);
+        for (int j = 0; j < NV; ++j) {
+          uint32_t w[4];
 #pragma unroll
-      for (int c = 0; c < EC; ++c) {
-        const float b = dls[wave][(4 * q + s) * LD + 16 * c + m];
+          for (int i = 0; i < 4; ++i) w[i] = j < 2 ? n.x[i].x : j < 4 ? n.x[i].y : j < 6 ? n.x[i].z : n.x[i].w;
+          Bf16Parts<4> xa;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j], b, acc[c][j], 0, 0, 0);
+          for (int i = 0; i < 2; ++i) xa.w[i] = j & 1 ? high_halves(w[2 * i], w[2 * i + 1]) : low_halves(w[2 * i], w[2 * i + 1]);
+#pragma unroll
+          for (int p = 2; p >= 0; --p) acc[c][j] = mfma_bf16(xa, part[p], acc[c][j]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float xv[NV];
+          unpack16<BF16>(n.x[i], xv);
+#pragma unroll
+          for (int j = 0; j < NV; ++j) acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(xv[j], v[i], acc[c][j], 0, 0, 0);
+        }
       }
     }
     wave_lds_order();
-    // lane (m, q) holds dx of tokens 4 q + i, columns 8 m + j
+    gate_grad_load<BF16, EC, K, DISPATCH>(a, t0 + step < a.T ? t0 + step : t0, col_byte, lane, n);
+    // dx
+    f32x4_t o[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) o[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (BF16) {
+      const Bf16Parts<KS>* const wl = reinterpret_cast<const Bf16Parts<KS>*>(lds) + lane;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        Bf16Parts<KS> hi, lo;
+        split2<KS>(dl + KS * kb, hi, lo);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          const Bf16Parts<KS> wh = wl[(j * 2 * KB + kb) * 64], wo = wl[((j * 2 + 1) * KB + kb) * 64];
+          o[j] = mfma_bf16(hi, wo, o[j]);
+          o[j] = mfma_bf16(lo, wh, o[j]);
+          o[j] = mfma_bf16(hi, wh, o[j]);
+        }
+      }
+    } else {
+      const float4* const wl = reinterpret_cast<const float4*>(lds);
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const float4 t = wl[(S * q + s) * 16 + m];
+        const float w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(dl[s], w[j], o[j], 0, 0, 0);
+      }
+    }
+    // lane (m, q) holds dx of tokens 4 q + i, columns NV m + j
+    if (DISPATCH) {
+#pragma unroll
+      for (int j = 0; j < K; ++j) {
+        if (j > 0) have = gate_grad_rows<K>(a, t0, col_byte, q, dst, j, dp);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float u[NV];
+          unpack16<BF16>(zero_unless((have >> i & 1u) != 0, dp[i]), u);
+#pragma unroll
+          for (int l = 0; l < NV; ++l) o[l][i] += u[l];
+        }
+      }
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int64_t t = t0 + 4 * q + i;
       if (t >= a.T || !in) continue;
-      float v[8];
+      float v[NV];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = o[j][i];
-      if (a.dst_row != nullptr) {
-        for (int j = 0; j < a.k; ++j) {
-          const int64_t r = a.dst_row[t * a.k + j];
-          if (r < 0) continue;
-#pragma unroll
-          for (int p = 0; p < PP; ++p) {
-            float u[NV];
-            unpack16<BF16>(load16(a.dxp + r * a.lddxp + static_cast<int64_t>(col) * (BF16 ? 2 : 4) + 16 * p), u);
-#pragma unroll
-            for (int n = 0; n < NV; ++n) v[p * NV + n] += u[n];
-          }
-        }
-      }
-#pragma unroll
-      for (int p = 0; p < PP; ++p) store16(a.dx + t * a.lddx + static_cast<int64_t>(col) * (BF16 ? 2 : 4) + 16 * p, pack16<BF16>(v + p * NV));
+      for (int j = 0; j < NV; ++j) v[j] = o[j][i];
+      store16(a.dx + t * a.lddx + col_byte, pack16<BF16>(v));
     }
   }
 
-  // Sums of the four waves, in their order.
-  __syncthreads();
-  for (int w = 0; w < 4; ++w) {
-    if (wave == w) {
+  // Sums of the four waves, 16 experts at a time: column NV (4 q + i) + j lies in the order (j, i, q), which 64 lanes write without a
+  // bank conflict.
+  float* const sums = reinterpret_cast<float*>(lds);
 #pragma unroll
-      for (int c = 0; c < EC; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float* to = &ws[(8 * (4 * q + i) + j) * EP + 16 * c + m];   // column 8 (4 q + i) + j, expert 16 c + m
-            *to = acc[c][j][i] + (w == 0 ? 0.0f : *to);
-          }
-#pragma unroll
-      for (int s = 0; s < S; ++s) {
-        float v = db[s];
-#pragma unroll
-        for (int off = 1; off < 16; off <<= 1) v += __shfl_xor(v, off, 64);
-        if (m == 0) dls[0][4 * s + q] = v + (w == 0 ? 0.0f : dls[0][4 * s + q]);
-      }
-    }
-    __syncthreads();
+  for (int c = 0; c < EC; ++c) {
+    float v = db[c];
+    v += __shfl_xor(v, 16, 64);
+    v += __shfl_xor(v, 32, 64);
+    if (q == 0) dbs[wave][16 * c + m] = v;
   }
-  float* dw = a.splits == 1 ? a.dWg : a.parts + split * a.stride;
-  for (int i = tid; i < cols * a.E; i += 256) dw[static_cast<int64_t>(c0) * a.E + i] = ws[(i / a.E) * EP + i % a.E];
-  if (c0 == 0) {
-    float* to = a.splits == 1 ? a.dbias : a.parts + split * a.stride + static_cast<int64_t>(a.d) * a.E;
-    if (to != nullptr)
-      for (int i = tid; i < a.E; i += 256) to[i] = dls[0][i];
+  float* const dw = (a.splits == 1 ? a.dWg : a.parts + split * a.stride) + static_cast<int64_t>(c0) * a.E;
+#pragma unroll
+  for (int c = 0; c < EC; ++c) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sums[wave * COLS * 16 + ((j * 4 + i) * 4 + q) * 16 + m] = acc[c][j][i];
+    __syncthreads();
+    const int e = 16 * c + (tid & 15);
+    for (int cc = tid >> 4; cc < cols; cc += 16) {
+      const int r = cc / NV;
+      const float* s = sums + ((cc % NV) * 16 + (r & 3) * 4 + (r >> 2)) * 16 + (tid & 15);
+      const float v = (s[0] + s[COLS * 16]) + (s[2 * COLS * 16] + s[3 * COLS * 16]);
+      if (e < a.E) dw[cc * a.E + e] = v;
+    }
+  }
+  if (c0 == 0 && tid < a.E) {
+    float* const to = a.splits == 1 ? a.dbias : a.parts + split * a.stride + static_cast<int64_t>(a.d) * a.E;
+    if (to != nullptr) to[tid] = (dbs[0][tid] + dbs[1][tid]) + (dbs[2][tid] + dbs[3][tid]);
   }
 }
 
+static int gate_grad_cols(int dtype) { return dtype == SCMOE_BF16 ? GateGradCfg<true, 1>::COLS : GateGradCfg<false, 1>::COLS; }
+
 // Two workgroups per compute unit where there are tokens for them.
-static int gate_grad_splits(int T, int d) {
-  const int blocks = (d + GG_COLS - 1) / GG_COLS;
-  const int64_t groups = (static_cast<int64_t>(T) + 4 * GG_TOKENS - 1) / (4 * GG_TOKENS);
+static int gate_grad_splits(int T, int d, int dtype) {
+  const int blocks = (d + gate_grad_cols(dtype) - 1) / gate_grad_cols(dtype);
+  const int64_t groups = (static_cast<int64_t>(T) + 4 * GG_TOK - 1) / (4 * GG_TOK);
   const int want = (2 * num_cus() + blocks - 1) / blocks;
   return static_cast<int>(groups < 1 ? 1 : groups < want ? groups : want);
 }
@@ -328,21 +504,33 @@ static int gate_grad_splits(int T, int d) {
 static int64_t gate_grad_stride(int d, int E) { return (static_cast<int64_t>(d) * E + E + 3) / 4 * 4; }
 
 static size_t gate_grad_bytes(int T, int d, int E) {
-  const int s = gate_grad_splits(T, d);
+  const int s = gate_grad_splits(T, d, SCMOE_BF16);         // the larger number of the two types
   return s == 1 ? 0 : static_cast<size_t>(s) * gate_grad_stride(d, E) * 4;
 }
 
 static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
-  dim3 grid((a.d + GG_COLS - 1) / GG_COLS * a.splits), block(256);
-#define SCMOE_GATE_GRAD(EC)                                                                                          \
-  do {                                                                                                               \
-    if (dtype == SCMOE_BF16) hipLaunchKernelGGL((gate_backward_kernel<true, EC>), grid, block, 0, stream, a);        \
-    else hipLaunchKernelGGL((gate_backward_kernel<false, EC>), grid, block, 0, stream, a);                           \
+  dim3 grid((a.d + gate_grad_cols(dtype) - 1) / gate_grad_cols(dtype) * a.splits), block(256);
+  const bool dispatch = a.dst_row != nullptr;
+#define SCMOE_GATE_GRAD_K(EC, K)                                                                                             \
+  do {                                                                                                                       \
+    if (dtype == SCMOE_BF16 && dispatch) hipLaunchKernelGGL((gate_backward_kernel<true, EC, K, true>), grid, block, 0, stream, a);        \
+    else if (dtype == SCMOE_BF16) hipLaunchKernelGGL((gate_backward_kernel<true, EC, K, false>), grid, block, 0, stream, a);              \
+    else if (dispatch) hipLaunchKernelGGL((gate_backward_kernel<false, EC, K, true>), grid, block, 0, stream, a);                         \
+    else hipLaunchKernelGGL((gate_backward_kernel<false, EC, K, false>), grid, block, 0, stream, a);                                      \
   } while (0)
-  if (a.E <= 16) SCMOE_GATE_GRAD(1);
-  else if (a.E <= 32) SCMOE_GATE_GRAD(2);
-  else SCMOE_GATE_GRAD(4);
+#define SCMOE_GATE_GRAD(EC)                      \
+  switch (a.k) {                                 \
+    case 1: SCMOE_GATE_GRAD_K(EC, 1); break;     \
+    case 2: SCMOE_GATE_GRAD_K(EC, 2); break;     \
+    case 3: SCMOE_GATE_GRAD_K(EC, 3); break;     \
+    default: SCMOE_GATE_GRAD_K(EC, 4); break;    \
+  }
+  static_assert(SCMOE_MAX_TOPK == 4, "one instantiation per k above");
+  if (a.E <= 16) { SCMOE_GATE_GRAD(1) }
+  else if (a.E <= 32) { SCMOE_GATE_GRAD(2) }
+  else { SCMOE_GATE_GRAD(4) }
 #undef SCMOE_GATE_GRAD
+#undef SCMOE_GATE_GRAD_K
   if (const int st = launch_status()) return st;
   if (a.splits == 1) return SCMOE_OK;
   return sum_parts(a.parts, a.splits, a.stride, a.dWg, static_cast<int64_t>(a.d) * a.E, a.dbias, a.E, stream);
@@ -421,7 +609,8 @@ extern "C" int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, co
   a.T = T; a.d = d; a.E = E; a.k = k; a.normalize = normalize;
   a.dxp = static_cast<const unsigned char*>(dx_perm); a.lddxp = ld_perm * eb; a.dst_row = dst_row;
   a.dx = static_cast<unsigned char*>(dx); a.lddx = lddx * eb;
-  a.splits = gate_grad_splits(T, d);
+  a.splits = gate_grad_splits(T, d, dtype);
+  a.probs16 = E % 4 == 0 && aligned16(probs);
   a.parts = static_cast<float*>(workspace); a.stride = gate_grad_stride(d, E);
   a.dWg = dW_g; a.dbias = dbias;
   return gate_backward(a, dtype, hs);
