@@ -148,7 +148,8 @@ def _ldw(t):
 
 def _stream(s):
     if s is None:
-        return torch.cuda.current_stream().cuda_stream
+        # (the handle alone: an object of the current stream costs 2.7 us, half of a small call)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return s.cuda_stream if hasattr(s, "cuda_stream") else int(s)
 
 
@@ -337,45 +338,57 @@ def moe_top2_layer_forward(desc, x, weights, y, workspace, routing=None, stream=
         workspace.numel() * workspace.element_size(), _stream(stream)), "moe_top2_layer_forward")
 
 
-def _rows_like(x, *others):
-    """Activations of one call: the same shape and type as x (None: not given)."""
-    for t in others:
-        if t is not None and (t.dtype != x.dtype or t.shape != x.shape):
-            raise TypeError("expected %s of %s, got %s of %s" % (tuple(x.shape), x.dtype, tuple(t.shape), t.dtype))
+def _refuse(t, want):
+    raise TypeError("expected %s on the GPU, got %s of %s on %s" % (want, tuple(t.shape), t.dtype, t.device))
 
 
-def _packed_like(x, *others):
-    """Packed rows: the width and the type of x."""
-    for t in others:
-        if t is not None and (t.dtype != x.dtype or t.dim() != 2 or t.shape[1] != x.shape[1]):
-            raise TypeError("expected rows of %d %s, got %s of %s" % (x.shape[1], x.dtype, tuple(t.shape), t.dtype))
+def _rows(t, shape, dtype):
+    """Address and row stride of activations of that shape and type (None: not given)."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
+        _refuse(t, "%s of %s" % (tuple(shape), dtype))
+    return t.data_ptr(), _ld(t)
 
 
-def _dense(dtype, *pairs):
-    """Pairs of a tensor (or None) and the number of elements it must have: dense and of that type."""
-    for t, n in pairs:
-        if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
-            raise TypeError("expected %d contiguous %s, got %s of %s" % (n, dtype, tuple(t.shape), t.dtype))
+def _packed(t, d, dtype):
+    """Address and row stride of packed rows of that width and type."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or t.dim() != 2 or t.shape[1] != d or not t.is_cuda:
+        _refuse(t, "rows of %d %s" % (d, dtype))
+    return t.data_ptr(), _ld(t)
+
+
+def _dense(t, n, dtype=torch.float32):
+    """Address of n elements of that type without gaps (None: not given)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        _refuse(t, "%d contiguous %s" % (n, dtype))
+    return t.data_ptr()
 
 
 def _mask(mask, T):
-    """One byte per token: torch.bool or torch.uint8."""
-    if mask is not None:
-        _dense(torch.bool if mask.dtype == torch.bool else torch.uint8, (mask, T))
+    """Address of one byte per token: torch.bool or torch.uint8."""
+    return None if mask is None else _dense(mask, T, torch.bool if mask.dtype is torch.bool else torch.uint8)
 
 
-def _nbytes(workspace):
-    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+def _scratch(workspace):
+    """Address and bytes of a workspace (None: none)."""
+    if workspace is None:
+        return None, 0
+    n = workspace.numel()
+    return _dense(workspace, n, workspace.dtype), n * workspace.element_size()
 
 
 def scmoe_layer_norm(x, gamma, beta, eps, y, residual=None, sum_out=None, mean=None, rstd=None, stream=None):
     """y = norm(x + residual) * gamma + beta; sum_out takes x + residual, mean and rstd what the backward pass needs."""
-    T, d = x.shape
-    _rows_like(x, y, residual, sum_out)
-    _dense(torch.float32, (gamma, d), (beta, d), (mean, T), (rstd, T))
-    _check(lib().scmoe_layer_norm(_ptr(x), _ld(x), dtype_code(x), _ptr(residual), _ld(residual), _ptr(gamma), _ptr(beta), eps, T, d,
-                                  _ptr(sum_out), _ld(sum_out), _ptr(y), _ld(y), _ptr(mean), _ptr(rstd), _stream(stream)),
-           "scmoe_layer_norm")
+    T, d = shape = x.shape
+    dtype = x.dtype
+    (xp, ldx), (rp, ldr), (sp, lds), (yp, ldy) = _rows(x, shape, dtype), _rows(residual, shape, dtype), _rows(sum_out, shape, dtype), _rows(y, shape, dtype)
+    _check(lib().scmoe_layer_norm(xp, ldx, dtype_code(x), rp, ldr, _dense(gamma, d), _dense(beta, d), eps, T, d, sp, lds, yp, ldy,
+                                  _dense(mean, T), _dense(rstd, T), _stream(stream)), "scmoe_layer_norm")
 
 
 def scmoe_layer_norm_backward_workspace_bytes(T, d):
@@ -386,12 +399,13 @@ def scmoe_layer_norm_backward_workspace_bytes(T, d):
 
 def scmoe_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, workspace=None, dsum=None, stream=None):
     """dx, dgamma and dbeta of scmoe_layer_norm; x is what was normed, dsum the gradient that reaches it beside the norm."""
-    T, d = x.shape
-    _rows_like(x, dy, dx, dsum)
-    _dense(torch.float32, (gamma, d), (mean, T), (rstd, T), (dgamma, d), (dbeta, d))
-    _check(lib().scmoe_layer_norm_backward(_ptr(dy), _ld(dy), _ptr(x), _ld(x), dtype_code(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
-                                           _ptr(dsum), _ld(dsum), T, d, _ptr(dx), _ld(dx), _ptr(dgamma), _ptr(dbeta),
-                                           _ptr(workspace), _nbytes(workspace), _stream(stream)), "scmoe_layer_norm_backward")
+    T, d = shape = x.shape
+    dtype = x.dtype
+    (gp, ldg), (xp, ldx), (sp, lds), (dp, ldd) = _rows(dy, shape, dtype), _rows(x, shape, dtype), _rows(dsum, shape, dtype), _rows(dx, shape, dtype)
+    wp, nb = _scratch(workspace)
+    _check(lib().scmoe_layer_norm_backward(gp, ldg, xp, ldx, dtype_code(x), _dense(gamma, d), _dense(mean, T), _dense(rstd, T), sp, lds, T, d,
+                                           dp, ldd, _dense(dgamma, d), _dense(dbeta, d), wp, nb, _stream(stream)),
+           "scmoe_layer_norm_backward")
 
 
 def scmoe_balance_loss_workspace_bytes(T, E):
@@ -403,11 +417,10 @@ def scmoe_balance_loss_workspace_bytes(T, E):
 def scmoe_balance_loss(probs, expert_idx, k, coef, load, mean_prob, slope, loss, workspace, mask=None, stream=None):
     """Loss, items per expert and the loss's slope in every counted token's probabilities."""
     T, E = probs.shape
-    _dense(torch.float32, (probs, T * E), (mean_prob, E), (slope, E), (loss, 1))
-    _dense(torch.int32, (expert_idx, T * k), (load, E))
-    _mask(mask, T)
-    _check(lib().scmoe_balance_loss(_ptr(probs), _ptr(expert_idx), _ptr(mask), T, E, k, coef, _ptr(load), _ptr(mean_prob), _ptr(slope),
-                                    _ptr(loss), _ptr(workspace), _nbytes(workspace), _stream(stream)), "scmoe_balance_loss")
+    wp, nb = _scratch(workspace)
+    _check(lib().scmoe_balance_loss(_dense(probs, T * E), _dense(expert_idx, T * k, torch.int32), _mask(mask, T), T, E, k, coef,
+                                    _dense(load, E, torch.int32), _dense(mean_prob, E), _dense(slope, E), _dense(loss, 1), wp, nb,
+                                    _stream(stream)), "scmoe_balance_loss")
 
 
 def scmoe_gate_backward_workspace_bytes(T, d, E):
@@ -420,27 +433,28 @@ def scmoe_gate_backward(x, W_g, probs, expert_idx, gate_w, dgate_w, dx, dW_g, db
                         mask=None, dx_perm=None, dst_row=None, stream=None):
     """dx, dW_g and dbias from the gradient of the gate weights, the balance loss's slope (times dloss) and the gradient of
     the packed rows."""
-    T, d = x.shape
+    T, d = shape = x.shape
     E = W_g.shape[1]
-    _rows_like(x, dx)
-    _packed_like(x, dx_perm)
-    _dense(torch.float32, (W_g, d * E), (probs, T * E), (gate_w, T * k), (dgate_w, T * k), (dW_g, d * E), (dbias, E), (slope, E), (dloss, 1))
-    _dense(torch.int32, (expert_idx, T * k), (dst_row, T * k))
-    _mask(mask, T)
-    _check(lib().scmoe_gate_backward(_ptr(x), _ld(x), dtype_code(x), _ptr(W_g), _ptr(probs), _ptr(expert_idx), _ptr(gate_w), _ptr(dgate_w),
-                                     _ptr(slope), _ptr(dloss), _ptr(mask), T, d, E, k, normalize, _ptr(dx_perm), _ld(dx_perm),
-                                     _ptr(dst_row), _ptr(dx), _ld(dx), _ptr(dW_g), _ptr(dbias), _ptr(workspace), _nbytes(workspace),
-                                     _stream(stream)), "scmoe_gate_backward")
+    dtype = x.dtype
+    if dx_perm is not None and dx_perm.shape[0] == 0:      # (nothing was kept: an empty tensor has no address)
+        dx_perm = dst_row = None
+    (xp, ldx), (dp, ldd), (pp, ldp) = _rows(x, shape, dtype), _rows(dx, shape, dtype), _packed(dx_perm, d, dtype)
+    wp, nb = _scratch(workspace)
+    _check(lib().scmoe_gate_backward(xp, ldx, dtype_code(x), _dense(W_g, d * E), _dense(probs, T * E), _dense(expert_idx, T * k, torch.int32),
+                                     _dense(gate_w, T * k), _dense(dgate_w, T * k), _dense(slope, E), _dense(dloss, 1), _mask(mask, T),
+                                     T, d, E, k, normalize, pp, ldp, _dense(dst_row, T * k, torch.int32), dp, ldd, _dense(dW_g, d * E),
+                                     _dense(dbias, E), wp, nb, _stream(stream)), "scmoe_gate_backward")
 
 
 def scmoe_combine_backward(dy, y_perm, dst_row, gate_w, k, dy_perm=None, dgate_w=None, base=None, coef=None, dbase=None, dcoef=None,
                            stream=None):
     """What reaches the packed rows, the gate weights, the shared expert's rows and the coefficients (each may be None)."""
-    T, d = dy.shape
-    _rows_like(dy, base, dbase)
-    _packed_like(dy, y_perm, dy_perm)
-    _dense(torch.float32, (gate_w, T * k), (dgate_w, T * k), (coef, 2 * T), (dcoef, 2 * T))
-    _dense(torch.int32, (dst_row, T * k))
-    _check(lib().scmoe_combine_backward(_ptr(dy), _ld(dy), dtype_code(dy), _ptr(y_perm), _ld(y_perm), _ptr(dst_row), _ptr(gate_w), T, d, k,
-                                        _ptr(base), _ld(base), _ptr(coef), _ptr(dy_perm), _ld(dy_perm), _ptr(dgate_w), _ptr(dbase),
-                                        _ld(dbase), _ptr(dcoef), _stream(stream)), "scmoe_combine_backward")
+    T, d = shape = dy.shape
+    dtype = dy.dtype
+    if y_perm is not None and y_perm.shape[0] == 0:        # (nothing was kept: an empty tensor has no address, and no row is read)
+        y_perm = dy
+    (gp, ldg), (yp, ldy), (bp, ldb) = _rows(dy, shape, dtype), _packed(y_perm, d, dtype), _rows(base, shape, dtype)
+    (pp, ldp), (op, ldo) = _packed(dy_perm, d, dtype), _rows(dbase, shape, dtype)
+    _check(lib().scmoe_combine_backward(gp, ldg, dtype_code(dy), yp, ldy, _dense(dst_row, T * k, torch.int32), _dense(gate_w, T * k), T, d, k,
+                                        bp, ldb, _dense(coef, 2 * T), pp, ldp, _dense(dgate_w, T * k), op, ldo, _dense(dcoef, 2 * T),
+                                        _stream(stream)), "scmoe_combine_backward")

@@ -120,6 +120,19 @@ def test_workspace_sizes(lib):
     assert lib.scmoe_gate_backward_workspace_bytes(1, 64, 4, None) == 1
 
 
+def test_binding_refuses_tensors_in_host_memory():
+    """An address that the GPU cannot read never reaches a kernel."""
+    import torch
+    from paper_2404_05019_amd import binding as B
+    x, v, i, s = torch.zeros(4, 64), torch.zeros(64), torch.zeros((4, 1), dtype=torch.int32), torch.zeros(4)
+    for call in (lambda: B.scmoe_layer_norm(x, v, v, 1e-5, x), lambda: B.scmoe_layer_norm_backward(x, x, v, s, s, x),
+                 lambda: B.scmoe_balance_loss(x, i, 1, 0.1, i, v, v, v[:1], v),
+                 lambda: B.scmoe_gate_backward(x, x.t().contiguous(), x, i, s, s, x, x, None, v),
+                 lambda: B.scmoe_combine_backward(x, x, i, s, 1, dgate_w=s)):
+        with pytest.raises(TypeError, match="on the GPU"):
+            call()
+
+
 CALLS = {"norm": norm, "norm_grad": norm_grad, "loss": loss, "gate_grad": gate_grad, "combine_grad": combine_grad}
 
 
