@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libscmoe.so")
 SOURCES = ["gate.hip", "dispatch.hip", "combine.hip", "ffn_mfma.hip", "ffn_direct.hip", "layer.hip",
-           "norm.hip", "gate_backward.hip", "combine_backward.hip", "sum_parts.hip"]
+           "norm.hip", "balance_loss.hip", "gate_backward.hip", "combine_backward.hip", "sum_parts.hip"]
 # Packed-fp32 instruction selection is switched off for all device code.
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,129 +1,12 @@
-// The balance loss of a gate, and the gradient of the gate: of the loss and of the gate weights through the softmax and
-// the gate product, and of the input encode.
+// The gradient of the gate: of the gate weights and of the balance loss through the softmax and the gate product, and of the
+// input encode.
 //
-//   loss       = coef E sum_e f_e P_e,  f_e = items of expert e / (k N),  P_e = mean of p[t,e] over the N counted tokens
-//   slope[e]   = dloss / dp[t,e] = coef E f_e / N        (the counts have no gradient)
 //   dl[t,e]    = p (g - sum_e' p g),  g = dloss slope[e] + the gradients of the full-softmax weights chosen there
 //                + w_j (dw_j - sum_i w_i dw_i) where weights are a softmax over the chosen logits alone
 //   dW_g = x^T dl,  dbias = sum_t dl,  dx = dl W_g^T + the encode's gradient rows gathered by dst_row
 #include "rows.hpp"
 
 namespace scmoe {
-
-// ---- balance loss ---------------------------------------------------------------------------------
-
-constexpr int LOSS_THREADS = 256;
-constexpr int LOSS_MAX_GROUPS = 256;
-
-// What a workgroup found: sums of p, items and (one number) counted tokens, EP experts wide.
-struct LossArgs {
-  const float* probs; const int32_t* idx; const uint8_t* mask;
-  int T, E, k, EP;               // EP: power of two >= E
-  float coef;
-  float* part_p; int32_t* part_n;   // [groups][EP], [groups][EP + 1]
-  int32_t* load; float* mean_prob; float* slope; float* loss;
-};
-
-// The lanes of a token are EP apart in thread index, lane e of a token reads p[t, e] and compares the token's choices
-// with e: loads are consecutive, and the counts need no atomics.
-__device__ __forceinline__ void loss_sums(const LossArgs& a, int block, int blocks, float& sum, int& items, int& tokens) {
-  const int per = LOSS_THREADS / a.EP, e = threadIdx.x & (a.EP - 1), sub = threadIdx.x / a.EP;
-  sum = 0.0f;
-  items = tokens = 0;
-  for (int64_t t0 = static_cast<int64_t>(block) * per; t0 < a.T; t0 += static_cast<int64_t>(blocks) * per) {
-    const int64_t t = t0 + sub;
-    if (t >= a.T || (a.mask != nullptr && a.mask[t] == 0)) continue;
-    ++tokens;
-    if (e < a.E) sum += a.probs[t * a.E + e];
-    for (int j = 0; j < a.k; ++j) items += a.idx[t * a.k + j] == e ? 1 : 0;
-  }
-}
-
-// Sums over the threads of a workgroup that have one expert, in the threads of the first EP.
-__device__ __forceinline__ void loss_fold(int EP, float& sum, int& items, int& tokens) {
-  __shared__ float sp[LOSS_THREADS];
-  __shared__ int si[LOSS_THREADS], st[LOSS_THREADS];
-  sp[threadIdx.x] = sum;
-  si[threadIdx.x] = items;
-  st[threadIdx.x] = tokens;
-  __syncthreads();
-  for (int half = LOSS_THREADS / 2; half >= EP; half >>= 1) {
-    if (static_cast<int>(threadIdx.x) < half) {
-      sp[threadIdx.x] += sp[threadIdx.x + half];
-      si[threadIdx.x] += si[threadIdx.x + half];
-      st[threadIdx.x] += st[threadIdx.x + half];
-    }
-    __syncthreads();
-  }
-  sum = sp[threadIdx.x];
-  items = si[threadIdx.x];
-  tokens = st[threadIdx.x];
-}
-
-// The first wave holds the sums of expert `lane`.
-__device__ __forceinline__ void loss_finish(const LossArgs& a, float sum, int items, int tokens) {
-  if (threadIdx.x >= 64) return;
-  const int e = threadIdx.x;
-  const bool in = e < a.E;
-  const int n = __shfl(tokens, 0, 64);
-  const float inv = n > 0 ? 1.0f / static_cast<float>(n) : 0.0f;   // nothing counted: loss and slopes are zero
-  const float mean = in ? sum * inv : 0.0f;
-  const float slope = in ? a.coef * a.E * (static_cast<float>(items) * inv / a.k) * inv : 0.0f;
-  const float loss = wave_sum(n > 0 && in ? slope * static_cast<float>(n) * mean : 0.0f);
-  if (in) {
-    a.load[e] = items;
-    a.mean_prob[e] = mean;
-    a.slope[e] = slope;
-  }
-  if (e == 0) a.loss[0] = loss;
-}
-
-__global__ __launch_bounds__(LOSS_THREADS) void balance_loss_kernel(LossArgs a) {
-  float sum;
-  int items, tokens;
-  loss_sums(a, blockIdx.x, gridDim.x, sum, items, tokens);
-  loss_fold(a.EP, sum, items, tokens);
-  if (gridDim.x == 1) {
-    loss_finish(a, sum, items, tokens);
-    return;
-  }
-  if (static_cast<int>(threadIdx.x) < a.EP) {
-    a.part_p[blockIdx.x * a.EP + threadIdx.x] = sum;
-    a.part_n[blockIdx.x * (a.EP + 1) + threadIdx.x] = items;
-    if (threadIdx.x == 0) a.part_n[blockIdx.x * (a.EP + 1) + a.EP] = tokens;
-  }
-}
-
-__global__ __launch_bounds__(LOSS_THREADS) void balance_loss_finish_kernel(LossArgs a, int groups) {
-  const int per = LOSS_THREADS / a.EP, e = threadIdx.x & (a.EP - 1);
-  float sum = 0.0f;
-  int items = 0, tokens = 0;
-  for (int i = threadIdx.x / a.EP; i < groups; i += per) {
-    sum += a.part_p[i * a.EP + e];
-    items += a.part_n[i * (a.EP + 1) + e];
-    tokens += a.part_n[i * (a.EP + 1) + a.EP];
-  }
-  loss_fold(a.EP, sum, items, tokens);
-  loss_finish(a, sum, items, tokens);
-}
-
-static int padded_experts(int E) {
-  int ep = 1;
-  while (ep < E) ep *= 2;
-  return ep;
-}
-
-static int loss_groups(int T, int E) {
-  const int per = LOSS_THREADS / padded_experts(E);
-  const int64_t g = (static_cast<int64_t>(T) + 4 * per - 1) / (4 * per);
-  return static_cast<int>(g < 1 ? 1 : g < LOSS_MAX_GROUPS ? g : LOSS_MAX_GROUPS);
-}
-
-static size_t loss_bytes(int T, int E) {
-  return static_cast<size_t>(loss_groups(T, E)) * (2 * padded_experts(E) + 1) * 4;
-}
-
-// ---- gradient of the gate -------------------------------------------------------------------------
 
 constexpr int GG_TOK = 16;       // tokens of a wave's step
 static_assert(GG_TOK * SCMOE_MAX_TOPK <= 64, "one register holds a step's items");
@@ -537,40 +420,6 @@ static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
 }
 
 }  // namespace scmoe
-
-extern "C" int scmoe_balance_loss_workspace_bytes(int32_t T, int32_t E, size_t* out) {
-  using namespace scmoe;
-  if (!out) return SCMOE_ERR_NULL;
-  if (T < 0 || E < 1 || E > SCMOE_MAX_EXPERTS) return SCMOE_ERR_SHAPE;
-  *out = loss_bytes(T, E);
-  return SCMOE_OK;
-}
-
-extern "C" int scmoe_balance_loss(const float* probs, const int32_t* expert_idx, const uint8_t* mask, int32_t T, int32_t E, int32_t k,
-                                  float coef, int32_t* load, float* mean_prob, float* slope, float* loss, void* workspace,
-                                  size_t ws_bytes, void* stream) {
-  using namespace scmoe;
-  if (T < 0 || E < 1 || E > SCMOE_MAX_EXPERTS) return SCMOE_ERR_SHAPE;
-  if (k < 1 || k > SCMOE_MAX_TOPK) return SCMOE_ERR_ARG;
-  if (k > E || static_cast<int64_t>(T) * k > 0x7fffffffLL) return SCMOE_ERR_SHAPE;   // counts are int32
-  if (!load || !mean_prob || !slope || !loss || (T > 0 && (!probs || !expert_idx || !workspace))) return SCMOE_ERR_NULL;
-  if (!aligned16(workspace)) return SCMOE_ERR_SHAPE;
-  if (T > 0 && ws_bytes < loss_bytes(T, E)) return SCMOE_ERR_WORKSPACE;
-  LossArgs a = {};
-  a.probs = probs; a.idx = expert_idx; a.mask = mask;
-  a.T = T; a.E = E; a.k = k; a.EP = padded_experts(E);
-  a.coef = coef;
-  const int groups = loss_groups(T, E);
-  a.part_p = static_cast<float*>(workspace);
-  a.part_n = reinterpret_cast<int32_t*>(a.part_p + groups * a.EP);
-  a.load = load; a.mean_prob = mean_prob; a.slope = slope; a.loss = loss;
-  hipStream_t hs = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(balance_loss_kernel, dim3(groups), dim3(LOSS_THREADS), 0, hs, a);
-  if (const int st = launch_status()) return st;
-  if (groups == 1) return SCMOE_OK;
-  hipLaunchKernelGGL(balance_loss_finish_kernel, dim3(1), dim3(LOSS_THREADS), 0, hs, a, groups);
-  return launch_status();
-}
 
 extern "C" int scmoe_gate_backward_workspace_bytes(int32_t T, int32_t d, int32_t E, size_t* out) {
   using namespace scmoe;

@@ -1,6 +1,7 @@
 // C-ABI entry points that are not a single kernel: status text, capacity, workspace sizes,
 // the expert FFN dispatcher, and the layer orchestration of ScMoE (paper Eq. (7), Sec. 3.2)
 // and of the standard top-k MoE layer (Eq. (1)-(4)).
+#include "arrival.hpp"
 #include "call_number.hpp"
 #include "common.hpp"
 
@@ -102,8 +103,8 @@ static LayerWs carve(const scmoe_desc* D, void* base, bool shared) {
   return w;
 }
 
-// Another number, never zero, for every call that uses one: of a count that starts at the clock, kept by the process.
-static unsigned long long next_call() {
+// Of a count that starts at the clock, kept by the process.
+unsigned long long next_call() {
   static std::atomic<unsigned long long> n{static_cast<unsigned long long>(std::chrono::steady_clock::now().time_since_epoch().count())};
   for (;;)
     if (const unsigned long long v = call_number(n.fetch_add(1, std::memory_order_relaxed))) return v;
