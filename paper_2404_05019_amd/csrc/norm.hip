@@ -34,25 +34,25 @@ struct NormGradArgs {
 // W = 1: four rows per workgroup and no barrier.
 constexpr int norm_threads(int W) { return W == 1 ? 256 : 64 * W; }
 
-// Sums of two values over the waves of a row.  `turn` alternates between calls: one barrier each is enough.
+// Sums of two values over the waves of a row.  Calls that follow each other use places `s` of their own: one barrier is enough.
 template <int W>
-__device__ __forceinline__ void row_sums(float& a, float& b, float2 (*s)[W], int turn) {
+__device__ __forceinline__ void row_sums(float& a, float& b, float2 (&s)[W]) {
   a = wave_sum(a);
   b = wave_sum(b);
   if (W > 1) {
-    if ((threadIdx.x & 63) == 0) s[turn][threadIdx.x >> 6] = make_float2(a, b);
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x / 64 % W] = make_float2(a, b);
     __syncthreads();
     a = b = 0.0f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const float2 p = s[turn][w];
+      const float2 p = s[w];
       a += p.x;
       b += p.y;
     }
   }
 }
 
-template <bool BF16, int V, int W>
+template <bool BF16, int V, int W, bool ST>
 __global__ __launch_bounds__(norm_threads(W)) void layer_norm_kernel(NormArgs a) {
   constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = 64 * W;
   __shared__ float2 s[2][W];
@@ -62,11 +62,11 @@ __global__ __launch_bounds__(norm_threads(W)) void layer_norm_kernel(NormArgs a)
        row += static_cast<int64_t>(gridDim.x) * (W == 1 ? 4 : 1)) {
     uint4 q[P];
 #pragma unroll
-    for (int p = 0; p < P; ++p) q[p] = load16(a.x + row * a.ldx + static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16);
+    for (int p = 0; p < P; ++p) q[p] = load16<ST>(a.x + row * a.ldx + static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16);
     if (a.residual != nullptr) {
       uint4 r[P];
 #pragma unroll
-      for (int p = 0; p < P; ++p) r[p] = load16(a.residual + row * a.ldres + static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16);
+      for (int p = 0; p < P; ++p) r[p] = load16<ST>(a.residual + row * a.ldres + static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16);
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         float v[NV], u[NV];
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(norm_threads(W)) void layer_norm_kernel(NormArgs a)
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] += u[i];
         q[p] = pack16<BF16>(v);       // what is normed is what is stored: the backward pass reads the stored sum
-        if (lane + p * STEP < pieces) store16(a.sum + row * a.ldsum + static_cast<int64_t>(lane + p * STEP) * 16, q[p]);
+        if (lane + p * STEP < pieces) store16<ST>(a.sum + row * a.ldsum + static_cast<int64_t>(lane + p * STEP) * 16, q[p]);
       }
     }
     float v[V];
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(norm_threads(W)) void layer_norm_kernel(NormArgs a)
 #pragma unroll
       for (int i = 0; i < NV; ++i) sum += v[p * NV + i];
     }
-    row_sums<W>(sum, none, s, 0);
+    row_sums<W>(sum, none, s[0]);
     const float inv = 1.0f / static_cast<float>(a.d);
     const float mean = sum * inv;
     float sq = 0.0f;
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(norm_threads(W)) void layer_norm_kernel(NormArgs a)
         sq += in ? c * c : 0.0f;
       }
     }
-    row_sums<W>(sq, none, s, 1);
+    row_sums<W>(sq, none, s[1]);
     const float rstd = 1.0f / sqrtf(sq * inv + a.eps);
     if (lane == 0) {
       if (a.mean != nullptr) a.mean[row] = mean;
@@ -121,164 +121,222 @@ __global__ __launch_bounds__(norm_threads(W)) void layer_norm_kernel(NormArgs a)
         o[i + 2] = fmaf(t[2] * rstd, g.z, b.z);
         o[i + 3] = fmaf(t[3] * rstd, g.w, b.w);
       }
-      store16(a.y + row * a.ldy + static_cast<int64_t>(c) * 16, pack16<BF16>(o));
+      store16<ST>(a.y + row * a.ldy + static_cast<int64_t>(c) * 16, pack16<BF16>(o));
     }
   }
 }
 
-// Every workgroup takes every gridDim.x-th row (group of four rows); a lane's columns are the same in all of them, so
-// dgamma and dbeta are summed in registers and leave as one part per workgroup.
-template <bool BF16, int V, int W>
-__global__ __launch_bounds__(norm_threads(W)) void layer_norm_backward_kernel(NormGradArgs a) {
-  constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = 64 * W, ROWS = W == 1 ? 4 : 1;
-  __shared__ float2 s[2][W];
-  extern __shared__ __attribute__((aligned(16))) float cols[];   // W == 1: [2][d]
-  const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+// Of a row of the gradient: x, dy, dsum, and its mean and 1 / deviation.
+template <int P>
+struct NormGradRow {
+  uint4 x[P], y[P], s[P];
+  float mean, rstd;
+};
+
+template <int P, int STEP, bool ST>
+__device__ __forceinline__ void norm_grad_load(const NormGradArgs& a, int64_t row, int lane, int pieces, NormGradRow<P>& r) {
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int64_t c = static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16;
+    r.x[p] = load16<ST>(a.x + row * a.ldx + c);
+    r.y[p] = load16<ST>(a.dy + row * a.lddy + c);
+    if (a.dsum != nullptr) r.s[p] = load16<ST>(a.dsum + row * a.lddsum + c);
+  }
+  r.mean = a.mean[row];
+  r.rstd = a.rstd[row];
+}
+
+// A workgroup has R rows at a time, W waves each, and takes every gridDim.x-th group of R; a lane's columns are the same in all of
+// them, so dgamma and dbeta are summed in registers and leave as one part per workgroup.  Where there are registers for it the
+// next row is loaded before this one is worked on.
+template <bool BF16, int V, int W, int R, bool ST>
+__global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(NormGradArgs a) {
+  constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = 64 * W, H = NV / 4, AREAS = W <= 2 ? 2 : 1;
+  constexpr bool AHEAD = P <= 2;
+  __shared__ float2 s[2][R][W];
+  extern __shared__ __attribute__((aligned(16))) float4 cols[];  // R > 1: AREAS of [dgamma, dbeta][half][piece]
+  const int mine = __builtin_amdgcn_readfirstlane(threadIdx.x / STEP);   // this wave's row of the R
+  const int lane = threadIdx.x - mine * STEP;
   const int pieces = a.d / NV;
   const float inv = 1.0f / static_cast<float>(a.d);
+  const int64_t step = static_cast<int64_t>(gridDim.x) * R, last = a.T - 1;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * R + mine;
+  NormGradRow<P> n;
+  if (AHEAD) norm_grad_load<P, STEP, ST>(a, row < a.T ? row : last, lane, pieces, n);
   float g[V], ag[V], ab[V];
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     const int c = min(lane + p * STEP, pieces - 1);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      g[p * NV + i] = a.gamma == nullptr ? 1.0f : a.gamma[c * NV + i];
-      ag[p * NV + i] = ab[p * NV + i] = 0.0f;
+    for (int i = 0; i < NV; i += 4) {
+      const float4 t = a.gamma == nullptr ? make_float4(1.0f, 1.0f, 1.0f, 1.0f) : *reinterpret_cast<const float4*>(a.gamma + c * NV + i);
+      g[p * NV + i] = t.x;
+      g[p * NV + i + 1] = t.y;
+      g[p * NV + i + 2] = t.z;
+      g[p * NV + i + 3] = t.w;
     }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) ag[p * NV + i] = ab[p * NV + i] = 0.0f;
   }
   int turn = 0;
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + (W == 1 ? threadIdx.x >> 6 : 0); row < a.T;
-       row += static_cast<int64_t>(gridDim.x) * ROWS) {
-    uint4 qx[P], qy[P];
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int64_t c = static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16;
-      qx[p] = load16(a.x + row * a.ldx + c);
-      qy[p] = load16(a.dy + row * a.lddy + c);
+  for (; row - mine < a.T; row += step) {               // (as many turns for every wave of the workgroup)
+    const bool live = row < a.T;
+    NormGradRow<P> q;
+    if (AHEAD) {
+      q = n;
+      norm_grad_load<P, STEP, ST>(a, row + step < a.T ? row + step : last, lane, pieces, n);
+    } else {
+      norm_grad_load<P, STEP, ST>(a, live ? row : last, lane, pieces, q);
     }
-    uint4 qs[P];
-    if (a.dsum != nullptr) {
-#pragma unroll
-      for (int p = 0; p < P; ++p) qs[p] = load16(a.dsum + row * a.lddsum + static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16);
-    }
-    const float mean = a.mean[row], rstd = a.rstd[row];
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const bool in = lane + p * STEP < pieces;
+      const bool in = live && lane + p * STEP < pieces;
       float x[NV], y[NV];
-      unpack16<BF16>(zero_unless(in, qx[p]), x);
-      unpack16<BF16>(zero_unless(in, qy[p]), y);
+      unpack16<BF16>(zero_unless(in, q.x[p]), x);
+      unpack16<BF16>(zero_unless(in, q.y[p]), y);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const float xh = (x[i] - mean) * rstd, gy = y[i] * g[p * NV + i];
+        const float xh = (x[i] - q.mean) * q.rstd, gy = y[i] * g[p * NV + i];
         s1 += gy;
         s2 = fmaf(gy, xh, s2);
         ag[p * NV + i] = fmaf(y[i], xh, ag[p * NV + i]);
         ab[p * NV + i] += y[i];
       }
     }
-    row_sums<W>(s1, s2, s, turn);
+    row_sums<W>(s1, s2, s[turn][mine]);
     turn ^= 1;
     s1 *= inv;
     s2 *= inv;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = lane + p * STEP;
-      if (c >= pieces) continue;
       float x[NV], y[NV], r[NV];
-      unpack16<BF16>(qx[p], x);
-      unpack16<BF16>(qy[p], y);
+      unpack16<BF16>(q.x[p], x);
+      unpack16<BF16>(q.y[p], y);
       if (a.dsum != nullptr) {
-        unpack16<BF16>(qs[p], r);
+        unpack16<BF16>(q.s[p], r);
       } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i) r[i] = 0.0f;
       }
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const float xh = (x[i] - mean) * rstd;
-        r[i] = fmaf(rstd, (y[i] * g[p * NV + i] - s1) - xh * s2, r[i]);
+        const float xh = (x[i] - q.mean) * q.rstd;
+        r[i] = fmaf(q.rstd, (y[i] * g[p * NV + i] - s1) - xh * s2, r[i]);
       }
-      store16(a.dx + row * a.lddx + static_cast<int64_t>(c) * 16, pack16<BF16>(r));
+      if (live && c < pieces) store16<ST>(a.dx + row * a.lddx + static_cast<int64_t>(c) * 16, pack16<BF16>(r));
     }
   }
   if (a.parts == nullptr) return;
-  float* part = a.parts + blockIdx.x * a.stride;
-  if (W == 1) {
-    // the four waves hold sums of the same columns: added in the waves' order
-    for (int w = 0; w < 4; ++w) {
-      if (static_cast<int>(threadIdx.x >> 6) == w) {
+  float4* const part = reinterpret_cast<float4*>(a.parts + blockIdx.x * a.stride);
+  const int half = a.d / 4;                             // float4 of dgamma; dbeta lies behind
+  if (R > 1) {
+    // The rows' waves hold sums of the same columns: every AREAS-th row's are added up in one area, in their order.  A lane's 4 or 8
+    // columns lie in two halves, so that neighbouring lanes use neighbouring banks.
+    float4* const area = cols + mine % AREAS * 2 * half;
+    for (int w = 0; w < (R + AREAS - 1) / AREAS; ++w) {
+      if (mine / AREAS == w) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           const int c = lane + p * STEP;
           if (c >= pieces) continue;
 #pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            cols[c * NV + i] = ag[p * NV + i] + (w == 0 ? 0.0f : cols[c * NV + i]);
-            cols[a.d + c * NV + i] = ab[p * NV + i] + (w == 0 ? 0.0f : cols[a.d + c * NV + i]);
+          for (int h = 0; h < H; ++h) {
+            const float* const u = ag + p * NV + 4 * h;
+            const float* const v = ab + p * NV + 4 * h;
+            float4 x = make_float4(u[0], u[1], u[2], u[3]), y = make_float4(v[0], v[1], v[2], v[3]);
+            if (w > 0) {
+              const float4 m = area[h * pieces + c], b = area[half + h * pieces + c];
+              x = make_float4(m.x + x.x, m.y + x.y, m.z + x.z, m.w + x.w);
+              y = make_float4(b.x + y.x, b.y + y.y, b.z + y.z, b.w + y.w);
+            }
+            area[h * pieces + c] = x;
+            area[half + h * pieces + c] = y;
           }
         }
       }
       __syncthreads();
     }
-    for (int i = threadIdx.x; i < a.d / 2; i += 256) reinterpret_cast<float4*>(part)[i] = reinterpret_cast<const float4*>(cols)[i];
+    for (int i = threadIdx.x; i < 2 * half; i += 64 * W * R) {
+      const int k = i < half ? i : i - half;
+      const int at = i - k + (k % H) * pieces + k / H;
+      float4 x = cols[at];
+      if (AREAS > 1) {
+        const float4 y = cols[2 * half + at];
+        x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+      }
+      part[i] = x;
+    }
   } else {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = lane + p * STEP;
       if (c >= pieces) continue;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        part[c * NV + i] = ag[p * NV + i];
-        part[a.d + c * NV + i] = ab[p * NV + i];
+      for (int h = 0; h < H; ++h) {
+        const float* const u = ag + p * NV + 4 * h;
+        const float* const v = ab + p * NV + 4 * h;
+        part[c * H + h] = make_float4(u[0], u[1], u[2], u[3]);
+        part[half + c * H + h] = make_float4(v[0], v[1], v[2], v[3]);
       }
     }
   }
 }
 
-// Workgroups of the backward kernel: two per compute unit, each with a part of 8 d bytes to leave.
+// Rows of a workgroup of the backward kernel, eight waves in all.  (Twelve, three a SIMD, took 30.2 us in place of 28.5 for 16384
+// rows of 1024: more of them wait for the last turn.)
+static int norm_grad_rows(int d) { return d <= 1024 ? 8 : d <= 2048 ? 4 : d <= 4096 ? 2 : 1; }
+
+// One workgroup per compute unit, each with a part of 8 d bytes to leave.
 static int norm_grad_groups(int T, int d) {
-  const int rows = d <= 2048 ? 4 : 1;
+  const int rows = norm_grad_rows(d);
   const int64_t most = (static_cast<int64_t>(T) + rows - 1) / rows;
-  const int cap = 2 * num_cus();
-  return static_cast<int>(most < cap ? most : cap);
+  return static_cast<int>(most < num_cus() ? most : num_cus());
 }
 
 constexpr int64_t NORM_MAX_GROUPS = 1 << 20;   // keeps the threads of a launch under 2^32; more rows than that take turns
 
-#define SCMOE_NORM_SIZES(LAUNCH)                    \
-  if (d <= 512) LAUNCH(8, 1);                       \
-  else if (d <= 1024) LAUNCH(16, 1);                \
-  else if (d <= 2048) LAUNCH(32, 1);                \
-  else if (d <= 4096) LAUNCH(16, 4);                \
-  else if (d <= 8192) LAUNCH(32, 4);                \
-  else LAUNCH(32, 8)
-
 static int layer_norm(const NormArgs& a, int dtype, hipStream_t stream) {
   const int d = a.d;
+  const bool st = streams_past_caches(static_cast<int64_t>(a.T) * d * elem_bytes(dtype) * (a.residual != nullptr ? 4 : 2));
 #define SCMOE_NORM(V, W)                                                                                                  \
   do {                                                                                                                    \
     const int64_t groups = W == 1 ? (static_cast<int64_t>(a.T) + 3) / 4 : a.T;                                            \
     dim3 grid(static_cast<unsigned>(groups < NORM_MAX_GROUPS ? groups : NORM_MAX_GROUPS)), block(norm_threads(W));        \
-    if (dtype == SCMOE_BF16) hipLaunchKernelGGL((layer_norm_kernel<true, V, W>), grid, block, 0, stream, a);             \
-    else hipLaunchKernelGGL((layer_norm_kernel<false, V, W>), grid, block, 0, stream, a);                                \
+    if (dtype == SCMOE_BF16 && st) hipLaunchKernelGGL((layer_norm_kernel<true, V, W, true>), grid, block, 0, stream, a);  \
+    else if (dtype == SCMOE_BF16) hipLaunchKernelGGL((layer_norm_kernel<true, V, W, false>), grid, block, 0, stream, a);  \
+    else if (st) hipLaunchKernelGGL((layer_norm_kernel<false, V, W, true>), grid, block, 0, stream, a);                   \
+    else hipLaunchKernelGGL((layer_norm_kernel<false, V, W, false>), grid, block, 0, stream, a);                          \
   } while (0)
-  SCMOE_NORM_SIZES(SCMOE_NORM);
+  if (d <= 512) SCMOE_NORM(8, 1);
+  else if (d <= 1024) SCMOE_NORM(16, 1);
+  else if (d <= 2048) SCMOE_NORM(32, 1);
+  else if (d <= 4096) SCMOE_NORM(16, 4);
+  else if (d <= 8192) SCMOE_NORM(32, 4);
+  else SCMOE_NORM(32, 8);
 #undef SCMOE_NORM
   return launch_status();
 }
 
 static int layer_norm_backward(const NormGradArgs& a, int dtype, int groups, hipStream_t stream) {
   const int d = a.d;
-#define SCMOE_NORM(V, W)                                                                                                  \
-  do {                                                                                                                    \
-    const size_t lds = W == 1 && a.parts != nullptr ? static_cast<size_t>(d) * 8 : 0;                                    \
-    dim3 grid(groups), block(norm_threads(W));                                                                            \
-    if (dtype == SCMOE_BF16) hipLaunchKernelGGL((layer_norm_backward_kernel<true, V, W>), grid, block, lds, stream, a);  \
-    else hipLaunchKernelGGL((layer_norm_backward_kernel<false, V, W>), grid, block, lds, stream, a);                     \
+  const bool st = streams_past_caches(static_cast<int64_t>(a.T) * d * elem_bytes(dtype) * (a.dsum != nullptr ? 4 : 3));
+#define SCMOE_NORM(V, W, R)                                                                                                             \
+  do {                                                                                                                                  \
+    const size_t lds = R > 1 && a.parts != nullptr ? static_cast<size_t>(d) * (W <= 2 ? 16 : 8) : 0;                                    \
+    dim3 grid(groups), block(64 * W * R);                                                                                               \
+    if (dtype == SCMOE_BF16 && st) hipLaunchKernelGGL((layer_norm_backward_kernel<true, V, W, R, true>), grid, block, lds, stream, a);  \
+    else if (dtype == SCMOE_BF16) hipLaunchKernelGGL((layer_norm_backward_kernel<true, V, W, R, false>), grid, block, lds, stream, a);  \
+    else if (st) hipLaunchKernelGGL((layer_norm_backward_kernel<false, V, W, R, true>), grid, block, lds, stream, a);                   \
+    else hipLaunchKernelGGL((layer_norm_backward_kernel<false, V, W, R, false>), grid, block, lds, stream, a);                          \
   } while (0)
-  SCMOE_NORM_SIZES(SCMOE_NORM);
+  if (d <= 512) SCMOE_NORM(8, 1, 8);
+  else if (d <= 1024) SCMOE_NORM(16, 1, 8);
+  else if (d <= 2048) SCMOE_NORM(16, 2, 4);
+  else if (d <= 4096) SCMOE_NORM(16, 4, 2);
+  else if (d <= 8192) SCMOE_NORM(16, 8, 1);
+  else SCMOE_NORM(32, 8, 1);
 #undef SCMOE_NORM
   return launch_status();
 }

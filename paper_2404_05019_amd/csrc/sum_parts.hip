@@ -11,12 +11,12 @@ constexpr int SUM_QUADS = 4;     // 16-byte column groups per workgroup: 64 byte
 __global__ __launch_bounds__(SUM_SLICES * SUM_QUADS) void sum_parts_kernel(const float* __restrict__ parts, int n, int64_t stride,
                                                                            float* __restrict__ a, int64_t na, float* __restrict__ b,
                                                                            int64_t nb) {
-  __shared__ float4 s[SUM_SLICES][SUM_QUADS];
+  __shared__ float4 s[SUM_SLICES * SUM_QUADS / 64][SUM_QUADS];
   const int quad = threadIdx.x % SUM_QUADS, slice = threadIdx.x / SUM_QUADS;
   const int64_t col = (static_cast<int64_t>(blockIdx.x) * SUM_QUADS + quad) * 4;
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   if (col < stride) {
-#pragma unroll 4
+#pragma unroll 8
     for (int i = slice; i < n; i += SUM_SLICES) {
       const float4 q = *reinterpret_cast<const float4*>(parts + i * stride + col);
       v.x += q.x;
@@ -25,25 +25,25 @@ __global__ __launch_bounds__(SUM_SLICES * SUM_QUADS) void sum_parts_kernel(const
       v.w += q.w;
     }
   }
-  s[slice][quad] = v;
-  __syncthreads();
+  // over the 16 slices of a wave, whose lanes of a quad are 4 apart, then over the waves
 #pragma unroll
-  for (int half = SUM_SLICES / 2; half > 0; half >>= 1) {
-    if (slice < half) {
-      const float4 p = s[slice][quad], q = s[slice + half][quad];
-      s[slice][quad] = make_float4(p.x + q.x, p.y + q.y, p.z + q.z, p.w + q.w);
-    }
-    __syncthreads();
+  for (int off = SUM_QUADS; off < 64; off <<= 1) {
+    v.x += __shfl_xor(v.x, off, 64);
+    v.y += __shfl_xor(v.y, off, 64);
+    v.z += __shfl_xor(v.z, off, 64);
+    v.w += __shfl_xor(v.w, off, 64);
   }
-  if (slice < 4) {
-    const int64_t c = col + slice;
-    const float4 q = s[0][quad];
-    const float r = slice == 0 ? q.x : slice == 1 ? q.y : slice == 2 ? q.z : q.w;
-    if (c < na) {
-      if (a != nullptr) a[c] = r;
-    } else if (c < na + nb) {
-      if (b != nullptr) b[c - na] = r;
-    }
+  if ((threadIdx.x & 63) < SUM_QUADS) s[threadIdx.x >> 6][quad] = v;
+  __syncthreads();
+  if (threadIdx.x >= 4 * SUM_QUADS) return;
+  const int64_t c = (static_cast<int64_t>(blockIdx.x) * SUM_QUADS * 4) + threadIdx.x;
+  float r = 0.0f;
+#pragma unroll
+  for (int w = 0; w < SUM_SLICES * SUM_QUADS / 64; ++w) r += reinterpret_cast<const float*>(s[w])[threadIdx.x];
+  if (c < na) {
+    if (a != nullptr) a[c] = r;
+  } else if (c < na + nb) {
+    if (b != nullptr) b[c - na] = r;
   }
 }
 
