@@ -55,6 +55,7 @@ class ScmoeError(RuntimeError):
 
 
 _lib = None
+_current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
 def lib():
@@ -111,7 +112,7 @@ def lib():
 
 
 def _check(status, where):
-    if status != 0:
+    if status:
         raise ScmoeError(status, where)
 
 
@@ -149,7 +150,7 @@ def _ldw(t):
 def _stream(s):
     if s is None:
         # (the handle alone: an object of the current stream costs 2.7 us, half of a small call)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return _current_stream(_current_device())
     return s.cuda_stream if hasattr(s, "cuda_stream") else int(s)
 
 
@@ -348,7 +349,9 @@ def _rows(t, shape, dtype):
         return None, 0
     if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
         _refuse(t, "%s of %s" % (tuple(shape), dtype))
-    return t.data_ptr(), _ld(t)
+    ld, one = t.stride()
+    assert one == 1, "rows must be contiguous"
+    return t.data_ptr(), ld
 
 
 def _packed(t, d, dtype):
