@@ -47,14 +47,14 @@ struct GateGradCfg {
   static constexpr int LDS = W_BYTES + 16 * EP * LD > SUM_BYTES ? W_BYTES + 16 * EP * LD : SUM_BYTES;
 };
 
-// What a step reads.
+// What a step reads, as it lies in memory: loaded a step ahead, so nothing here may be looked at (and waited for) before it is due.
 template <bool BF16, int EC>
 struct GateGradStep {
   uint4 x[4];                          // tokens 4 q + i
   float p[GateGradCfg<BF16, EC>::S];   // token m
   int idx, dst;                        // item `lane` of the step's 16 k
   float add, w;                        // its dgate_w, its gate_w
-  uint32_t use;                        // tokens that count, one bit each
+  uint32_t mask;                       // token m
 };
 
 template <bool BF16, int EC, int K, bool DISPATCH>
@@ -63,19 +63,14 @@ __device__ __forceinline__ void gate_grad_load(const GateGradArgs& a, int64_t t0
   const int m = lane & 15, q = lane >> 4;
   const int left = a.T - t0 < GG_TOK ? static_cast<int>(a.T - t0) : GG_TOK;   // tokens of this step
   const int mine = min(m, left - 1);
-  const bool on = m < left && (a.mask == nullptr || a.mask[t0 + mine] != 0);
-  n.use = static_cast<uint32_t>(__ballot(on)) & 0xffffu;
-  // items of this step in the order of memory: the expert and what it adds to g (to dl itself with normalize)
+  n.mask = 1;
+  if (a.mask != nullptr) n.mask = a.mask[t0 + mine];
   const int at = min(lane, left * K - 1);
   n.idx = n.dst = -1;
-  n.add = 0.0f;
-  if (DISPATCH) {
-    const int r = a.dst_row[t0 * K + at];
-    n.dst = lane < left * K ? r : -1;
-  }
+  n.add = n.w = 0.0f;
+  if (DISPATCH) n.dst = a.dst_row[t0 * K + at];
   if (a.dgate_w != nullptr) {
-    const int e = a.idx[t0 * K + at];
-    n.idx = lane < left * K && e < a.E ? e : -1;
+    n.idx = a.idx[t0 * K + at];
     n.add = a.dgate_w[t0 * K + at];
     if (a.normalize) n.w = a.gate_w[t0 * K + at];
   }
@@ -172,21 +167,38 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
 
   // W_g as operands of dx, in the order in which the lanes read them
   const float* const wg = a.Wg + static_cast<int64_t>(c0) * a.E;
-  if (BF16) {
+  if constexpr (BF16) {
     Bf16Parts<KS>* const wl = reinterpret_cast<Bf16Parts<KS>*>(lds);   // [column tile][part][k block][lane]
-    for (int i = tid; i < NV * KB * 64; i += 256) {
-      const int l = i % 64, kb = i / 64 % KB, j = i / (64 * KB);
-      const int c = NV * (l & 15) + j, e = S * (l >> 4) + KS * kb;
-      float v[KS];
+    constexpr int N = NV * KB * 64 / 256;
+    float v[N][KS];
 #pragma unroll
-      for (int s = 0; s < KS; ++s) v[s] = c < cols && e + s < a.E ? wg[c * a.E + e + s] : 0.0f;
-      split2<KS>(v, wl[(j * 2 * KB + kb) * 64 + l], wl[((j * 2 + 1) * KB + kb) * 64 + l]);
+    for (int n = 0; n < N; ++n) {
+      const int i = tid + n * 256, l = i % 64, kb = i / 64 % KB, j = i / (64 * KB);
+      const int c = NV * (l & 15) + j, e = S * (l >> 4) + KS * kb;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) v[n][s] = wg[min(c, cols - 1) * a.E + min(e + s, a.E - 1)];
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = tid + n * 256, l = i % 64, kb = i / 64 % KB, j = i / (64 * KB);
+      const int c = NV * (l & 15) + j, e = S * (l >> 4) + KS * kb;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) v[n][s] = c < cols && e + s < a.E ? v[n][s] : 0.0f;
+      split2<KS>(v[n], wl[(j * 2 * KB + kb) * 64 + l], wl[((j * 2 + 1) * KB + kb) * 64 + l]);
     }
   } else {
     float* const wl = reinterpret_cast<float*>(lds);                 // [expert][column]
-    for (int i = tid; i < EP * COLS; i += 256) {
-      const int c = i / EP, e = i % EP;
-      wl[e * COLS + c] = c < cols && e < a.E ? wg[c * a.E + e] : 0.0f;
+    constexpr int N = EP * COLS / 256;
+    float v[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = tid + n * 256, c = i / EP, e = i % EP;
+      v[n] = wg[min(c, cols - 1) * a.E + min(e, a.E - 1)];
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = tid + n * 256, c = i / EP, e = i % EP;
+      wl[e * COLS + c] = c < cols && e < a.E ? v[n] : 0.0f;
     }
   }
   float slope[S];
@@ -204,11 +216,16 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
   }
 
   for (; t0 < a.T; t0 += step) {
-    const uint32_t use = n.use;
-    const int dst = n.dst;
+    GateGradStep<BF16, EC> ahead;
+    // tokens that count, one bit each; items that are there
+    const int left = a.T - t0 < GG_TOK ? static_cast<int>(a.T - t0) : GG_TOK;
+    const uint32_t use = static_cast<uint32_t>(__ballot(m < left && n.mask != 0)) & 0xffffu;
+    const int dst = lane < left * K ? n.dst : -1;
+    n.idx = lane < left * K && n.idx < a.E ? n.idx : -1;
     uint4 dp[4];
     uint32_t have = 0;
     if (DISPATCH) have = gate_grad_rows<K>(a, t0, col_byte, q, dst, 0, dp);
+    gate_grad_load<BF16, EC, K, DISPATCH>(a, t0 + step < a.T ? t0 + step : t0, col_byte, lane, ahead);
     // dl of token m, experts S q + s
     float dl[S];
     {
@@ -287,7 +304,6 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
       }
     }
     wave_lds_order();
-    gate_grad_load<BF16, EC, K, DISPATCH>(a, t0 + step < a.T ? t0 + step : t0, col_byte, lane, n);
     // dx
     f32x4_t o[NV];
 #pragma unroll
@@ -330,6 +346,8 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
         }
       }
     }
+    loads_have_arrived();
+    n = ahead;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int64_t t = t0 + 4 * q + i;
@@ -376,18 +394,21 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
 
 static int gate_grad_cols(int dtype) { return dtype == SCMOE_BF16 ? GateGradCfg<true, 1>::COLS : GateGradCfg<false, 1>::COLS; }
 
-// Two workgroups per compute unit where there are tokens for them.
-static int gate_grad_splits(int T, int d, int dtype) {
+// Workgroups that share a column block, each with a part of dW_g to leave: as many as are resident together (two per compute unit,
+// one beyond 32 experts), and no more than it takes for the same number of turns.
+static int gate_grad_splits(int T, int d, int E, int dtype) {
   const int blocks = (d + gate_grad_cols(dtype) - 1) / gate_grad_cols(dtype);
   const int64_t groups = (static_cast<int64_t>(T) + 4 * GG_TOK - 1) / (4 * GG_TOK);
-  const int want = (2 * num_cus() + blocks - 1) / blocks;
-  return static_cast<int>(groups < 1 ? 1 : groups < want ? groups : want);
+  const int resident = (E <= 32 ? 2 : 1) * num_cus();
+  const int64_t most = resident > blocks ? resident / blocks : 1;
+  const int64_t turns = (groups + most - 1) / most;
+  return turns < 1 ? 1 : static_cast<int>((groups + turns - 1) / turns);
 }
 
 static int64_t gate_grad_stride(int d, int E) { return (static_cast<int64_t>(d) * E + E + 3) / 4 * 4; }
 
-static size_t gate_grad_bytes(int T, int d, int E) {
-  const int s = gate_grad_splits(T, d, SCMOE_BF16);         // the larger number of the two types
+static size_t gate_grad_bytes(int T, int d, int E) {        // (for either type)
+  const int b = gate_grad_splits(T, d, E, SCMOE_BF16), f = gate_grad_splits(T, d, E, SCMOE_F32), s = b > f ? b : f;
   return s == 1 ? 0 : static_cast<size_t>(s) * gate_grad_stride(d, E) * 4;
 }
 
@@ -458,7 +479,7 @@ extern "C" int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, co
   a.T = T; a.d = d; a.E = E; a.k = k; a.normalize = normalize;
   a.dxp = static_cast<const unsigned char*>(dx_perm); a.lddxp = ld_perm * eb; a.dst_row = dst_row;
   a.dx = static_cast<unsigned char*>(dx); a.lddx = lddx * eb;
-  a.splits = gate_grad_splits(T, d, dtype);
+  a.splits = gate_grad_splits(T, d, E, dtype);
   a.probs16 = E % 4 == 0 && aligned16(probs);
   a.parts = static_cast<float*>(workspace); a.stride = gate_grad_stride(d, E);
   a.dWg = dW_g; a.dbias = dbias;

@@ -208,6 +208,7 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
     turn ^= 1;
     s1 *= inv;
     s2 *= inv;
+    if (AHEAD) loads_have_arrived();
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = lane + p * STEP;

@@ -70,6 +70,12 @@ __device__ __forceinline__ float wave_sum(float v) {
   return (r0 + r1) + (r2 + r3);
 }
 
+// Waits for every load in flight, ahead of stores: where what was loaded ahead is due in the next turn of a loop, the wait the compiler
+// puts there would be one for the stores as well (one counter has both, and a store under a condition cannot be counted off).
+__device__ __forceinline__ void loads_have_arrived() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+}
+
 // Between a wave's LDS writes and its reads of what other lanes of it wrote (the LDS serves a wave in order; this
 // keeps the compiler to that order).
 __device__ __forceinline__ void wave_lds_order() {
