@@ -156,7 +156,12 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
   __shared__ float dbs[4][EP];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, q = lane >> 4;
   float* const dls = reinterpret_cast<float*>(lds + C::W_BYTES) + wave * EP * LD;   // dl of this wave's tokens: [expert][token]
-  const int split = blockIdx.x % a.splits, c0 = (blockIdx.x / a.splits) * COLS;
+  // Consecutive workgroups go to the eight dies in turn: each die takes a run of (split, column block), so that the blocks of a
+  // token's row, whose ends share cache lines and whose probabilities are the same, meet in one L2.
+  const int blocks = (a.d + COLS - 1) / COLS;
+  const int id = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  if (id >= a.splits * blocks) return;
+  const int split = id / blocks, c0 = id % blocks * COLS;
   const int cols = min(COLS, a.d - c0);
   const bool in = NV * m < cols;                      // (lanes past the end move what they do not use)
   const int64_t col_byte = static_cast<int64_t>(c0 + min(NV * m, cols - NV)) * (16 / NV);
@@ -413,7 +418,7 @@ static size_t gate_grad_bytes(int T, int d, int E) {        // (for either type)
 }
 
 static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
-  dim3 grid((a.d + gate_grad_cols(dtype) - 1) / gate_grad_cols(dtype) * a.splits), block(256);
+  dim3 grid(((a.d + gate_grad_cols(dtype) - 1) / gate_grad_cols(dtype) * a.splits + 7) / 8 * 8), block(256);
   const bool dispatch = a.dst_row != nullptr;
 #define SCMOE_GATE_GRAD_K(EC, K)                                                                                             \
   do {                                                                                                                       \
