@@ -16,7 +16,7 @@ struct GateGradArgs {
   const float* Wg; const float* probs; const int32_t* idx; const float* gate_w; const float* dgate_w;
   const float* slope; const float* dloss; const uint8_t* mask;
   int T, d, E, k, normalize;
-  int probs16;                                  // rows of probs are 16-byte aligned
+  int probs16, Wg16;                            // rows of probs, of W_g are 16-byte aligned
   const unsigned char* dxp; int64_t lddxp; const int32_t* dst_row;
   unsigned char* dx; int64_t lddx;
   float* parts; int64_t stride;                 // [splits][d E + E, padded to 4]; one split: dW_g and dbias themselves
@@ -43,9 +43,12 @@ struct GateGradCfg {
   static constexpr int KS = EC == 1 ? 4 : 8;                         // and values of a lane in one
   static constexpr int LD = GG_TOK + 4;                              // floats per expert of the dl buffer
   static constexpr int W_BYTES = EP * COLS * 4;
-  static constexpr int SUM_BYTES = 4 * COLS * 16 * 4;                // dW_g of four waves, 16 experts
+  static constexpr int SUM_BYTES = (EC > 1 ? 2 : 1) * 4 * COLS * 16 * 4;   // dW_g of four waves, 16 experts, twice
   static constexpr int LDS = W_BYTES + 16 * EP * LD > SUM_BYTES ? W_BYTES + 16 * EP * LD : SUM_BYTES;
 };
+
+// Tokens of a step.
+__device__ __forceinline__ int gate_grad_left(const GateGradArgs& a, int64_t t0) { return a.T - t0 < GG_TOK ? static_cast<int>(a.T - t0) : GG_TOK; }
 
 // What a step reads, as it lies in memory: loaded a step ahead, so nothing here may be looked at (and waited for) before it is due.
 template <bool BF16, int EC>
@@ -61,7 +64,7 @@ template <bool BF16, int EC, int K, bool DISPATCH>
 __device__ __forceinline__ void gate_grad_load(const GateGradArgs& a, int64_t t0, int64_t col_byte, int lane, GateGradStep<BF16, EC>& n) {
   using C = GateGradCfg<BF16, EC>;
   const int m = lane & 15, q = lane >> 4;
-  const int left = a.T - t0 < GG_TOK ? static_cast<int>(a.T - t0) : GG_TOK;   // tokens of this step
+  const int left = gate_grad_left(a, t0);
   const int mine = min(m, left - 1);
   n.mask = 1;
   if (a.mask != nullptr) n.mask = a.mask[t0 + mine];
@@ -135,23 +138,38 @@ __device__ __forceinline__ void split3(const float* v, Bf16Parts<4> (&part)[3]) 
 
 // Rows of the encode's gradient for choice j of tokens 4 q + i, as far as they were kept.
 template <int K>
-__device__ __forceinline__ uint32_t gate_grad_rows(const GateGradArgs& a, int64_t t0, int64_t col_byte, int q, int dst, int j, uint4 (&dp)[4]) {
+__device__ __forceinline__ uint32_t gate_grad_rows(const GateGradArgs& a, int64_t t0, int64_t col_byte, int lane, int dst, int j, uint4 (&dp)[4]) {
   uint32_t have = 0;
+  const int items = gate_grad_left(a, t0) * K;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int r = __shfl(dst, (4 * q + i) * K + j, 64);
-    have |= r >= 0 ? 1u << i : 0u;
+    const int item = (4 * (lane >> 4) + i) * K + j, r = __shfl(dst, item, 64);
+    const bool there = r >= 0 && item < items;
+    have |= there ? 1u << i : 0u;
     // (no row: the x of the step's first token, which is there)
-    const unsigned char* row = r >= 0 ? a.dxp + r * a.lddxp : a.x + t0 * a.ldx;
+    const unsigned char* row = there ? a.dxp + r * a.lddxp : a.x + t0 * a.ldx;
     dp[i] = load16(row + col_byte);
   }
   return have;
+}
+
+// Adds them to dx: lane (m, q) holds tokens 4 q + i, columns NV m + l.
+template <bool BF16, int NV>
+__device__ __forceinline__ void gate_grad_add(const uint4 (&dp)[4], uint32_t have, f32x4_t (&o)[NV]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float u[NV];
+    unpack16<BF16>(zero_unless((have >> i & 1u) != 0, dp[i]), u);
+#pragma unroll
+    for (int l = 0; l < NV; ++l) o[l][i] += u[l];
+  }
 }
 
 template <bool BF16, int EC, int K, bool DISPATCH>
 __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(GateGradArgs a) {
   using C = GateGradCfg<BF16, EC>;
   constexpr int EP = C::EP, S = C::S, LD = C::LD, NV = C::NV, COLS = C::COLS, KB = C::KB, KS = C::KS;
+  constexpr bool SECOND = DISPATCH && K > 1;
   __shared__ __attribute__((aligned(16))) unsigned char lds[C::LDS];
   __shared__ float dbs[4][EP];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, q = lane >> 4;
@@ -168,6 +186,8 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
   const int64_t step = static_cast<int64_t>(a.splits) * 4 * GG_TOK;
   int64_t t0 = (static_cast<int64_t>(split) * 4 + wave) * GG_TOK;
   GateGradStep<BF16, EC> n;
+  uint4 dp[4];                                        // the encode's rows of the first choice
+  uint32_t have = 0;
   if (t0 < a.T) gate_grad_load<BF16, EC, K, DISPATCH>(a, t0, col_byte, lane, n);
 
   // W_g as operands of dx, in the order in which the lanes read them
@@ -180,8 +200,20 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
     for (int n = 0; n < N; ++n) {
       const int i = tid + n * 256, l = i % 64, kb = i / 64 % KB, j = i / (64 * KB);
       const int c = NV * (l & 15) + j, e = S * (l >> 4) + KS * kb;
+      const float* const row = wg + min(c, cols - 1) * a.E;
+      if (a.Wg16) {
 #pragma unroll
-      for (int s = 0; s < KS; ++s) v[n][s] = wg[min(c, cols - 1) * a.E + min(e + s, a.E - 1)];
+        for (int s = 0; s < KS; s += 4) {
+          const float4 t = *reinterpret_cast<const float4*>(row + min(e + s, a.E - 4));
+          v[n][s] = t.x;
+          v[n][s + 1] = t.y;
+          v[n][s + 2] = t.z;
+          v[n][s + 3] = t.w;
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) v[n][s] = row[min(e + s, a.E - 1)];
+      }
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -206,6 +238,7 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
       wl[e * COLS + c] = c < cols && e < a.E ? v[n] : 0.0f;
     }
   }
+  if (DISPATCH && t0 < a.T) have = gate_grad_rows<K>(a, t0, col_byte, lane, n.dst, 0, dp);
   float slope[S];
 #pragma unroll
   for (int s = 0; s < S; ++s) slope[s] = a.slope != nullptr && S * q + s < a.E ? a.slope[S * q + s] * (a.dloss != nullptr ? a.dloss[0] : 1.0f) : 0.0f;
@@ -221,16 +254,21 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
   }
 
   for (; t0 < a.T; t0 += step) {
-    GateGradStep<BF16, EC> ahead;
+    // (the lane's places in shuffles and rows are worked out anew in every step: kept, they would take tens of registers)
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int m = lane & 15, q = lane >> 4;
     // tokens that count, one bit each; items that are there
-    const int left = a.T - t0 < GG_TOK ? static_cast<int>(a.T - t0) : GG_TOK;
+    const int left = gate_grad_left(a, t0);
     const uint32_t use = static_cast<uint32_t>(__ballot(m < left && n.mask != 0)) & 0xffffu;
-    const int dst = lane < left * K ? n.dst : -1;
     n.idx = lane < left * K && n.idx < a.E ? n.idx : -1;
-    uint4 dp[4];
-    uint32_t have = 0;
-    if (DISPATCH) have = gate_grad_rows<K>(a, t0, col_byte, q, dst, 0, dp);
-    gate_grad_load<BF16, EC, K, DISPATCH>(a, t0 + step < a.T ? t0 + step : t0, col_byte, lane, ahead);
+    // rows of the second choice where there are registers for them, then everything the next step reads
+    uint4 second[4];
+    uint32_t have_second = 0;
+    if (SECOND) have_second = gate_grad_rows<K>(a, t0, col_byte, lane, n.dst, 1, second);
+    const bool last = t0 + step >= a.T;
+    GateGradStep<BF16, EC> ahead = n;
+    if (!last) gate_grad_load<BF16, EC, K, DISPATCH>(a, t0 + step, col_byte, lane, ahead);
     // dl of token m, experts S q + s
     float dl[S];
     {
@@ -337,22 +375,20 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
         for (int j = 0; j < NV; ++j) o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(dl[s], w[j], o[j], 0, 0, 0);
       }
     }
-    // lane (m, q) holds dx of tokens 4 q + i, columns NV m + j
     if (DISPATCH) {
+      gate_grad_add<BF16>(dp, have, o);
+      if (SECOND) gate_grad_add<BF16>(second, have_second, o);
 #pragma unroll
-      for (int j = 0; j < K; ++j) {
-        if (j > 0) have = gate_grad_rows<K>(a, t0, col_byte, q, dst, j, dp);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float u[NV];
-          unpack16<BF16>(zero_unless((have >> i & 1u) != 0, dp[i]), u);
-#pragma unroll
-          for (int l = 0; l < NV; ++l) o[l][i] += u[l];
-        }
+      for (int j = SECOND ? 2 : 1; j < K; ++j) {
+        int dst = n.dst;
+        asm volatile("" : "+v"(dst)::"memory");       // (no earlier: their addresses would take registers from here to the top)
+        have = gate_grad_rows<K>(a, t0, col_byte, lane, dst, j, dp);
+        gate_grad_add<BF16>(dp, have, o);
       }
     }
     loads_have_arrived();
     n = ahead;
+    if (DISPATCH && !last) have = gate_grad_rows<K>(a, t0 + step, col_byte, lane, n.dst, 0, dp);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int64_t t = t0 + 4 * q + i;
@@ -366,7 +402,6 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
 
   // Sums of the four waves, 16 experts at a time: column NV (4 q + i) + j lies in the order (j, i, q), which 64 lanes write without a
   // bank conflict.
-  float* const sums = reinterpret_cast<float*>(lds);
 #pragma unroll
   for (int c = 0; c < EC; ++c) {
     float v = db[c];
@@ -375,20 +410,28 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
     if (q == 0) dbs[wave][16 * c + m] = v;
   }
   float* const dw = (a.splits == 1 ? a.dWg : a.parts + split * a.stride) + static_cast<int64_t>(c0) * a.E;
+  __syncthreads();
 #pragma unroll
   for (int c = 0; c < EC; ++c) {
-    __syncthreads();
+    if (16 * c >= a.E) break;
+    float* const sums = reinterpret_cast<float*>(lds) + (c & 1) * 4 * COLS * 16;   // (read two turns ago: a barrier lies between)
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) sums[wave * COLS * 16 + ((j * 4 + i) * 4 + q) * 16 + m] = acc[c][j][i];
     __syncthreads();
     const int e = 16 * c + (tid & 15);
-    for (int cc = tid >> 4; cc < cols; cc += 16) {
-      const int r = cc / NV;
+    float v[COLS / 16];
+#pragma unroll
+    for (int n = 0; n < COLS / 16; ++n) {
+      const int cc = (tid >> 4) + 16 * n, r = cc / NV;
       const float* s = sums + ((cc % NV) * 16 + (r & 3) * 4 + (r >> 2)) * 16 + (tid & 15);
-      const float v = (s[0] + s[COLS * 16]) + (s[2 * COLS * 16] + s[3 * COLS * 16]);
-      if (e < a.E) dw[cc * a.E + e] = v;
+      v[n] = (s[0] + s[COLS * 16]) + (s[2 * COLS * 16] + s[3 * COLS * 16]);
+    }
+#pragma unroll
+    for (int n = 0; n < COLS / 16; ++n) {
+      const int cc = (tid >> 4) + 16 * n;
+      if (e < a.E && cc < cols) dw[cc * a.E + e] = v[n];
     }
   }
   if (c0 == 0 && tid < a.E) {
@@ -486,6 +529,7 @@ extern "C" int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, co
   a.dx = static_cast<unsigned char*>(dx); a.lddx = lddx * eb;
   a.splits = gate_grad_splits(T, d, E, dtype);
   a.probs16 = E % 4 == 0 && aligned16(probs);
+  a.Wg16 = E % 4 == 0 && aligned16(W_g);
   a.parts = static_cast<float*>(workspace); a.stride = gate_grad_stride(d, E);
   a.dWg = dW_g; a.dbias = dbias;
   return gate_backward(a, dtype, hs);
