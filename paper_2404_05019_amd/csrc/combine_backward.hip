@@ -22,7 +22,7 @@ struct CombineGradArgs {
 };
 
 // A token belongs to W waves; PER pieces of 16 bytes per lane are in flight at a time.
-template <bool BF16, int K, int W>
+template <bool BF16, int K, int W, bool ST>
 __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a) {
   constexpr int NV = BF16 ? 8 : 4, STEP = 64 * W, PER = K == 1 ? 4 : 2, TOK = 4 / W;
   __shared__ float part[2][4][K + 1];
@@ -46,19 +46,19 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
         at[p] = static_cast<int64_t>(min(p0 + p * STEP, a.pieces - 1)) * 16;
-        g[p] = load16(dyr + at[p]);
+        g[p] = load16<ST>(dyr + at[p]);
       }
       if (a.yp != nullptr) {
 #pragma unroll
         for (int j = 0; j < K; ++j)
           if (r[j] >= 0) {
 #pragma unroll
-            for (int p = 0; p < PER; ++p) y[j][p] = load16(a.yp + r[j] * a.ldyp + at[p]);
+            for (int p = 0; p < PER; ++p) y[j][p] = load16<ST>(a.yp + r[j] * a.ldyp + at[p]);
           }
       }
       if (a.base != nullptr) {
 #pragma unroll
-        for (int p = 0; p < PER; ++p) b[p] = load16(a.base + t * a.ldbase + at[p]);
+        for (int p = 0; p < PER; ++p) b[p] = load16<ST>(a.base + t * a.ldbase + at[p]);
       }
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a
         if (a.dbase != nullptr) {
 #pragma unroll
           for (int i = 0; i < NV; ++i) o[i] = c0 * v[i];
-          store16(a.dbase + t * a.lddbase + at[p], pack16<BF16>(o));
+          store16<ST>(a.dbase + t * a.lddbase + at[p], pack16<BF16>(o));
         }
 #pragma unroll
         for (int j = 0; j < K; ++j) {
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a
             const float f = c1 * w[j];
 #pragma unroll
             for (int i = 0; i < NV; ++i) o[i] = f * v[i];
-            store16(a.dyp + r[j] * a.lddyp + at[p], pack16<BF16>(o));
+            store16<ST>(a.dyp + r[j] * a.lddyp + at[p], pack16<BF16>(o));
           }
         }
       }
@@ -130,12 +130,19 @@ static int combine_backward(const CombineGradArgs& a, int dtype, int k, hipStrea
   const bool wide = a.T < 8 * num_cus() && a.pieces > 64;
   const int64_t groups = wide ? a.T : (static_cast<int64_t>(a.T) + 3) / 4;
   dim3 grid(static_cast<unsigned>(groups < COMBINE_GRAD_MAX_GROUPS ? groups : COMBINE_GRAD_MAX_GROUPS)), block(256);
-#define SCMOE_COMBINE_GRAD(K)                                                                                                    \
-  do {                                                                                                                           \
-    if (dtype == SCMOE_BF16 && wide) hipLaunchKernelGGL((combine_backward_kernel<true, K, 4>), grid, block, 0, stream, a);       \
-    else if (dtype == SCMOE_BF16) hipLaunchKernelGGL((combine_backward_kernel<true, K, 1>), grid, block, 0, stream, a);          \
-    else if (wide) hipLaunchKernelGGL((combine_backward_kernel<false, K, 4>), grid, block, 0, stream, a);                        \
-    else hipLaunchKernelGGL((combine_backward_kernel<false, K, 1>), grid, block, 0, stream, a);                                  \
+  const int64_t rows = 1 + (a.base ? 1 : 0) + (a.dbase ? 1 : 0) + k * ((a.yp ? 1 : 0) + (a.dyp ? 1 : 0));
+  const bool st = streams_past_caches(rows * a.T * a.pieces * 16);
+#define SCMOE_COMBINE_GRAD_ST(K, ST)                                                                                                 \
+  do {                                                                                                                               \
+    if (dtype == SCMOE_BF16 && wide) hipLaunchKernelGGL((combine_backward_kernel<true, K, 4, ST>), grid, block, 0, stream, a);       \
+    else if (dtype == SCMOE_BF16) hipLaunchKernelGGL((combine_backward_kernel<true, K, 1, ST>), grid, block, 0, stream, a);          \
+    else if (wide) hipLaunchKernelGGL((combine_backward_kernel<false, K, 4, ST>), grid, block, 0, stream, a);                        \
+    else hipLaunchKernelGGL((combine_backward_kernel<false, K, 1, ST>), grid, block, 0, stream, a);                                  \
+  } while (0)
+#define SCMOE_COMBINE_GRAD(K)                  \
+  do {                                         \
+    if (st) SCMOE_COMBINE_GRAD_ST(K, true);    \
+    else SCMOE_COMBINE_GRAD_ST(K, false);      \
   } while (0)
   static_assert(SCMOE_MAX_TOPK == 4, "one instantiation per k below");
   switch (k) {
@@ -145,6 +152,7 @@ static int combine_backward(const CombineGradArgs& a, int dtype, int k, hipStrea
     default: SCMOE_COMBINE_GRAD(4); break;
   }
 #undef SCMOE_COMBINE_GRAD
+#undef SCMOE_COMBINE_GRAD_ST
   return launch_status();
 }
 

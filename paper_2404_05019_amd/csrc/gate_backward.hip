@@ -22,6 +22,7 @@ struct GateGradArgs {
   float* parts; int64_t stride;                 // [splits][d E + E, padded to 4]; one split: dW_g and dbias themselves
   float* dWg; float* dbias;
   int splits;
+  int stream;                                   // rows are moved past the caches (streams_past_caches)
 };
 
 // A workgroup has COLS columns and every `splits`-th group of 64 tokens, a wave 16 tokens of it at a time.  Outputs of both
@@ -91,8 +92,13 @@ __device__ __forceinline__ void gate_grad_load(const GateGradArgs& a, int64_t t0
 #pragma unroll
     for (int s = 0; s < C::S; ++s) n.p[s] = row[min(C::S * q + s, a.E - 1)];
   }
+  if (a.stream) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) n.x[i] = load16(a.x + (t0 + min(4 * q + i, left - 1)) * a.ldx + col_byte);
+    for (int i = 0; i < 4; ++i) n.x[i] = load16<true>(a.x + (t0 + min(4 * q + i, left - 1)) * a.ldx + col_byte);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n.x[i] = load16(a.x + (t0 + min(4 * q + i, left - 1)) * a.ldx + col_byte);
+  }
 }
 
 template <int N>
@@ -141,14 +147,21 @@ template <int K>
 __device__ __forceinline__ uint32_t gate_grad_rows(const GateGradArgs& a, int64_t t0, int64_t col_byte, int lane, int dst, int j, uint4 (&dp)[4]) {
   uint32_t have = 0;
   const int items = gate_grad_left(a, t0) * K;
+  const unsigned char* at[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int item = (4 * (lane >> 4) + i) * K + j, r = __shfl(dst, item, 64);
     const bool there = r >= 0 && item < items;
     have |= there ? 1u << i : 0u;
     // (no row: the x of the step's first token, which is there)
-    const unsigned char* row = there ? a.dxp + r * a.lddxp : a.x + t0 * a.ldx;
-    dp[i] = load16(row + col_byte);
+    at[i] = (there ? a.dxp + r * a.lddxp : a.x + t0 * a.ldx) + col_byte;
+  }
+  if (a.stream) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dp[i] = load16<true>(at[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dp[i] = load16(at[i]);
   }
   return have;
 }
@@ -396,7 +409,9 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
       float v[NV];
 #pragma unroll
       for (int j = 0; j < NV; ++j) v[j] = o[j][i];
-      store16(a.dx + t * a.lddx + col_byte, pack16<BF16>(v));
+      unsigned char* const to = a.dx + t * a.lddx + col_byte;
+      if (a.stream) store16<true>(to, pack16<BF16>(v));
+      else store16(to, pack16<BF16>(v));
     }
   }
 
@@ -528,6 +543,7 @@ extern "C" int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, co
   a.dxp = static_cast<const unsigned char*>(dx_perm); a.lddxp = ld_perm * eb; a.dst_row = dst_row;
   a.dx = static_cast<unsigned char*>(dx); a.lddx = lddx * eb;
   a.splits = gate_grad_splits(T, d, E, dtype);
+  a.stream = streams_past_caches(static_cast<int64_t>(T) * d * eb * (dx_perm ? 2 + k : 2));
   a.probs16 = E % 4 == 0 && aligned16(probs);
   a.Wg16 = E % 4 == 0 && aligned16(W_g);
   a.parts = static_cast<float*>(workspace); a.stride = gate_grad_stride(d, E);
