@@ -21,4 +21,41 @@ __device__ __forceinline__ bool all_arrived(unsigned long long* marks, unsigned 
   return __all(there);
 }
 
+// Data handed from one workgroup to another inside a launch: device scope, past the caches that are not shared.
+template <typename V>
+__device__ __forceinline__ void leave(V* p, V v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename V>
+__device__ __forceinline__ V left_there(const V* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// The same for a whole workgroup that has left its part: true in every thread of the last one (of several, if so), which clears the
+// marks.  `flag` is one int of LDS.
+__device__ __forceinline__ bool last_to_arrive(unsigned long long* marks, unsigned long long call, int mine, int all, int* flag) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // what this wave left is where every workgroup sees it
+  __syncthreads();                                        // ... and every wave's
+  if (threadIdx.x < 64) {
+    const bool there = all_arrived(marks, call, mine, all);
+    if (threadIdx.x == 0) *flag = there;
+  }
+  __syncthreads();
+  if (*flag == 0) return false;                           // (two may find all the others done: they write the same)
+  for (int i = threadIdx.x; i < all; i += blockDim.x) leave(marks + i, 0ull);
+  return true;
+}
+
+// Sum over `n` parts, `stride` floats apart, of the two floats at each; in their order.
+__device__ __forceinline__ float2 sum_left(const float* part, int n, int64_t stride) {
+  float2 v = make_float2(0.0f, 0.0f);
+#pragma unroll 16
+  for (int i = 0; i < n; ++i) {
+    const unsigned long long q = left_there(reinterpret_cast<const unsigned long long*>(part + i * stride));
+    v.x += __uint_as_float(static_cast<uint32_t>(q));
+    v.y += __uint_as_float(static_cast<uint32_t>(q >> 32));
+  }
+  return v;
+}
+
+__device__ __forceinline__ void leave2(float* p, float x, float y) {
+  leave(reinterpret_cast<unsigned long long*>(p), static_cast<unsigned long long>(__float_as_uint(y)) << 32 | __float_as_uint(x));
+}
+
 }  // namespace scmoe

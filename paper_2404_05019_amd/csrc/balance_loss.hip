@@ -23,11 +23,6 @@ struct LossArgs {
   int32_t* load; float* mean_prob; float* slope; float* loss;
 };
 
-__device__ __forceinline__ void leave(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ void leave(int32_t* p, int32_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-template <typename V>
-__device__ __forceinline__ V left_there(const V* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-
 // The first wave; lane e has the sums of expert e.
 __device__ __forceinline__ void loss_finish(const LossArgs& a, float sum, int items, int n) {
   const int e = threadIdx.x;
@@ -124,15 +119,9 @@ __global__ __launch_bounds__(LOSS_THREADS) void balance_loss_kernel(LossArgs a) 
       leave(a.part_p + blockIdx.x * 64 + lane, s);
       leave(a.part_n + blockIdx.x * 65 + lane, sn[lane]);
       if (lane == 0) leave(a.part_n + blockIdx.x * 65 + 64, st);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      const bool all = all_arrived(a.marks, a.call, blockIdx.x, gridDim.x);
-      if (lane == 0) last = all;
     }
   }
-  if (gridDim.x == 1) return;
-  __syncthreads();
-  if (last == 0) return;                                 // (two may find all the others done: they write the same)
-  for (int i = tid; i < static_cast<int>(gridDim.x); i += LOSS_THREADS) __hip_atomic_store(a.marks + i, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (gridDim.x == 1 || !last_to_arrive(a.marks, a.call, blockIdx.x, gridDim.x, &last)) return;
   float s = 0.0f;
   int n = 0, t = 0;
 #pragma unroll 16

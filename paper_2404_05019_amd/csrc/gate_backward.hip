@@ -4,6 +4,7 @@
 //   dl[t,e]    = p (g - sum_e' p g),  g = dloss slope[e] + the gradients of the full-softmax weights chosen there
 //                + w_j (dw_j - sum_i w_i dw_i) where weights are a softmax over the chosen logits alone
 //   dW_g = x^T dl,  dbias = sum_t dl,  dx = dl W_g^T + the encode's gradient rows gathered by dst_row
+#include "arrival.hpp"
 #include "rows.hpp"
 
 namespace scmoe {
@@ -22,6 +23,7 @@ struct GateGradArgs {
   float* parts; int64_t stride;                 // [splits][d E + E, padded to 4]; one split: dW_g and dbias themselves
   float* dWg; float* dbias;
   int splits;
+  unsigned long long* marks; unsigned long long call;   // one launch: the last workgroup of a column block adds up its parts (nullptr: not)
   int stream;                                   // rows are moved past the caches (streams_past_caches)
 };
 
@@ -185,6 +187,7 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
   constexpr bool SECOND = DISPATCH && K > 1;
   __shared__ __attribute__((aligned(16))) unsigned char lds[C::LDS];
   __shared__ float dbs[4][EP];
+  __shared__ int last_one;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, q = lane >> 4;
   float* const dls = reinterpret_cast<float*>(lds + C::W_BYTES) + wave * EP * LD;   // dl of this wave's tokens: [expert][token]
   // Consecutive workgroups go to the eight dies in turn: each die takes a run of (split, column block), so that the blocks of a
@@ -446,12 +449,29 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
 #pragma unroll
     for (int n = 0; n < COLS / 16; ++n) {
       const int cc = (tid >> 4) + 16 * n;
-      if (e < a.E && cc < cols) dw[cc * a.E + e] = v[n];
+      if (e < a.E && cc < cols) {
+        if (a.marks != nullptr) leave(dw + cc * a.E + e, v[n]);
+        else dw[cc * a.E + e] = v[n];
+      }
     }
   }
   if (c0 == 0 && tid < a.E) {
     float* const to = a.splits == 1 ? a.dbias : a.parts + split * a.stride + static_cast<int64_t>(a.d) * a.E;
-    if (to != nullptr) to[tid] = (dbs[0][tid] + dbs[1][tid]) + (dbs[2][tid] + dbs[3][tid]);
+    const float v = (dbs[0][tid] + dbs[1][tid]) + (dbs[2][tid] + dbs[3][tid]);
+    if (a.marks != nullptr) leave(to + tid, v);
+    else if (to != nullptr) to[tid] = v;
+  }
+  if (a.marks == nullptr || !last_to_arrive(a.marks + static_cast<int64_t>(c0 / COLS) * a.splits, a.call, split, a.splits, &last_one)) return;
+  const int64_t first = static_cast<int64_t>(c0) * a.E;
+  for (int i = 2 * tid; i < cols * a.E; i += 512) {       // (an even number: columns come in eights)
+    const float2 v = sum_left(a.parts + first + i, a.splits, a.stride);
+    a.dWg[first + i] = v.x;
+    a.dWg[first + i + 1] = v.y;
+  }
+  if (c0 == 0 && a.dbias != nullptr && tid < a.E) {
+    float v = 0.0f;
+    for (int i = 0; i < a.splits; ++i) v += left_there(a.parts + i * a.stride + static_cast<int64_t>(a.d) * a.E + tid);
+    a.dbias[tid] = v;
   }
 }
 
@@ -472,8 +492,12 @@ static int64_t gate_grad_stride(int d, int E) { return (static_cast<int64_t>(d) 
 
 static size_t gate_grad_bytes(int T, int d, int E) {        // (for either type)
   const int b = gate_grad_splits(T, d, E, SCMOE_BF16), f = gate_grad_splits(T, d, E, SCMOE_F32), s = b > f ? b : f;
-  return s == 1 ? 0 : static_cast<size_t>(s) * gate_grad_stride(d, E) * 4;
+  const size_t blocks = (d + gate_grad_cols(SCMOE_F32) - 1) / gate_grad_cols(SCMOE_F32);
+  return s == 1 ? 0 : static_cast<size_t>(s) * (gate_grad_stride(d, E) * 4 + 8 * blocks);   // parts and marks
 }
+
+// Where a column block's parts are few bytes, its last workgroup adds them up in the same launch.
+constexpr int64_t GATE_GRAD_ONE_LAUNCH = 64 << 10;
 
 static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
   dim3 grid(((a.d + gate_grad_cols(dtype) - 1) / gate_grad_cols(dtype) * a.splits + 7) / 8 * 8), block(256);
@@ -499,7 +523,7 @@ static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
 #undef SCMOE_GATE_GRAD
 #undef SCMOE_GATE_GRAD_K
   if (const int st = launch_status()) return st;
-  if (a.splits == 1) return SCMOE_OK;
+  if (a.splits == 1 || a.marks != nullptr) return SCMOE_OK;
   return sum_parts(a.parts, a.splits, a.stride, a.dWg, static_cast<int64_t>(a.d) * a.E, a.dbias, a.E, stream);
 }
 
@@ -548,5 +572,9 @@ extern "C" int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, co
   a.Wg16 = E % 4 == 0 && aligned16(W_g);
   a.parts = static_cast<float*>(workspace); a.stride = gate_grad_stride(d, E);
   a.dWg = dW_g; a.dbias = dbias;
+  if (a.splits > 1 && static_cast<int64_t>(a.splits) * gate_grad_cols(dtype) * E * 4 <= GATE_GRAD_ONE_LAUNCH) {
+    a.marks = reinterpret_cast<unsigned long long*>(a.parts + a.splits * a.stride);
+    a.call = next_call();
+  }
   return gate_backward(a, dtype, hs);
 }

@@ -5,6 +5,7 @@
 //
 // Bound by HBM: a row is read once, kept in registers (the squares are summed about the mean in a second walk over
 // them, so that a large mean costs no digits) and written once.  All arithmetic in fp32.
+#include "arrival.hpp"
 #include "rows.hpp"
 
 namespace scmoe {
@@ -28,6 +29,10 @@ struct NormGradArgs {
   int T, d;
   unsigned char* dx; int64_t lddx;
   float* parts; int64_t stride;                  // one part per workgroup: dgamma [d], dbeta [d]; nullptr: neither is wanted
+  // In one launch (else both nullptr): the last workgroup adds up the parts.  One workgroup: marks is not used.
+  float* dgamma; float* dbeta;
+  int one_launch;
+  unsigned long long* marks; unsigned long long call;   // (all_arrived)
 };
 
 // A row belongs to W waves, a lane to V of its values (V / 8 or V / 4 pieces of 16 bytes, 64 W pieces apart).
@@ -149,11 +154,36 @@ __device__ __forceinline__ void norm_grad_load(const NormGradArgs& a, int64_t ro
 // A workgroup has R rows at a time, W waves each, and takes every gridDim.x-th group of R; a lane's columns are the same in all of
 // them, so dgamma and dbeta are summed in registers and leave as one part per workgroup.  Where there are registers for it the
 // next row is loaded before this one is worked on.
+// Columns 4 i and on of [dgamma, dbeta] of the whole call.
+__device__ __forceinline__ void norm_grad_put(const NormGradArgs& a, int i, const float4& v) {
+  float* const to = 4 * i < a.d ? a.dgamma : a.dbeta;
+  if (to == nullptr) return;
+  const int c = 4 * i < a.d ? 4 * i : 4 * i - a.d;
+  to[c] = v.x;
+  to[c + 1] = v.y;
+  to[c + 2] = v.z;
+  to[c + 3] = v.w;
+}
+
+// ... of this workgroup's part.
+__device__ __forceinline__ void norm_grad_leave(const NormGradArgs& a, int i, const float4& v) {
+  float* const part = a.parts + blockIdx.x * a.stride + 4 * i;
+  if (!a.one_launch) {
+    *reinterpret_cast<float4*>(part) = v;
+  } else if (gridDim.x == 1) {
+    norm_grad_put(a, i, v);
+  } else {
+    leave2(part, v.x, v.y);
+    leave2(part + 2, v.z, v.w);
+  }
+}
+
 template <bool BF16, int V, int W, int R, bool ST>
 __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(NormGradArgs a) {
   constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = 64 * W, H = NV / 4, AREAS = W <= 2 ? 2 : 1;
   constexpr bool AHEAD = P <= 2;
   __shared__ float2 s[2][R][W];
+  __shared__ int last_one;
   extern __shared__ __attribute__((aligned(16))) float4 cols[];  // R > 1: AREAS of [dgamma, dbeta][half][piece]
   const int mine = __builtin_amdgcn_readfirstlane(threadIdx.x / STEP);   // this wave's row of the R
   const int lane = threadIdx.x - mine * STEP;
@@ -230,7 +260,6 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
     }
   }
   if (a.parts == nullptr) return;
-  float4* const part = reinterpret_cast<float4*>(a.parts + blockIdx.x * a.stride);
   const int half = a.d / 4;                             // float4 of dgamma; dbeta lies behind
   if (R > 1) {
     // The rows' waves hold sums of the same columns: every AREAS-th row's are added up in one area, in their order.  A lane's 4 or 8
@@ -267,7 +296,7 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
         const float4 y = cols[2 * half + at];
         x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
       }
-      part[i] = x;
+      norm_grad_leave(a, i, x);
     }
   } else {
 #pragma unroll
@@ -278,10 +307,18 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
       for (int h = 0; h < H; ++h) {
         const float* const u = ag + p * NV + 4 * h;
         const float* const v = ab + p * NV + 4 * h;
-        part[c * H + h] = make_float4(u[0], u[1], u[2], u[3]);
-        part[half + c * H + h] = make_float4(v[0], v[1], v[2], v[3]);
+        norm_grad_leave(a, c * H + h, make_float4(u[0], u[1], u[2], u[3]));
+        norm_grad_leave(a, half + c * H + h, make_float4(v[0], v[1], v[2], v[3]));
       }
     }
+  }
+  if (!a.one_launch || gridDim.x == 1 || !last_to_arrive(a.marks, a.call, blockIdx.x, gridDim.x, &last_one)) return;
+  for (int i = threadIdx.x; i < a.d; i += 64 * W * R) {
+    const float2 v = sum_left(a.parts + 2 * i, gridDim.x, a.stride);
+    float* const to = 2 * i < a.d ? a.dgamma : a.dbeta;
+    if (to == nullptr) continue;
+    to[2 * i < a.d ? 2 * i : 2 * i - a.d] = v.x;
+    to[(2 * i < a.d ? 2 * i : 2 * i - a.d) + 1] = v.y;
   }
 }
 
@@ -289,11 +326,22 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
 // rows of 1024: more of them wait for the last turn.)
 static int norm_grad_rows(int d) { return d <= 1024 ? 8 : d <= 2048 ? 4 : d <= 4096 ? 2 : 1; }
 
-// One workgroup per compute unit, each with a part of 8 d bytes to leave.
-static int norm_grad_groups(int T, int d) {
+// One workgroup per compute unit, each with a part of 8 d bytes to leave.  Where the parts are few bytes, or would be with up to four
+// turns for each workgroup, the last one adds them up in the same launch.
+constexpr int64_t NORM_GRAD_ONE_LAUNCH = 128 << 10;
+
+static int norm_grad_groups(int T, int d, bool* one_launch) {
   const int rows = norm_grad_rows(d);
-  const int64_t most = (static_cast<int64_t>(T) + rows - 1) / rows;
-  return static_cast<int>(most < num_cus() ? most : num_cus());
+  const int64_t most = (static_cast<int64_t>(T) + rows - 1) / rows, fit = NORM_GRAD_ONE_LAUNCH / (8 * d);
+  const int64_t groups = most < num_cus() ? most : num_cus();
+  *one_launch = groups <= fit || most <= 4 * fit;
+  return static_cast<int>(*one_launch && groups > fit ? fit : groups);
+}
+
+static size_t norm_grad_bytes(int T, int d) {
+  bool one;
+  const int groups = norm_grad_groups(T, d, &one);
+  return static_cast<size_t>(groups) * (8 * static_cast<size_t>(d) + 8);   // parts and marks
 }
 
 constexpr int64_t NORM_MAX_GROUPS = 1 << 20;   // keeps the threads of a launch under 2^32; more rows than that take turns
@@ -375,7 +423,7 @@ extern "C" int scmoe_layer_norm_backward_workspace_bytes(int32_t T, int32_t d, s
   using namespace scmoe;
   if (!out) return SCMOE_ERR_NULL;
   if (const int st = norm_shape(SCMOE_F32, T, d)) return st;
-  *out = static_cast<size_t>(norm_grad_groups(T, d)) * d * 8;
+  *out = norm_grad_bytes(T, d);
   return SCMOE_OK;
 }
 
@@ -391,9 +439,10 @@ extern "C" int scmoe_layer_norm_backward(const void* dy, int64_t lddy, const voi
   if (!dy || !x || !mean || !rstd || !dx || (sums && !workspace)) return SCMOE_ERR_NULL;
   if (!view_ok(dy, lddy, d, dtype) || !view_ok(x, ldx, d, dtype) || !view_ok(dx, lddx, d, dtype) || !aligned16(gamma)) return SCMOE_ERR_SHAPE;
   if (dsum && !view_ok(dsum, lddsum, d, dtype)) return SCMOE_ERR_SHAPE;
-  const int groups = norm_grad_groups(T, d);
   if (sums && !aligned16(workspace)) return SCMOE_ERR_SHAPE;
-  if (sums && ws_bytes < static_cast<size_t>(groups) * d * 8) return SCMOE_ERR_WORKSPACE;
+  if (sums && ws_bytes < norm_grad_bytes(T, d)) return SCMOE_ERR_WORKSPACE;
+  bool one;
+  const int groups = norm_grad_groups(T, d, &one);
   const int eb = elem_bytes(dtype);
   NormGradArgs a = {};
   a.dy = static_cast<const unsigned char*>(dy); a.lddy = lddy * eb;
@@ -404,6 +453,12 @@ extern "C" int scmoe_layer_norm_backward(const void* dy, int64_t lddy, const voi
   a.dx = static_cast<unsigned char*>(dx); a.lddx = lddx * eb;
   a.parts = sums ? static_cast<float*>(workspace) : nullptr;
   a.stride = 2 * static_cast<int64_t>(d);
+  a.dgamma = dgamma; a.dbeta = dbeta;
+  a.one_launch = one;
+  if (sums && one && groups > 1) {
+    a.marks = reinterpret_cast<unsigned long long*>(a.parts + groups * a.stride);
+    a.call = next_call();
+  }
   if (const int st = layer_norm_backward(a, dtype, groups, hs)) return st;
-  return sums ? sum_parts(a.parts, groups, a.stride, dgamma, d, dbeta, d, hs) : SCMOE_OK;
+  return sums && !one ? sum_parts(a.parts, groups, a.stride, dgamma, d, dbeta, d, hs) : SCMOE_OK;
 }
