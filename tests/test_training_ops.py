@@ -593,6 +593,157 @@ def test_offsets_past_32_bits(dtype):
     assert all(torch.equal(a, b) for a, b in zip(near, both(x, dy, far)))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_small_calls_in_graphs(dtype):
+    """Calls whose sums over the tokens are finished by the last workgroup of their one launch, replayed over a workspace that other
+    work has written to in between."""
+    g = gen(9)
+    T, d, E = 250, 136, 4
+    x, dy, gamma, Wg = normal(g, T, d, dtype=dtype), normal(g, T, d, dtype=dtype), normal(g, d), normal(g, d, E)
+    p, idx, w = routing(g, T, E, 1, 0)
+    mean, rstd, dw = normal(g, T), torch.rand(T, generator=g, device=DEV), normal(g, T, 1)
+    big_p, big_idx, _ = routing(g, 9000, 24, 2, 0)
+    dx, dh = empty(T, d, dtype), empty(T, d, dtype)
+    sums = [torch.zeros(n, device=DEV) for n in (d, d, d * E, E, 24, 24, 1)]
+    load = torch.zeros(24, dtype=torch.int32, device=DEV)
+    ws = torch.full((1 << 18,), NAN, device=DEV)
+
+    def run():
+        B.scmoe_layer_norm_backward(dy, x, gamma, mean, rstd, dx, sums[0], sums[1], ws)
+        B.scmoe_gate_backward(x, Wg, p, idx, w, dw, dh, sums[2].view(d, E), sums[3], ws)
+        B.scmoe_balance_loss(big_p, big_idx, 2, 0.1, load, sums[4], sums[5], sums[6], ws)
+    run()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (dx, dh, load, *sums)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for i in range(5):
+        for t in (dx, dh, load, *sums):
+            t.fill_(-1)
+        if i % 2:
+            ws.copy_(torch.randn(ws.shape, generator=g, device=DEV))
+        graph.replay()
+        if i > 2:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (dx, dh, load, *sums)))
+        run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (dx, dh, load, *sums)))
+
+
+@pytest.mark.parametrize("T,d", [(1, 64), (8, 1024), (9, 1024), (64 * 8, 1024), (64 * 8 + 1, 1024), (255 * 8, 64), (2600, 64), (16, 4096), (17, 4096),
+                                 (4, 16384), (5, 16384)])
+def test_norm_gradient_sums_on_both_sides_of_their_rules(T, d):
+    """One workgroup, one launch, one launch with more turns, two launches: dgamma and dbeta."""
+    g = gen(T)
+    x, dy, gamma, mean, rstd = normal(g, T, d), normal(g, T, d), normal(g, d), 0.1 * normal(g, T), 0.5 + torch.rand(T, generator=g, device=DEV)
+    ws, whole = workspace(B.scmoe_layer_norm_backward_workspace_bytes(T, d))
+    dx, dgamma, dbeta = empty(T, d, "f32"), torch.full((d + 1,), NAN, device=DEV)[1:], torch.full((d + 1,), NAN, device=DEV)[1:]
+    B.scmoe_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws)
+    wx, sx, wg, sg, wb, sb = norm_grad_ref(dy, x, gamma, mean, rstd, None)
+    close(dx, wx, sx)
+    close(dgamma, wg, sg)
+    close(dbeta, wb, sb)
+    assert bool(whole[ws.numel():].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,E", [(64, 4), (65, 4), (500, 8), (1100, 16), (300, 64), (4000, 32)])
+def test_unaligned_probabilities_and_gate_matrix(T, E, dtype):
+    """Rows that 16-byte loads could take but for where the tensors begin: the same bits as from aligned ones."""
+    g = gen(T + E)
+    d = 136
+    x, Wg = normal(g, T, d, dtype=dtype), normal(g, d, E)
+    p, idx, w = routing(g, T, E, 2, 1)
+    dw, slope = normal(g, T, 2), normal(g, E)
+
+    def shifted(t):
+        store = torch.full((t.numel() + 1,), NAN, device=DEV)
+        store[1:] = t.reshape(-1)
+        return store[1:].view(t.shape)
+    ws, _ = workspace(B.scmoe_gate_backward_workspace_bytes(T, d, E))
+    out = []
+    for f in (lambda t: t, shifted):
+        dx, dW, db = empty(T, d, dtype), torch.full((d, E), NAN, device=DEV), torch.full((E,), NAN, device=DEV)
+        B.scmoe_gate_backward(x, f(Wg), f(p), idx, f(w), f(dw), dx, f(dW), f(db), ws, k=2, normalize=1, slope=f(slope))
+        dW, db = f(dW), f(db)
+        B.scmoe_gate_backward(x, f(Wg), f(p), idx, f(w), f(dw), dx, dW, db, ws, k=2, normalize=1, slope=f(slope))
+        load, m, s, loss = torch.zeros(E, dtype=torch.int32, device=DEV), f(torch.zeros(E, device=DEV)), f(torch.zeros(E, device=DEV)), f(torch.zeros(1, device=DEV))
+        wl, _ = workspace(B.scmoe_balance_loss_workspace_bytes(T, E))
+        B.scmoe_balance_loss(f(p), idx, 2, 0.5, load, m, s, loss, wl)
+        out.append((dx, dW.clone(), db.clone(), load, s.clone(), m.clone(), loss.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(out[0][:5], out[1][:5]))
+    close(out[1][5], out[0][5].double(), 256 * H * out[0][5].double())     # (summed in another order)
+    close(out[1][6], out[0][6].double(), 320 * H * out[0][6].double())
+
+
+def test_nothing_dispatched():
+    """Packed rows of which there are none: what stays is the gate's own gradient, and zeros for the weights."""
+    T, d, E = 40, 64, 4
+    g = gen(3)
+    x, Wg = normal(g, T, d), normal(g, d, E)
+    p, idx, w = routing(g, T, E, 1, 0)
+    dw, dst, none = normal(g, T, 1), torch.full((T, 1), -1, dtype=torch.int32, device=DEV), torch.zeros((0, d), device=DEV)
+    out = []
+    for kw in (dict(), dict(dx_perm=none, dst_row=dst)):
+        dx, dW = empty(T, d, "f32"), torch.zeros(d, E, device=DEV)
+        B.scmoe_gate_backward(x, Wg, p, idx, w, dw, dx, dW, None, None, **kw)
+        out.append((dx, dW))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+    B.scmoe_combine_backward(x, none, dst, w, 1, dy_perm=none, dgate_w=dw)
+    assert bool((dw == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_calls_past_the_caches(dtype):
+    """More than 256 MB: loads and stores go past the caches.  Rows have the same bits as in calls of a part of them, which do not."""
+    d, E = 1024, 8
+    T = 50000 if dtype == "bf16" else 25000
+    g = gen(12)
+    x, r, gamma, beta = normal(g, T, d, dtype=dtype), normal(g, T, d, dtype=dtype), normal(g, d), normal(g, d)
+    half = [slice(0, T // 2), slice(T // 2, T)]
+    y, s, mean, rstd = empty(T, d, dtype), empty(T, d, dtype), torch.zeros(T, device=DEV), torch.zeros(T, device=DEV)
+    B.scmoe_layer_norm(x, gamma, beta, 1e-5, y, residual=r, sum_out=s, mean=mean, rstd=rstd)
+    for at in half:
+        y2, s2 = empty(T // 2, d, dtype), empty(T // 2, d, dtype)
+        B.scmoe_layer_norm(x[at], gamma, beta, 1e-5, y2, residual=r[at], sum_out=s2)
+        assert torch.equal(y[at], y2) and torch.equal(s[at], s2)
+    ws = torch.zeros(8 << 20, device=DEV)
+    dx, dgamma, dbeta = empty(T, d, dtype), torch.zeros(d, device=DEV), torch.zeros(d, device=DEV)
+    B.scmoe_layer_norm_backward(y, s, gamma, mean, rstd, dx, dgamma, dbeta, ws, dsum=r)
+    for at in half:
+        dx2 = empty(T // 2, d, dtype)
+        B.scmoe_layer_norm_backward(y[at], s[at], gamma, mean[at], rstd[at], dx2, dsum=r[at])
+        assert torch.equal(dx[at], dx2)
+    xh = (s.double() - mean.double()[:, None]) * rstd.double()[:, None] * y.double()
+    close(dgamma, xh.sum(0), 256 * H * xh.abs().sum(0))
+    del xh
+    close(dbeta, y.double().sum(0), 256 * H * y.double().abs().sum(0))
+    p, idx, w = routing(g, T, E, 2, 1)
+    dst, yp = packed(g, T, E, 2, idx, d, dtype)
+    dyp, dw = empty(yp.shape[0], d, dtype), torch.zeros((T, 2), device=DEV)
+    B.scmoe_combine_backward(x, yp, dst, w, 2, dy_perm=dyp, dgate_w=dw)
+    dyp2, dw2 = empty(yp.shape[0], d, dtype), torch.zeros((T, 2), device=DEV)
+    for at in half:
+        B.scmoe_combine_backward(x[at], yp, dst[at], w[at], 2, dy_perm=dyp2, dgate_w=dw2[at])
+    assert torch.equal(dyp, dyp2) and torch.equal(dw, dw2)
+    Wg, dW, db = normal(g, d, E), torch.zeros(d, E, device=DEV), torch.zeros(E, device=DEV)
+    B.scmoe_gate_backward(y, Wg, p, idx, w, dw, dx, dW, db, ws, k=2, normalize=1, dx_perm=dyp, dst_row=dst)
+    dW2, db2 = torch.zeros(d, E, dtype=torch.float64, device=DEV), torch.zeros(E, dtype=torch.float64, device=DEV)
+    for at in half:
+        dx2, dWh, dbh = empty(T // 2, d, dtype), torch.zeros(d, E, device=DEV), torch.zeros(E, device=DEV)
+        B.scmoe_gate_backward(y[at], Wg, p[at], idx[at], w[at], dw[at], dx2, dWh, dbh, ws, k=2, normalize=1, dx_perm=dyp, dst_row=dst[at])
+        assert torch.equal(dx[at], dx2)
+        dW2 += dWh.double()
+        db2 += dbh.double()
+    _, _, _, wW, sW, wb, sb = gate_grad_ref(y, Wg, p, idx, w, dw, 1, None, None, None, None, None)
+    close(dW, wW, 256 * H * sW)
+    close(db, wb, 256 * H * sb)
+    close(dW2, wW, 256 * H * sW)
+
+
 def test_binding_refuses_tensors_that_do_not_fit():
     x, v = torch.zeros((4, 64), device=DEV), torch.zeros(64, device=DEV)
     with pytest.raises(TypeError):
