@@ -744,6 +744,14 @@ def test_calls_past_the_caches(dtype):
     close(dW2, wW, 256 * H * sW)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_router_learns(dtype):
+    """The example: forty steps find most of the hidden router's choices (by chance 2 of 8 experts agree at a quarter)."""
+    from paper_2404_05019_amd.train_routing import train
+    errors, first, last = train(steps=40, T=1024, d=128, F=256, dtype=TYPES[dtype])
+    assert first < 0.4 and last > 0.75 and errors[-1] < errors[0] / 3, (errors[0], errors[-1], first, last)
+
+
 def test_binding_refuses_tensors_that_do_not_fit():
     x, v = torch.zeros((4, 64), device=DEV), torch.zeros(64, device=DEV)
     with pytest.raises(TypeError):
