@@ -333,6 +333,18 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
       for (int i = 0; i < 4; ++i) n.x[i] = zero_unless((use >> (4 * q + i) & 1u) != 0, n.x[i]);
     }
     wave_lds_order();
+    // (products that add to the same tile are kept apart: each would wait for the one before)
+    Bf16Parts<4> xa[NV];
+    if constexpr (BF16) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = j < 2 ? n.x[i].x : j < 4 ? n.x[i].y : j < 6 ? n.x[i].z : n.x[i].w;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) xa[j].w[i] = j & 1 ? high_halves(w[2 * i], w[2 * i + 1]) : low_halves(w[2 * i], w[2 * i + 1]);
+      }
+    }
 #pragma unroll
     for (int c = 0; c < EC; ++c) {
       const float4 t = *reinterpret_cast<const float4*>(&dls[(c * 16 + m) * LD + 4 * q]);
@@ -342,16 +354,9 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
         Bf16Parts<4> part[3];
         split3(v, part);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          uint32_t w[4];
+        for (int p = 2; p >= 0; --p)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = j < 2 ? n.x[i].x : j < 4 ? n.x[i].y : j < 6 ? n.x[i].z : n.x[i].w;
-          Bf16Parts<4> xa;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) xa.w[i] = j & 1 ? high_halves(w[2 * i], w[2 * i + 1]) : low_halves(w[2 * i], w[2 * i + 1]);
-#pragma unroll
-          for (int p = 2; p >= 0; --p) acc[c][j] = mfma_bf16(xa, part[p], acc[c][j]);
-        }
+          for (int j = 0; j < NV; ++j) acc[c][j] = mfma_bf16(xa[j], part[p], acc[c][j]);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -374,11 +379,19 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
         Bf16Parts<KS> hi, lo;
         split2<KS>(dl + KS * kb, hi, lo);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          const Bf16Parts<KS> wh = wl[(j * 2 * KB + kb) * 64], wo = wl[((j * 2 + 1) * KB + kb) * 64];
-          o[j] = mfma_bf16(hi, wo, o[j]);
-          o[j] = mfma_bf16(lo, wh, o[j]);
-          o[j] = mfma_bf16(hi, wh, o[j]);
+        for (int j0 = 0; j0 < NV; j0 += 4) {
+          Bf16Parts<KS> wh[4], wo[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            wh[j] = wl[((j0 + j) * 2 * KB + kb) * 64];
+            wo[j] = wl[(((j0 + j) * 2 + 1) * KB + kb) * 64];
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j0 + j] = mfma_bf16(hi, wo[j], o[j0 + j]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j0 + j] = mfma_bf16(lo, wh[j], o[j0 + j]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j0 + j] = mfma_bf16(hi, wh[j], o[j0 + j]);
         }
       }
     } else {
