@@ -21,14 +21,14 @@ struct CombineGradArgs {
   float* dcoef;                                // [T][2]
 };
 
-// A token belongs to W waves; PER pieces of 16 bytes per lane are in flight at a time.
-template <bool BF16, int K, int W, bool ST>
+// A token belongs to W waves, or to L lanes of one (narrow rows); PER pieces of 16 bytes per lane are in flight at a time.
+template <bool BF16, int K, int W, int L, int PER, bool ST>
 __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a) {
-  constexpr int NV = BF16 ? 8 : 4, STEP = 64 * W, PER = K == 1 ? 4 : 2, TOK = 4 / W;
+  constexpr int NV = BF16 ? 8 : 4, STEP = L * W, TOK = 256 / STEP;
   __shared__ float part[2][4][K + 1];
   const int lane = threadIdx.x % STEP, wave = threadIdx.x >> 6;
   int turn = 0;
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * TOK + (W == 1 ? wave : 0); t < a.T; t += static_cast<int64_t>(gridDim.x) * TOK) {
+  for (int64_t t = static_cast<int64_t>(blockIdx.x) * TOK + threadIdx.x / STEP; t < a.T; t += static_cast<int64_t>(gridDim.x) * TOK) {
     int64_t r[K];
     float w[K], dot[K + 1];
 #pragma unroll
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a
     }
     if (a.yp == nullptr && a.base == nullptr) continue;
 #pragma unroll
-    for (int j = 0; j <= K; ++j) dot[j] = wave_sum(dot[j]);
+    for (int j = 0; j <= K; ++j) dot[j] = wave_sum<L>(dot[j]);
     if (W > 1) {
       if ((threadIdx.x & 63) == 0) {
 #pragma unroll
@@ -126,23 +126,29 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a
 constexpr int COMBINE_GRAD_MAX_GROUPS = 1 << 20;   // keeps the threads of a launch under 2^32
 
 static int combine_backward(const CombineGradArgs& a, int dtype, int k, hipStream_t stream) {
-  // Four waves on a token's row where there are too few tokens to fill the chip with one each.
+  // Four waves on a token's row where there are too few tokens to fill the chip with one each; lanes of a wave share out several tokens
+  // whose rows one piece per lane covers (32768 tokens of 128, two each, bf16: 10.8 us with 16 lanes, 20.1 with 64), and wider rows keep
+  // no more pieces in flight than they have (32768 of 384, bf16: 15.7 us with one piece per lane, 22.1 with four).
   const bool wide = a.T < 8 * num_cus() && a.pieces > 64;
-  const int64_t groups = wide ? a.T : (static_cast<int64_t>(a.T) + 3) / 4;
+  const int lanes = wide ? 256 : a.pieces <= 16 ? 16 : a.pieces <= 32 ? 32 : 64;
+  const int64_t groups = (static_cast<int64_t>(a.T) + 256 / lanes - 1) / (256 / lanes);
   dim3 grid(static_cast<unsigned>(groups < COMBINE_GRAD_MAX_GROUPS ? groups : COMBINE_GRAD_MAX_GROUPS)), block(256);
   const int64_t rows = 1 + (a.base ? 1 : 0) + (a.dbase ? 1 : 0) + k * ((a.yp ? 1 : 0) + (a.dyp ? 1 : 0));
-  const bool st = streams_past_caches(rows * a.T * a.pieces * 16);
-#define SCMOE_COMBINE_GRAD_ST(K, ST)                                                                                                 \
+  const bool st = a.pieces > 128 && streams_past_caches(rows * a.T * a.pieces * 16);
+#define SCMOE_COMBINE_GRAD_L(K, W, L, PER, ST)                                                                                       \
   do {                                                                                                                               \
-    if (dtype == SCMOE_BF16 && wide) hipLaunchKernelGGL((combine_backward_kernel<true, K, 4, ST>), grid, block, 0, stream, a);       \
-    else if (dtype == SCMOE_BF16) hipLaunchKernelGGL((combine_backward_kernel<true, K, 1, ST>), grid, block, 0, stream, a);          \
-    else if (wide) hipLaunchKernelGGL((combine_backward_kernel<false, K, 4, ST>), grid, block, 0, stream, a);                        \
-    else hipLaunchKernelGGL((combine_backward_kernel<false, K, 1, ST>), grid, block, 0, stream, a);                                  \
+    if (dtype == SCMOE_BF16) hipLaunchKernelGGL((combine_backward_kernel<true, K, W, L, PER, ST>), grid, block, 0, stream, a);       \
+    else hipLaunchKernelGGL((combine_backward_kernel<false, K, W, L, PER, ST>), grid, block, 0, stream, a);                          \
   } while (0)
-#define SCMOE_COMBINE_GRAD(K)                  \
-  do {                                         \
-    if (st) SCMOE_COMBINE_GRAD_ST(K, true);    \
-    else SCMOE_COMBINE_GRAD_ST(K, false);      \
+#define SCMOE_COMBINE_GRAD(K)                                                               \
+  do {                                                                                      \
+    if (wide) SCMOE_COMBINE_GRAD_L(K, 4, 64, 1, false);                                     \
+    else if (lanes == 16) SCMOE_COMBINE_GRAD_L(K, 1, 16, 1, false);                         \
+    else if (lanes == 32) SCMOE_COMBINE_GRAD_L(K, 1, 32, 1, false);                         \
+    else if (a.pieces <= 64) SCMOE_COMBINE_GRAD_L(K, 1, 64, 1, false);                      \
+    else if (a.pieces <= 128) SCMOE_COMBINE_GRAD_L(K, 1, 64, 2, false);                     \
+    else if (st) SCMOE_COMBINE_GRAD_L(K, 1, 64, (K == 1 ? 4 : 2), true);                    \
+    else SCMOE_COMBINE_GRAD_L(K, 1, 64, (K == 1 ? 4 : 2), false);                           \
   } while (0)
   static_assert(SCMOE_MAX_TOPK == 4, "one instantiation per k below");
   switch (k) {
@@ -152,7 +158,7 @@ static int combine_backward(const CombineGradArgs& a, int dtype, int k, hipStrea
     default: SCMOE_COMBINE_GRAD(4); break;
   }
 #undef SCMOE_COMBINE_GRAD
-#undef SCMOE_COMBINE_GRAD_ST
+#undef SCMOE_COMBINE_GRAD_L
   return launch_status();
 }
 

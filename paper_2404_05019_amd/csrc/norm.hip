@@ -35,15 +35,15 @@ struct NormGradArgs {
   unsigned long long* marks; unsigned long long call;   // (all_arrived)
 };
 
-// A row belongs to W waves, a lane to V of its values (V / 8 or V / 4 pieces of 16 bytes, 64 W pieces apart).
-// W = 1: four rows per workgroup and no barrier.
+// A row belongs to W waves, or to L lanes of one (16 and 32: narrow rows), a lane to V of its values (V / 8 or V / 4 pieces of 16
+// bytes, L W pieces apart).  W = 1: several rows per workgroup and no barrier.
 constexpr int norm_threads(int W) { return W == 1 ? 256 : 64 * W; }
 
 // Sums of two values over the waves of a row.  Calls that follow each other use places `s` of their own: one barrier is enough.
-template <int W>
+template <int W, int L>
 __device__ __forceinline__ void row_sums(float& a, float& b, float2 (&s)[W]) {
-  a = wave_sum(a);
-  b = wave_sum(b);
+  a = wave_sum<L>(a);
+  b = wave_sum<L>(b);
   if (W > 1) {
     if ((threadIdx.x & 63) == 0) s[threadIdx.x / 64 % W] = make_float2(a, b);
     __syncthreads();
@@ -57,14 +57,13 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float2 (&s)[W]) {
   }
 }
 
-template <bool BF16, int V, int W, bool ST>
+template <bool BF16, int V, int W, bool ST, int L = 64>
 __global__ __launch_bounds__(norm_threads(W)) void layer_norm_kernel(NormArgs a) {
-  constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = 64 * W;
+  constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = L * W, ROWS = W == 1 ? 256 / L : 1;
   __shared__ float2 s[2][W];
-  const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int lane = threadIdx.x % STEP;
   const int pieces = a.d / NV;
-  for (int64_t row = W == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6) : blockIdx.x; row < a.T;
-       row += static_cast<int64_t>(gridDim.x) * (W == 1 ? 4 : 1)) {
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / STEP; row < a.T; row += static_cast<int64_t>(gridDim.x) * ROWS) {
     uint4 q[P];
 #pragma unroll
     for (int p = 0; p < P; ++p) q[p] = load16<ST>(a.x + row * a.ldx + static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16);
@@ -91,7 +90,7 @@ __global__ __launch_bounds__(norm_threads(W)) void layer_norm_kernel(NormArgs a)
 #pragma unroll
       for (int i = 0; i < NV; ++i) sum += v[p * NV + i];
     }
-    row_sums<W>(sum, none, s[0]);
+    row_sums<W, L>(sum, none, s[0]);
     const float inv = 1.0f / static_cast<float>(a.d);
     const float mean = sum * inv;
     float sq = 0.0f;
@@ -105,7 +104,7 @@ __global__ __launch_bounds__(norm_threads(W)) void layer_norm_kernel(NormArgs a)
         sq += in ? c * c : 0.0f;
       }
     }
-    row_sums<W>(sq, none, s[1]);
+    row_sums<W, L>(sq, none, s[1]);
     const float rstd = 1.0f / sqrtf(sq * inv + a.eps);
     if (lane == 0) {
       if (a.mean != nullptr) a.mean[row] = mean;
@@ -178,19 +177,20 @@ __device__ __forceinline__ void norm_grad_leave(const NormGradArgs& a, int i, co
   }
 }
 
-template <bool BF16, int V, int W, int R, bool ST>
+template <bool BF16, int V, int W, int R, bool ST, int L = 64>
 __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(NormGradArgs a) {
-  constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = 64 * W, H = NV / 4, AREAS = W <= 2 ? 2 : 1;
+  constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = L * W, H = NV / 4, AREAS = W <= 2 ? 2 : 1, ROWS = R * (64 / L);
   constexpr bool AHEAD = P <= 2;
   __shared__ float2 s[2][R][W];
   __shared__ int last_one;
   extern __shared__ __attribute__((aligned(16))) float4 cols[];  // R > 1: AREAS of [dgamma, dbeta][half][piece]
-  const int mine = __builtin_amdgcn_readfirstlane(threadIdx.x / STEP);   // this wave's row of the R
+  const int slot = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W));   // of the R
+  const int mine = L == 64 ? slot : static_cast<int>(threadIdx.x / STEP);     // this lane's row of the ROWS
   const int lane = threadIdx.x - mine * STEP;
   const int pieces = a.d / NV;
   const float inv = 1.0f / static_cast<float>(a.d);
-  const int64_t step = static_cast<int64_t>(gridDim.x) * R, last = a.T - 1;
-  int64_t row = static_cast<int64_t>(blockIdx.x) * R + mine;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * ROWS, last = a.T - 1;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + mine;
   NormGradRow<P> n;
   if (AHEAD) norm_grad_load<P, STEP, ST>(a, row < a.T ? row : last, lane, pieces, n);
   float g[V], ag[V], ab[V];
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
     for (int i = 0; i < NV; ++i) ag[p * NV + i] = ab[p * NV + i] = 0.0f;
   }
   int turn = 0;
-  for (; row - mine < a.T; row += step) {               // (as many turns for every wave of the workgroup)
+  for (int64_t first = static_cast<int64_t>(blockIdx.x) * ROWS; first < a.T; first += step, row += step) {               // (as many turns for every wave of the workgroup)
     const bool live = row < a.T;
     NormGradRow<P> q;
     if (AHEAD) {
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
         ab[p * NV + i] += y[i];
       }
     }
-    row_sums<W>(s1, s2, s[turn][mine]);
+    row_sums<W, L>(s1, s2, s[turn][slot]);
     turn ^= 1;
     s1 *= inv;
     s2 *= inv;
@@ -264,13 +264,22 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
   if (R > 1) {
     // The rows' waves hold sums of the same columns: every AREAS-th row's are added up in one area, in their order.  A lane's 4 or 8
     // columns lie in two halves, so that neighbouring lanes use neighbouring banks.
-    float4* const area = cols + mine % AREAS * 2 * half;
+    float4* const area = cols + slot % AREAS * 2 * half;
+    if (L < 64) {                                       // the rows of one wave first
+#pragma unroll
+      for (int off = L; off < 64; off <<= 1)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          ag[i] += __shfl_xor(ag[i], off, 64);
+          ab[i] += __shfl_xor(ab[i], off, 64);
+        }
+    }
     for (int w = 0; w < (R + AREAS - 1) / AREAS; ++w) {
-      if (mine / AREAS == w) {
+      if (slot / AREAS == w) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           const int c = lane + p * STEP;
-          if (c >= pieces) continue;
+          if (c >= pieces || (L < 64 && (threadIdx.x & 63) >= L)) continue;
 #pragma unroll
           for (int h = 0; h < H; ++h) {
             const float* const u = ag + p * NV + 4 * h;
@@ -322,25 +331,35 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
   }
 }
 
+// Lanes of a row: fewer than a wave where one piece of 16 bytes per lane covers it.  32768 rows of 128 in bf16 with their residual: 9.1 us
+// with 16 lanes and 13.0 with 64, the gradient 13.5 and 19.5.
+static int norm_lanes(int d, int dtype) {
+  const int pieces = d / vec_elems(dtype);
+  return pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64;
+}
+
 // Rows of a workgroup of the backward kernel, eight waves in all.  (Twelve, three a SIMD, took 30.2 us in place of 28.5 for 16384
 // rows of 1024: more of them wait for the last turn.)
-static int norm_grad_rows(int d) { return d <= 1024 ? 8 : d <= 2048 ? 4 : d <= 4096 ? 2 : 1; }
+static int norm_grad_rows(int d, int dtype) {
+  const int lanes = norm_lanes(d, dtype);
+  return lanes < 64 ? 8 * (64 / lanes) : d <= 1024 ? 8 : d <= 2048 ? 4 : d <= 4096 ? 2 : 1;
+}
 
 // One workgroup per compute unit, each with a part of 8 d bytes to leave.  Where the parts are few bytes, or would be with up to four
 // turns for each workgroup, the last one adds them up in the same launch.
 constexpr int64_t NORM_GRAD_ONE_LAUNCH = 128 << 10;
 
-static int norm_grad_groups(int T, int d, bool* one_launch) {
-  const int rows = norm_grad_rows(d);
+static int norm_grad_groups(int T, int d, int dtype, bool* one_launch) {
+  const int rows = norm_grad_rows(d, dtype);
   const int64_t most = (static_cast<int64_t>(T) + rows - 1) / rows, fit = NORM_GRAD_ONE_LAUNCH / (8 * d);
   const int64_t groups = most < num_cus() ? most : num_cus();
   *one_launch = groups <= fit || most <= 4 * fit;
   return static_cast<int>(*one_launch && groups > fit ? fit : groups);
 }
 
-static size_t norm_grad_bytes(int T, int d) {
+static size_t norm_grad_bytes(int T, int d) {          // (fp32 has as many workgroups or more)
   bool one;
-  const int groups = norm_grad_groups(T, d, &one);
+  const int groups = norm_grad_groups(T, d, SCMOE_F32, &one);
   return static_cast<size_t>(groups) * (8 * static_cast<size_t>(d) + 8);   // parts and marks
 }
 
@@ -348,6 +367,17 @@ constexpr int64_t NORM_MAX_GROUPS = 1 << 20;   // keeps the threads of a launch 
 
 static int layer_norm(const NormArgs& a, int dtype, hipStream_t stream) {
   const int d = a.d;
+  const int lanes = norm_lanes(d, dtype);
+  if (lanes < 64) {
+    const int rows = 256 / lanes;
+    const int64_t groups = (static_cast<int64_t>(a.T) + rows - 1) / rows;
+    dim3 grid(static_cast<unsigned>(groups < NORM_MAX_GROUPS ? groups : NORM_MAX_GROUPS)), block(256);
+    if (dtype == SCMOE_BF16 && lanes == 16) hipLaunchKernelGGL((layer_norm_kernel<true, 8, 1, false, 16>), grid, block, 0, stream, a);
+    else if (dtype == SCMOE_BF16) hipLaunchKernelGGL((layer_norm_kernel<true, 8, 1, false, 32>), grid, block, 0, stream, a);
+    else if (lanes == 16) hipLaunchKernelGGL((layer_norm_kernel<false, 4, 1, false, 16>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((layer_norm_kernel<false, 4, 1, false, 32>), grid, block, 0, stream, a);
+    return launch_status();
+  }
   const bool st = streams_past_caches(static_cast<int64_t>(a.T) * d * elem_bytes(dtype) * (a.residual != nullptr ? 4 : 2));
 #define SCMOE_NORM(V, W)                                                                                                  \
   do {                                                                                                                    \
@@ -370,6 +400,16 @@ static int layer_norm(const NormArgs& a, int dtype, hipStream_t stream) {
 
 static int layer_norm_backward(const NormGradArgs& a, int dtype, int groups, hipStream_t stream) {
   const int d = a.d;
+  const int lanes = norm_lanes(d, dtype);
+  if (lanes < 64) {
+    const size_t lds = a.parts != nullptr ? static_cast<size_t>(d) * 16 : 0;
+    dim3 grid(groups), block(512);
+    if (dtype == SCMOE_BF16 && lanes == 16) hipLaunchKernelGGL((layer_norm_backward_kernel<true, 8, 1, 8, false, 16>), grid, block, lds, stream, a);
+    else if (dtype == SCMOE_BF16) hipLaunchKernelGGL((layer_norm_backward_kernel<true, 8, 1, 8, false, 32>), grid, block, lds, stream, a);
+    else if (lanes == 16) hipLaunchKernelGGL((layer_norm_backward_kernel<false, 4, 1, 8, false, 16>), grid, block, lds, stream, a);
+    else hipLaunchKernelGGL((layer_norm_backward_kernel<false, 4, 1, 8, false, 32>), grid, block, lds, stream, a);
+    return launch_status();
+  }
   const bool st = streams_past_caches(static_cast<int64_t>(a.T) * d * elem_bytes(dtype) * (a.dsum != nullptr ? 4 : 3));
 #define SCMOE_NORM(V, W, R)                                                                                                             \
   do {                                                                                                                                  \
@@ -442,7 +482,7 @@ extern "C" int scmoe_layer_norm_backward(const void* dy, int64_t lddy, const voi
   if (sums && !aligned16(workspace)) return SCMOE_ERR_SHAPE;
   if (sums && ws_bytes < norm_grad_bytes(T, d)) return SCMOE_ERR_WORKSPACE;
   bool one;
-  const int groups = norm_grad_groups(T, d, &one);
+  const int groups = norm_grad_groups(T, d, dtype, &one);
   const int eb = elem_bytes(dtype);
   NormGradArgs a = {};
   a.dy = static_cast<const unsigned char*>(dy); a.lddy = lddy * eb;

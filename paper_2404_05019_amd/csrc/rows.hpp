@@ -57,13 +57,17 @@ __device__ __forceinline__ float dpp_add(float v) {
   return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 
-// Sum over the 64 lanes, all of them active, in every lane: within rows of 16 lanes by the vector unit's lane moves (neighbour,
-// pair, mirrored 8, mirrored 16), which cost no trip to the LDS, then over the four rows.
+// Sum over L neighbouring lanes (16, 32 or all 64 of the wave, all of them active), in every one of them: within rows of 16 lanes by the
+// vector unit's lane moves (neighbour, pair, mirrored 8, mirrored 16), which cost no trip to the LDS, then over the rows.
+template <int L = 64>
 __device__ __forceinline__ float wave_sum(float v) {
+  static_assert(L == 16 || L == 32 || L == 64);
   v = dpp_add<0xB1>(v);
   v = dpp_add<0x4E>(v);
   v = dpp_add<0x141>(v);
   v = dpp_add<0x140>(v);
+  if (L == 16) return v;
+  if (L == 32) return v + __shfl_xor(v, 16, 64);
   const int b = __float_as_int(v);
   const float r0 = __int_as_float(__builtin_amdgcn_readlane(b, 0)), r1 = __int_as_float(__builtin_amdgcn_readlane(b, 16));
   const float r2 = __int_as_float(__builtin_amdgcn_readlane(b, 32)), r3 = __int_as_float(__builtin_amdgcn_readlane(b, 48));

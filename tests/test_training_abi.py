@@ -63,7 +63,7 @@ def test_layer_norm_refuses(lib, want, bad):
     (NULL, dict(dy=None)), (NULL, dict(x=None)), (NULL, dict(mean=None)), (NULL, dict(rstd=None)), (NULL, dict(dx=None)), (NULL, dict(ws=None)),
     (NULL, dict(ws=None, dbeta=None)), (SHAPE, dict(T=-1)), (SHAPE, dict(d=12)), (SHAPE, dict(d=16392)), (SHAPE, dict(lddy=0)),
     (SHAPE, dict(lddx=60)), (SHAPE, dict(dsum=P, ldds=32)), (SHAPE, dict(ws=P + 8)), (SHAPE, dict(gamma=P + 4)), (DTYPE, dict(dtype=9)),
-    (WORKSPACE, dict(nb=0)), (WORKSPACE, dict(nb=2 * 64 * 8 - 1)),
+    (WORKSPACE, dict(nb=0)), (WORKSPACE, dict(nb=64 * 8 + 7)),
 ])
 def test_layer_norm_backward_refuses(lib, want, bad):
     assert norm_grad(lib, **bad) == want
