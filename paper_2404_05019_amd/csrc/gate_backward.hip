@@ -41,7 +41,8 @@ template <bool BF16, int EC>
 struct GateGradCfg {
   static constexpr int EP = 16 * EC;                                 // experts, padded
   static constexpr int S = EP / 4;                                   // experts of a lane
-  static constexpr int NV = BF16 ? 8 : 4, COLS = 16 * NV;
+  static constexpr int NV = BF16 && EC < 4 ? 8 : 4, COLS = 16 * NV, EB = BF16 ? 2 : 4;
+  using Piece = std::conditional_t<NV * EB == 16, uint4, uint2>;     // a lane's columns of a row
   static constexpr int KB = EC == 4 ? 2 : 1;                         // bf16: k blocks of dx
   static constexpr int KS = EC == 1 ? 4 : 8;                         // and values of a lane in one
   static constexpr int LD = GG_TOK + 4;                              // floats per expert of the dl buffer
@@ -50,13 +51,48 @@ struct GateGradCfg {
   static constexpr int LDS = W_BYTES + 16 * EP * LD > SUM_BYTES ? W_BYTES + 16 * EP * LD : SUM_BYTES;
 };
 
+// A piece as fp32 values and back, 16 bytes or 8; its bytes in memory.
+template <bool BF16>
+__device__ __forceinline__ void unpack(const uint4& q, float* v) { unpack16<BF16>(q, v); }
+template <bool BF16>
+__device__ __forceinline__ void unpack(const uint2& q, float* v) {
+  v[0] = __uint_as_float(q.x << 16);
+  v[1] = __uint_as_float(q.x & 0xffff0000u);
+  v[2] = __uint_as_float(q.y << 16);
+  v[3] = __uint_as_float(q.y & 0xffff0000u);
+}
+template <bool BF16>
+__device__ __forceinline__ void pack(const float* v, uint4& q) { q = pack16<BF16>(v); }
+template <bool BF16>
+__device__ __forceinline__ void pack(const float* v, uint2& q) { q = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])); }
+__device__ __forceinline__ uint2 zero_unless(bool keep, const uint2& q) { return make_uint2(keep ? q.x : 0u, keep ? q.y : 0u); }
+template <bool STREAM>
+__device__ __forceinline__ void load_piece(const unsigned char* p, uint4& q) { q = load16<STREAM>(p); }
+template <bool STREAM>
+__device__ __forceinline__ void load_piece(const unsigned char* p, uint2& q) {
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  const u32x2_t v = STREAM ? __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(p)) : *reinterpret_cast<const u32x2_t*>(p);
+  q = make_uint2(v.x, v.y);
+}
+template <bool STREAM>
+__device__ __forceinline__ void store_piece(unsigned char* p, const uint4& q) { store16<STREAM>(p, q); }
+template <bool STREAM>
+__device__ __forceinline__ void store_piece(unsigned char* p, const uint2& q) {
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  if (STREAM) __builtin_nontemporal_store(u32x2_t{q.x, q.y}, reinterpret_cast<u32x2_t*>(p));
+  else *reinterpret_cast<u32x2_t*>(p) = u32x2_t{q.x, q.y};
+}
+// Columns 2 i and 2 i + 1 in bf16.
+__device__ __forceinline__ uint32_t word(const uint4& q, int i) { return i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w; }
+__device__ __forceinline__ uint32_t word(const uint2& q, int i) { return i == 0 ? q.x : q.y; }
+
 // Tokens of a step.
 __device__ __forceinline__ int gate_grad_left(const GateGradArgs& a, int64_t t0) { return a.T - t0 < GG_TOK ? static_cast<int>(a.T - t0) : GG_TOK; }
 
 // What a step reads, as it lies in memory: loaded a step ahead, so nothing here may be looked at (and waited for) before it is due.
 template <bool BF16, int EC>
 struct GateGradStep {
-  uint4 x[4];                          // tokens 4 q + i
+  typename GateGradCfg<BF16, EC>::Piece x[4];   // tokens 4 q + i
   float p[GateGradCfg<BF16, EC>::S];   // token m
   int idx, dst;                        // item `lane` of the step's 16 k
   float add, w;                        // its dgate_w, its gate_w
@@ -96,10 +132,10 @@ __device__ __forceinline__ void gate_grad_load(const GateGradArgs& a, int64_t t0
   }
   if (a.stream) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) n.x[i] = load16<true>(a.x + (t0 + min(4 * q + i, left - 1)) * a.ldx + col_byte);
+    for (int i = 0; i < 4; ++i) load_piece<true>(a.x + (t0 + min(4 * q + i, left - 1)) * a.ldx + col_byte, n.x[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) n.x[i] = load16(a.x + (t0 + min(4 * q + i, left - 1)) * a.ldx + col_byte);
+    for (int i = 0; i < 4; ++i) load_piece<false>(a.x + (t0 + min(4 * q + i, left - 1)) * a.ldx + col_byte, n.x[i]);
   }
 }
 
@@ -145,8 +181,8 @@ __device__ __forceinline__ void split3(const float* v, Bf16Parts<4> (&part)[3]) 
 }
 
 // Rows of the encode's gradient for choice j of tokens 4 q + i, as far as they were kept.
-template <int K>
-__device__ __forceinline__ uint32_t gate_grad_rows(const GateGradArgs& a, int64_t t0, int64_t col_byte, int lane, int dst, int j, uint4 (&dp)[4]) {
+template <int K, typename Piece>
+__device__ __forceinline__ uint32_t gate_grad_rows(const GateGradArgs& a, int64_t t0, int64_t col_byte, int lane, int dst, int j, Piece (&dp)[4]) {
   uint32_t have = 0;
   const int items = gate_grad_left(a, t0) * K;
   const unsigned char* at[4];
@@ -160,28 +196,28 @@ __device__ __forceinline__ uint32_t gate_grad_rows(const GateGradArgs& a, int64_
   }
   if (a.stream) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) dp[i] = load16<true>(at[i]);
+    for (int i = 0; i < 4; ++i) load_piece<true>(at[i], dp[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) dp[i] = load16(at[i]);
+    for (int i = 0; i < 4; ++i) load_piece<false>(at[i], dp[i]);
   }
   return have;
 }
 
 // Adds them to dx: lane (m, q) holds tokens 4 q + i, columns NV m + l.
-template <bool BF16, int NV>
-__device__ __forceinline__ void gate_grad_add(const uint4 (&dp)[4], uint32_t have, f32x4_t (&o)[NV]) {
+template <bool BF16, int NV, typename Piece>
+__device__ __forceinline__ void gate_grad_add(const Piece (&dp)[4], uint32_t have, f32x4_t (&o)[NV]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float u[NV];
-    unpack16<BF16>(zero_unless((have >> i & 1u) != 0, dp[i]), u);
+    unpack<BF16>(zero_unless((have >> i & 1u) != 0, dp[i]), u);
 #pragma unroll
     for (int l = 0; l < NV; ++l) o[l][i] += u[l];
   }
 }
 
 template <bool BF16, int EC, int K, bool DISPATCH>
-__global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(GateGradArgs a) {
+__global__ __launch_bounds__(256, 2) void gate_backward_kernel(GateGradArgs a) {
   using C = GateGradCfg<BF16, EC>;
   constexpr int EP = C::EP, S = C::S, LD = C::LD, NV = C::NV, COLS = C::COLS, KB = C::KB, KS = C::KS;
   constexpr bool SECOND = DISPATCH && K > 1;
@@ -198,11 +234,11 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
   const int split = id / blocks, c0 = id % blocks * COLS;
   const int cols = min(COLS, a.d - c0);
   const bool in = NV * m < cols;                      // (lanes past the end move what they do not use)
-  const int64_t col_byte = static_cast<int64_t>(c0 + min(NV * m, cols - NV)) * (16 / NV);
+  const int64_t col_byte = static_cast<int64_t>(c0 + min(NV * m, cols - NV)) * C::EB;
   const int64_t step = static_cast<int64_t>(a.splits) * 4 * GG_TOK;
   int64_t t0 = (static_cast<int64_t>(split) * 4 + wave) * GG_TOK;
   GateGradStep<BF16, EC> n;
-  uint4 dp[4];                                        // the encode's rows of the first choice
+  typename C::Piece dp[4];                                        // the encode's rows of the first choice
   uint32_t have = 0;
   if (t0 < a.T) gate_grad_load<BF16, EC, K, DISPATCH>(a, t0, col_byte, lane, n);
 
@@ -279,7 +315,7 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
     const uint32_t use = static_cast<uint32_t>(__ballot(m < left && n.mask != 0)) & 0xffffu;
     n.idx = lane < left * K && n.idx < a.E ? n.idx : -1;
     // rows of the second choice where there are registers for them, then everything the next step reads
-    uint4 second[4];
+    typename C::Piece second[4];
     uint32_t have_second = 0;
     if (SECOND) have_second = gate_grad_rows<K>(a, t0, col_byte, lane, n.dst, 1, second);
     const bool last = t0 + step >= a.T;
@@ -340,7 +376,7 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
       for (int j = 0; j < NV; ++j) {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = j < 2 ? n.x[i].x : j < 4 ? n.x[i].y : j < 6 ? n.x[i].z : n.x[i].w;
+        for (int i = 0; i < 4; ++i) w[i] = word(n.x[i], j / 2);
 #pragma unroll
         for (int i = 0; i < 2; ++i) xa[j].w[i] = j & 1 ? high_halves(w[2 * i], w[2 * i + 1]) : low_halves(w[2 * i], w[2 * i + 1]);
       }
@@ -361,7 +397,7 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float xv[NV];
-          unpack16<BF16>(n.x[i], xv);
+          unpack<BF16>(n.x[i], xv);
 #pragma unroll
           for (int j = 0; j < NV; ++j) acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(xv[j], v[i], acc[c][j], 0, 0, 0);
         }
@@ -426,8 +462,10 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
 #pragma unroll
       for (int j = 0; j < NV; ++j) v[j] = o[j][i];
       unsigned char* const to = a.dx + t * a.lddx + col_byte;
-      if (a.stream) store16<true>(to, pack16<BF16>(v));
-      else store16(to, pack16<BF16>(v));
+      typename C::Piece out;
+      pack<BF16>(v, out);
+      if (a.stream) store_piece<true>(to, out);
+      else store_piece<false>(to, out);
     }
   }
 
@@ -488,14 +526,16 @@ __global__ __launch_bounds__(256, EC == 4 ? 1 : 2) void gate_backward_kernel(Gat
   }
 }
 
-static int gate_grad_cols(int dtype) { return dtype == SCMOE_BF16 ? GateGradCfg<true, 1>::COLS : GateGradCfg<false, 1>::COLS; }
+static int gate_grad_cols(int E, int dtype) {
+  return dtype != SCMOE_BF16 ? GateGradCfg<false, 1>::COLS : E > 32 ? GateGradCfg<true, 4>::COLS : GateGradCfg<true, 1>::COLS;
+}
 
-// Workgroups that share a column block, each with a part of dW_g to leave: as many as are resident together (two per compute unit,
-// one beyond 32 experts), and no more than it takes for the same number of turns.
+// Workgroups that share a column block, each with a part of dW_g to leave: as many as are resident together (two per compute unit),
+// and no more than it takes for the same number of turns.
 static int gate_grad_splits(int T, int d, int E, int dtype) {
-  const int blocks = (d + gate_grad_cols(dtype) - 1) / gate_grad_cols(dtype);
+  const int blocks = (d + gate_grad_cols(E, dtype) - 1) / gate_grad_cols(E, dtype);
   const int64_t groups = (static_cast<int64_t>(T) + 4 * GG_TOK - 1) / (4 * GG_TOK);
-  const int resident = (E <= 32 ? 2 : 1) * num_cus();
+  const int resident = 2 * num_cus();
   const int64_t most = resident > blocks ? resident / blocks : 1;
   const int64_t turns = (groups + most - 1) / most;
   return turns < 1 ? 1 : static_cast<int>((groups + turns - 1) / turns);
@@ -505,7 +545,7 @@ static int64_t gate_grad_stride(int d, int E) { return (static_cast<int64_t>(d) 
 
 static size_t gate_grad_bytes(int T, int d, int E) {        // (for either type)
   const int b = gate_grad_splits(T, d, E, SCMOE_BF16), f = gate_grad_splits(T, d, E, SCMOE_F32), s = b > f ? b : f;
-  const size_t blocks = (d + gate_grad_cols(SCMOE_F32) - 1) / gate_grad_cols(SCMOE_F32);
+  const size_t blocks = (d + gate_grad_cols(E, SCMOE_F32) - 1) / gate_grad_cols(E, SCMOE_F32);
   return s == 1 ? 0 : static_cast<size_t>(s) * (gate_grad_stride(d, E) * 4 + 8 * blocks);   // parts and marks
 }
 
@@ -513,7 +553,8 @@ static size_t gate_grad_bytes(int T, int d, int E) {        // (for either type)
 constexpr int64_t GATE_GRAD_ONE_LAUNCH = 64 << 10;
 
 static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
-  dim3 grid(((a.d + gate_grad_cols(dtype) - 1) / gate_grad_cols(dtype) * a.splits + 7) / 8 * 8), block(256);
+  const int cols = gate_grad_cols(a.E, dtype);
+  dim3 grid(((a.d + cols - 1) / cols * a.splits + 7) / 8 * 8), block(256);
   const bool dispatch = a.dst_row != nullptr;
 #define SCMOE_GATE_GRAD_K(EC, K)                                                                                             \
   do {                                                                                                                       \
@@ -585,7 +626,7 @@ extern "C" int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, co
   a.Wg16 = E % 4 == 0 && aligned16(W_g);
   a.parts = static_cast<float*>(workspace); a.stride = gate_grad_stride(d, E);
   a.dWg = dW_g; a.dbias = dbias;
-  if (a.splits > 1 && static_cast<int64_t>(a.splits) * gate_grad_cols(dtype) * E * 4 <= GATE_GRAD_ONE_LAUNCH) {
+  if (a.splits > 1 && static_cast<int64_t>(a.splits) * gate_grad_cols(E, dtype) * E * 4 <= GATE_GRAD_ONE_LAUNCH) {
     a.marks = reinterpret_cast<unsigned long long*>(a.parts + a.splits * a.stride);
     a.call = next_call();
   }
