@@ -218,6 +218,7 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
     } else {
       norm_grad_load<P, STEP, ST>(a, live ? row : last, lane, pieces, q);
     }
+    if (!live) q.mean = q.rstd = 0.0f;                  // (a row that is there for the barrier adds zeros, whatever the last row holds)
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
