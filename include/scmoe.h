@@ -28,6 +28,8 @@
  *  - bf16 buffers must be 16-byte aligned with row strides that are multiples of 8
  *    elements; fp32 buffers 16-byte aligned with strides that are multiples of 4.
  *    d and F must be multiples of 8.  Violations give SCMOE_ERR_SHAPE.
+ *  - A workspace need not be cleared and may serve calls of any kind that follow each other on one
+ *    stream; calls that may run at the same time (eager or in replayed graphs) need one each.
  *  - T == 0 is legal everywhere (no-op, SCMOE_OK; sums over the tokens are written: zeros).
  */
 #ifndef SCMOE_H

