@@ -42,15 +42,25 @@ __device__ __forceinline__ bool last_to_arrive(unsigned long long* marks, unsign
   return true;
 }
 
-// Sum over `n` parts, `stride` floats apart, of the two floats at each; in their order.
+// Sum over `n` parts, `stride` floats apart, of the two floats at each; in their order, N loads in flight together (the last of them
+// again where there are no more: a loop over a remainder would wait for each).
+template <int N>
+__device__ __forceinline__ void add_left(const float* part, int from, int n, int64_t stride, float2& v) {
+  unsigned long long q[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) q[i] = left_there(reinterpret_cast<const unsigned long long*>(part + min(from + i, n - 1) * stride));
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v.x += from + i < n ? __uint_as_float(static_cast<uint32_t>(q[i])) : 0.0f;
+    v.y += from + i < n ? __uint_as_float(static_cast<uint32_t>(q[i] >> 32)) : 0.0f;
+  }
+}
+
 __device__ __forceinline__ float2 sum_left(const float* part, int n, int64_t stride) {
   float2 v = make_float2(0.0f, 0.0f);
-#pragma unroll 16
-  for (int i = 0; i < n; ++i) {
-    const unsigned long long q = left_there(reinterpret_cast<const unsigned long long*>(part + i * stride));
-    v.x += __uint_as_float(static_cast<uint32_t>(q));
-    v.y += __uint_as_float(static_cast<uint32_t>(q >> 32));
-  }
+  int i = 0;
+  for (; i + 8 < n; i += 32) add_left<32>(part, i, n, stride, v);
+  if (i < n) add_left<8>(part, i, n, stride, v);
   return v;
 }
 

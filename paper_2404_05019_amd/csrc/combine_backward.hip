@@ -22,14 +22,12 @@ struct CombineGradArgs {
   float* dcoef;                                // [T][2]
 };
 
-// A token belongs to W waves, or to L lanes of one (narrow rows); PER pieces of 16 bytes per lane are in flight at a time.
-template <bool BF16, int K, int W, int L, int PER, bool ST>
+// A token belongs to L lanes of a wave; PER pieces of 16 bytes per lane are in flight at a time.
+template <bool BF16, int K, int L, int PER, bool ST>
 __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a) {
-  constexpr int NV = BF16 ? 8 : 4, STEP = L * W, TOK = 256 / STEP;
-  __shared__ float part[2][4][K + 1];
-  const int lane = threadIdx.x % STEP, wave = threadIdx.x >> 6;
-  int turn = 0;
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * TOK + threadIdx.x / STEP; t < a.T; t += static_cast<int64_t>(gridDim.x) * TOK) {
+  constexpr int NV = BF16 ? 8 : 4, TOK = 256 / L;
+  const int lane = threadIdx.x % L;
+  for (int64_t t = static_cast<int64_t>(blockIdx.x) * TOK + threadIdx.x / L; t < a.T; t += static_cast<int64_t>(gridDim.x) * TOK) {
     int64_t r[K];
     float w[K], dot[K + 1];
 #pragma unroll
@@ -41,12 +39,12 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a
     for (int j = 0; j <= K; ++j) dot[j] = 0.0f;
     const float c0 = a.coef == nullptr ? 1.0f : a.coef[2 * t], c1 = a.coef == nullptr ? 1.0f : a.coef[2 * t + 1];
     const unsigned char* dyr = a.dy + t * a.lddy;
-    for (int p0 = lane; p0 < a.pieces; p0 += PER * STEP) {
+    for (int p0 = lane; p0 < a.pieces; p0 += PER * L) {
       uint4 g[PER], y[K][PER], b[PER];
       int64_t at[PER];
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
-        at[p] = static_cast<int64_t>(min(p0 + p * STEP, a.pieces - 1)) * 16;
+        at[p] = static_cast<int64_t>(min(p0 + p * L, a.pieces - 1)) * 16;
         g[p] = load16<ST>(dyr + at[p]);
       }
       if (a.yp != nullptr) {
@@ -63,7 +61,7 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a
       }
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
-        if (p0 + p * STEP >= a.pieces) continue;
+        if (p0 + p * L >= a.pieces) continue;
         float v[NV], u[NV], o[NV];
         unpack16<BF16>(g[p], v);
         if (a.base != nullptr) {
@@ -96,20 +94,6 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a
     if (a.yp == nullptr && a.base == nullptr) continue;
 #pragma unroll
     for (int j = 0; j <= K; ++j) dot[j] = wave_sum<L>(dot[j]);
-    if (W > 1) {
-      if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-        for (int j = 0; j <= K; ++j) part[turn][wave][j] = dot[j];
-      }
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j <= K; ++j) {
-        dot[j] = 0.0f;
-#pragma unroll
-        for (int v = 0; v < W; ++v) dot[j] += part[turn][v][j];
-      }
-      turn ^= 1;
-    }
     if (lane != 0) continue;
     float dc1 = 0.0f;
 #pragma unroll
@@ -127,29 +111,27 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(CombineGradArgs a
 constexpr int COMBINE_GRAD_MAX_GROUPS = 1 << 20;   // keeps the threads of a launch under 2^32
 
 static int combine_backward(const CombineGradArgs& a, int dtype, int k, hipStream_t stream) {
-  // Four waves on a token's row where there are too few tokens to fill the chip with one each; lanes of a wave share out several tokens
-  // whose rows one piece per lane covers (32768 tokens of 128, two each, bf16: 10.8 us with 16 lanes, 20.1 with 64), and wider rows keep
-  // no more pieces in flight than they have (32768 of 384, bf16: 15.7 us with one piece per lane, 22.1 with four).
-  const bool wide = a.T < 8 * num_cus() && a.pieces > 64;
-  const int lanes = wide ? 256 : a.pieces <= 16 ? 16 : a.pieces <= 32 ? 32 : 64;
+  // Lanes of a wave share out several tokens whose rows one piece per lane covers (32768 tokens of 128, two each, bf16: 10.8 us with 16
+  // lanes, 20.1 with 64), and wider rows keep no more pieces in flight than they have (32768 of 384, bf16: 15.7 us with one piece per
+  // lane, 22.1 with four).  Several waves on a row gained nothing for any number of tokens.
+  const int lanes = a.pieces <= 16 ? 16 : a.pieces <= 32 ? 32 : 64;
   const int64_t groups = (static_cast<int64_t>(a.T) + 256 / lanes - 1) / (256 / lanes);
   dim3 grid(static_cast<unsigned>(groups < COMBINE_GRAD_MAX_GROUPS ? groups : COMBINE_GRAD_MAX_GROUPS)), block(256);
   const int64_t rows = 1 + (a.base ? 1 : 0) + (a.dbase ? 1 : 0) + k * ((a.yp ? 1 : 0) + (a.dyp ? 1 : 0));
   const bool st = a.pieces > 128 && streams_past_caches(rows * a.T * a.pieces * 16);
-#define SCMOE_COMBINE_GRAD_L(K, W, L, PER, ST)                                                                                       \
-  do {                                                                                                                               \
-    if (dtype == SCMOE_BF16) hipLaunchKernelGGL((combine_backward_kernel<true, K, W, L, PER, ST>), grid, block, 0, stream, a);       \
-    else hipLaunchKernelGGL((combine_backward_kernel<false, K, W, L, PER, ST>), grid, block, 0, stream, a);                          \
+#define SCMOE_COMBINE_GRAD_L(K, L, PER, ST)                                                                                    \
+  do {                                                                                                                         \
+    if (dtype == SCMOE_BF16) hipLaunchKernelGGL((combine_backward_kernel<true, K, L, PER, ST>), grid, block, 0, stream, a);    \
+    else hipLaunchKernelGGL((combine_backward_kernel<false, K, L, PER, ST>), grid, block, 0, stream, a);                       \
   } while (0)
-#define SCMOE_COMBINE_GRAD(K)                                                               \
-  do {                                                                                      \
-    if (wide) SCMOE_COMBINE_GRAD_L(K, 4, 64, 1, false);                                     \
-    else if (lanes == 16) SCMOE_COMBINE_GRAD_L(K, 1, 16, 1, false);                         \
-    else if (lanes == 32) SCMOE_COMBINE_GRAD_L(K, 1, 32, 1, false);                         \
-    else if (a.pieces <= 64) SCMOE_COMBINE_GRAD_L(K, 1, 64, 1, false);                      \
-    else if (a.pieces <= 128) SCMOE_COMBINE_GRAD_L(K, 1, 64, 2, false);                     \
-    else if (st) SCMOE_COMBINE_GRAD_L(K, 1, 64, (K == 1 ? 4 : 2), true);                    \
-    else SCMOE_COMBINE_GRAD_L(K, 1, 64, (K == 1 ? 4 : 2), false);                           \
+#define SCMOE_COMBINE_GRAD(K)                                                        \
+  do {                                                                               \
+    if (lanes == 16) SCMOE_COMBINE_GRAD_L(K, 16, 1, false);                          \
+    else if (lanes == 32) SCMOE_COMBINE_GRAD_L(K, 32, 1, false);                     \
+    else if (a.pieces <= 64) SCMOE_COMBINE_GRAD_L(K, 64, 1, false);                  \
+    else if (a.pieces <= 128) SCMOE_COMBINE_GRAD_L(K, 64, 2, false);                 \
+    else if (st) SCMOE_COMBINE_GRAD_L(K, 64, (K == 1 ? 4 : 2), true);                \
+    else SCMOE_COMBINE_GRAD_L(K, 64, (K == 1 ? 4 : 2), false);                       \
   } while (0)
   static_assert(SCMOE_MAX_TOPK == 4, "one instantiation per k below");
   switch (k) {
