@@ -557,9 +557,11 @@ static size_t gate_grad_bytes(int T, int d, int E) {        // (for either type)
   return s == 1 ? 0 : static_cast<size_t>(s) * (gate_grad_stride(d, E) * 4 + 8 * blocks);   // parts and marks
 }
 
-// Where a column block's parts are few bytes, its last workgroup adds them up in the same launch (256 tokens of 64, 4 experts, fp32:
-// 9.6 us a call in place of 12.5).
-constexpr int64_t GATE_GRAD_ONE_LAUNCH = 64 << 10;
+// A column block's last workgroup adds up its parts in the same launch where they are few and small: as many as it reads in one go.
+// 512 tokens of 1024, bf16, a call (one launch / two): 8 experts 10.8 / 13.9 us, 16 11.9 / 13.9; 1024 tokens (16 parts), 8 experts
+// 13.1 / 13.8, and 30.9 / 27.4 where the caller waits for each; 256 tokens, 32 experts (16 KB) 15.8 / 13.6.
+constexpr int GATE_GRAD_FEW_PARTS = 8;
+constexpr int64_t GATE_GRAD_SMALL_PART = 8 << 10;
 
 static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
   const int cols = gate_grad_cols(a.E, dtype);
@@ -635,7 +637,7 @@ extern "C" int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, co
   a.Wg16 = E % 4 == 0 && aligned16(W_g);
   a.parts = static_cast<float*>(workspace); a.stride = gate_grad_stride(d, E);
   a.dWg = dW_g; a.dbias = dbias;
-  if (a.splits > 1 && static_cast<int64_t>(a.splits) * gate_grad_cols(E, dtype) * E * 4 <= GATE_GRAD_ONE_LAUNCH) {
+  if (a.splits > 1 && a.splits <= GATE_GRAD_FEW_PARTS && gate_grad_cols(E, dtype) * E * 4 <= GATE_GRAD_SMALL_PART) {
     a.marks = reinterpret_cast<unsigned long long*>(a.parts + a.splits * a.stride);
     a.call = next_call();
   }

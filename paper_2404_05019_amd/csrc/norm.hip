@@ -349,14 +349,18 @@ static int norm_grad_rows(int d, int dtype) {
 }
 
 // One workgroup per compute unit, each with a part of 8 d bytes to leave.  Where the parts are few bytes, or would be with up to four
-// turns for each workgroup, the last one adds them up in the same launch (78 rows of 312: 8.5 us a call in place of 13.5).
-constexpr int64_t NORM_GRAD_ONE_LAUNCH = 128 << 10;
+// turns for each workgroup, the last one adds them up in the same launch: up to 32 parts, which it reads in one go, of 64 KB in all.  A
+// call of 256 rows of 512, bf16, 9.0 us (two launches 11.4), 4096 of 128 9.3 (11.4), 256 of 1024 11.0 (11.7), 64 of 2048 11.3 (11.3); with
+// 128 KB 512 of 1024 14.9 (11.7).  Where the caller waits for each call two launches are up to 4 us faster (512 rows of 512 22.1 / 26.2).
+constexpr int64_t NORM_GRAD_ONE_LAUNCH = 64 << 10;
+constexpr int64_t NORM_GRAD_FEW_PARTS = 32;
 
 static int norm_grad_groups(int T, int d, int dtype, bool* one_launch) {
   const int rows = norm_grad_rows(d, dtype);
-  const int64_t most = (static_cast<int64_t>(T) + rows - 1) / rows, fit = NORM_GRAD_ONE_LAUNCH / (8 * d);
-  const int64_t groups = most < num_cus() ? most : num_cus();
-  *one_launch = groups <= fit || most <= 4 * fit;
+  const int64_t most = (static_cast<int64_t>(T) + rows - 1) / rows, groups = most < num_cus() ? most : num_cus();
+  int64_t fit = NORM_GRAD_ONE_LAUNCH / (8 * d);
+  fit = fit < 1 ? 1 : fit < NORM_GRAD_FEW_PARTS ? fit : NORM_GRAD_FEW_PARTS;
+  *one_launch = most <= 4 * fit;
   return static_cast<int>(*one_launch && groups > fit ? fit : groups);
 }
 

@@ -633,8 +633,8 @@ def test_small_calls_in_graphs(dtype):
         assert all(torch.equal(a, b) for a, b in zip(want, (dx, dh, load, *sums)))
 
 
-@pytest.mark.parametrize("T,d", [(1, 64), (8, 1024), (9, 1024), (64 * 8, 1024), (64 * 8 + 1, 1024), (255 * 8, 64), (2600, 64), (16, 4096), (17, 4096),
-                                 (4, 16384), (5, 16384)])
+@pytest.mark.parametrize("T,d", [(1, 64), (8, 1024), (9, 1024), (32 * 8, 1024), (32 * 8 + 1, 1024), (64 * 8, 1024), (64 * 8 + 1, 1024), (255 * 8, 64),
+                                 (2600, 64), (128 * 32, 64), (128 * 32 + 1, 64), (16, 4096), (17, 4096), (4, 16384), (5, 16384)])
 def test_norm_gradient_sums_on_both_sides_of_their_rules(T, d):
     """One workgroup, one launch, one launch with more turns, two launches: dgamma and dbeta."""
     g = gen(T)
