@@ -6,7 +6,7 @@
 //   dW_g = x^T dl,  dbias = sum_t dl,  dx = dl W_g^T + the encode's gradient rows gathered by dst_row
 //
 // Bound by HBM where there are many tokens and up to 32 experts (32768 tokens of 2048, 16 experts, bf16, with the encode: 76 us for
-// 410 MB, and 5 us for adding up the parts); by issue beyond (64 experts, two each: 212 us, where every column block works out
+// 410 MB, and 5 us for adding up the parts); by issue beyond (64 experts, two each: 222 us, where every column block works out
 // dl of its tokens anew and the products take 31 us of matrix pipe); by the chain of one step and the kernel's start and end where there are
 // few tokens (5003 of 1024, 32 experts: 23 us, of which the rows' loads 10, W_g 3, sums 2).
 #include "arrival.hpp"
@@ -29,7 +29,6 @@ struct GateGradArgs {
   float* dWg; float* dbias;
   int splits;
   unsigned long long* marks; unsigned long long call;   // one launch: the last workgroup of a column block adds up its parts (nullptr: not)
-  int stream;                                   // rows are moved past the caches (streams_past_caches)
 };
 
 // A workgroup has COLS columns and every `splits`-th group of 64 tokens, a wave 16 tokens of it at a time.  Outputs of both
@@ -38,7 +37,7 @@ struct GateGradArgs {
 //   dW_g: rows = columns, k = tokens:  lane (m, q) holds x[tokens 4 q + i, columns NV m + j] as it was loaded, and
 //         dl[tokens 4 q + i, expert m] through LDS
 // Column tile j of a lane's NV is column NV m + j, so rows of x and dx are moved in pieces of 16 bytes (8 for bf16 beyond 32
-// experts, whose accumulators leave room for two waves per SIMD only so: 4 tokens 12.6 -> 8.6 us, many as before) and nothing is
+// experts, whose accumulators leave room for two waves per SIMD only so: 4 tokens 12.6 -> 8.6 us, 32768 of 2048 217 -> 222) and nothing is
 // shuffled.  fp32: the fp32 instruction (k = 4).  bf16: the bf16 ones (k = 16 and 32, 8 and 16 times the rate):
 //   dx:   dl and W_g each as two bf16 parts, rounded, 2^-16 of the value; the product of the low parts is left out
 //   dW_g: x is bf16; dl in three truncated parts, which hold its 24 bits exactly
@@ -97,6 +96,9 @@ __device__ __forceinline__ uint32_t word(const uint2& q, int i) { return i == 0 
 // Tokens of a step.
 __device__ __forceinline__ int gate_grad_left(const GateGradArgs& a, int64_t t0) { return a.T - t0 < GG_TOK ? static_cast<int>(a.T - t0) : GG_TOK; }
 
+// ST: rows are moved past the caches (streams_past_caches); a choice at run time between the two kinds of store came out of the compiler
+// as one, without the hint.
+
 // What a step reads, as it lies in memory: loaded a step ahead, so nothing here may be looked at (and waited for) before it is due.
 template <bool BF16, int EC>
 struct GateGradStep {
@@ -107,7 +109,7 @@ struct GateGradStep {
   uint32_t mask;                       // token m
 };
 
-template <bool BF16, int EC, int K, bool DISPATCH>
+template <bool BF16, int EC, int K, bool DISPATCH, bool ST>
 __device__ __forceinline__ void gate_grad_load(const GateGradArgs& a, int64_t t0, int64_t col_byte, int lane, GateGradStep<BF16, EC>& n) {
   using C = GateGradCfg<BF16, EC>;
   const int m = lane & 15, q = lane >> 4;
@@ -138,13 +140,8 @@ __device__ __forceinline__ void gate_grad_load(const GateGradArgs& a, int64_t t0
 #pragma unroll
     for (int s = 0; s < C::S; ++s) n.p[s] = row[min(C::S * q + s, a.E - 1)];
   }
-  if (a.stream) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_piece<true>(a.x + (t0 + min(4 * q + i, left - 1)) * a.ldx + col_byte, n.x[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) load_piece<false>(a.x + (t0 + min(4 * q + i, left - 1)) * a.ldx + col_byte, n.x[i]);
-  }
+  for (int i = 0; i < 4; ++i) load_piece<ST>(a.x + (t0 + min(4 * q + i, left - 1)) * a.ldx + col_byte, n.x[i]);
 }
 
 template <int N>
@@ -189,7 +186,7 @@ __device__ __forceinline__ void split3(const float* v, Bf16Parts<4> (&part)[3]) 
 }
 
 // Rows of the encode's gradient for choice j of tokens 4 q + i, as far as they were kept.
-template <int K, typename Piece>
+template <int K, bool ST, typename Piece>
 __device__ __forceinline__ uint32_t gate_grad_rows(const GateGradArgs& a, int64_t t0, int64_t col_byte, int lane, int dst, int j, Piece (&dp)[4]) {
   uint32_t have = 0;
   const int items = gate_grad_left(a, t0) * K;
@@ -202,13 +199,8 @@ __device__ __forceinline__ uint32_t gate_grad_rows(const GateGradArgs& a, int64_
     // (no row: the x of the step's first token, which is there)
     at[i] = (there ? a.dxp + r * a.lddxp : a.x + t0 * a.ldx) + col_byte;
   }
-  if (a.stream) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_piece<true>(at[i], dp[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) load_piece<false>(at[i], dp[i]);
-  }
+  for (int i = 0; i < 4; ++i) load_piece<ST>(at[i], dp[i]);
   return have;
 }
 
@@ -224,7 +216,7 @@ __device__ __forceinline__ void gate_grad_add(const Piece (&dp)[4], uint32_t hav
   }
 }
 
-template <bool BF16, int EC, int K, bool DISPATCH>
+template <bool BF16, int EC, int K, bool DISPATCH, bool ST>
 __global__ __launch_bounds__(256, 2) void gate_backward_kernel(GateGradArgs a) {
   using C = GateGradCfg<BF16, EC>;
   constexpr int EP = C::EP, S = C::S, LD = C::LD, NV = C::NV, COLS = C::COLS, KB = C::KB, KS = C::KS;
@@ -248,7 +240,7 @@ __global__ __launch_bounds__(256, 2) void gate_backward_kernel(GateGradArgs a) {
   GateGradStep<BF16, EC> n;
   typename C::Piece dp[4];                                        // the encode's rows of the first choice
   uint32_t have = 0;
-  if (t0 < a.T) gate_grad_load<BF16, EC, K, DISPATCH>(a, t0, col_byte, lane, n);
+  if (t0 < a.T) gate_grad_load<BF16, EC, K, DISPATCH, ST>(a, t0, col_byte, lane, n);
 
   // W_g as operands of dx, in the order in which the lanes read them
   const float* const wg = a.Wg + static_cast<int64_t>(c0) * a.E;
@@ -298,7 +290,7 @@ __global__ __launch_bounds__(256, 2) void gate_backward_kernel(GateGradArgs a) {
       wl[e * COLS + c] = c < cols && e < a.E ? v[n] : 0.0f;
     }
   }
-  if (DISPATCH && t0 < a.T) have = gate_grad_rows<K>(a, t0, col_byte, lane, n.dst, 0, dp);
+  if (DISPATCH && t0 < a.T) have = gate_grad_rows<K, ST>(a, t0, col_byte, lane, n.dst, 0, dp);
   float slope[S];
 #pragma unroll
   for (int s = 0; s < S; ++s) slope[s] = a.slope != nullptr && S * q + s < a.E ? a.slope[S * q + s] * (a.dloss != nullptr ? a.dloss[0] : 1.0f) : 0.0f;
@@ -325,10 +317,10 @@ __global__ __launch_bounds__(256, 2) void gate_backward_kernel(GateGradArgs a) {
     // rows of the second choice where there are registers for them, then everything the next step reads
     typename C::Piece second[4];
     uint32_t have_second = 0;
-    if (SECOND) have_second = gate_grad_rows<K>(a, t0, col_byte, lane, n.dst, 1, second);
+    if (SECOND) have_second = gate_grad_rows<K, ST>(a, t0, col_byte, lane, n.dst, 1, second);
     const bool last = t0 + step >= a.T;
     GateGradStep<BF16, EC> ahead = n;
-    if (!last) gate_grad_load<BF16, EC, K, DISPATCH>(a, t0 + step, col_byte, lane, ahead);
+    if (!last) gate_grad_load<BF16, EC, K, DISPATCH, ST>(a, t0 + step, col_byte, lane, ahead);
     // dl of token m, experts S q + s
     float dl[S];
     {
@@ -455,13 +447,13 @@ __global__ __launch_bounds__(256, 2) void gate_backward_kernel(GateGradArgs a) {
       for (int j = SECOND ? 2 : 1; j < K; ++j) {
         int dst = n.dst;
         asm volatile("" : "+v"(dst)::"memory");       // (no earlier: their addresses would take registers from here to the top)
-        have = gate_grad_rows<K>(a, t0, col_byte, lane, dst, j, dp);
+        have = gate_grad_rows<K, ST>(a, t0, col_byte, lane, dst, j, dp);
         gate_grad_add<BF16>(dp, have, o);
       }
     }
     loads_have_arrived();
     n = ahead;
-    if (DISPATCH && !last) have = gate_grad_rows<K>(a, t0 + step, col_byte, lane, n.dst, 0, dp);
+    if (DISPATCH && !last) have = gate_grad_rows<K, ST>(a, t0 + step, col_byte, lane, n.dst, 0, dp);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int64_t t = t0 + 4 * q + i;
@@ -472,8 +464,7 @@ __global__ __launch_bounds__(256, 2) void gate_backward_kernel(GateGradArgs a) {
       unsigned char* const to = a.dx + t * a.lddx + col_byte;
       typename C::Piece out;
       pack<BF16>(v, out);
-      if (a.stream) store_piece<true>(to, out);
-      else store_piece<false>(to, out);
+      store_piece<ST>(to, out);
     }
   }
 
@@ -567,12 +558,18 @@ static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
   const int cols = gate_grad_cols(a.E, dtype);
   dim3 grid(((a.d + cols - 1) / cols * a.splits + 7) / 8 * 8), block(256);
   const bool dispatch = a.dst_row != nullptr;
-#define SCMOE_GATE_GRAD_K(EC, K)                                                                                             \
-  do {                                                                                                                       \
-    if (dtype == SCMOE_BF16 && dispatch) hipLaunchKernelGGL((gate_backward_kernel<true, EC, K, true>), grid, block, 0, stream, a);        \
-    else if (dtype == SCMOE_BF16) hipLaunchKernelGGL((gate_backward_kernel<true, EC, K, false>), grid, block, 0, stream, a);              \
-    else if (dispatch) hipLaunchKernelGGL((gate_backward_kernel<false, EC, K, true>), grid, block, 0, stream, a);                         \
-    else hipLaunchKernelGGL((gate_backward_kernel<false, EC, K, false>), grid, block, 0, stream, a);                                      \
+  const bool st = streams_past_caches(static_cast<int64_t>(a.T) * a.d * elem_bytes(dtype) * (dispatch ? 2 + a.k : 2));
+#define SCMOE_GATE_GRAD_ST(EC, K, ST)                                                                                                      \
+  do {                                                                                                                                     \
+    if (dtype == SCMOE_BF16 && dispatch) hipLaunchKernelGGL((gate_backward_kernel<true, EC, K, true, ST>), grid, block, 0, stream, a);     \
+    else if (dtype == SCMOE_BF16) hipLaunchKernelGGL((gate_backward_kernel<true, EC, K, false, ST>), grid, block, 0, stream, a);           \
+    else if (dispatch) hipLaunchKernelGGL((gate_backward_kernel<false, EC, K, true, ST>), grid, block, 0, stream, a);                      \
+    else hipLaunchKernelGGL((gate_backward_kernel<false, EC, K, false, ST>), grid, block, 0, stream, a);                                   \
+  } while (0)
+#define SCMOE_GATE_GRAD_K(EC, K)                    \
+  do {                                              \
+    if (st) SCMOE_GATE_GRAD_ST(EC, K, true);        \
+    else SCMOE_GATE_GRAD_ST(EC, K, false);          \
   } while (0)
 #define SCMOE_GATE_GRAD(EC)                      \
   switch (a.k) {                                 \
@@ -587,6 +584,7 @@ static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
   else { SCMOE_GATE_GRAD(4) }
 #undef SCMOE_GATE_GRAD
 #undef SCMOE_GATE_GRAD_K
+#undef SCMOE_GATE_GRAD_ST
   if (const int st = launch_status()) return st;
   if (a.splits == 1 || a.marks != nullptr) return SCMOE_OK;
   return sum_parts(a.parts, a.splits, a.stride, a.dWg, static_cast<int64_t>(a.d) * a.E, a.dbias, a.E, stream);
@@ -632,7 +630,6 @@ extern "C" int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, co
   a.dxp = static_cast<const unsigned char*>(dx_perm); a.lddxp = ld_perm * eb; a.dst_row = dst_row;
   a.dx = static_cast<unsigned char*>(dx); a.lddx = lddx * eb;
   a.splits = gate_grad_splits(T, d, E, dtype);
-  a.stream = streams_past_caches(static_cast<int64_t>(T) * d * eb * (dx_perm ? 2 + k : 2));
   a.probs16 = E % 4 == 0 && aligned16(probs);
   a.Wg16 = E % 4 == 0 && aligned16(W_g);
   a.parts = static_cast<float*>(workspace); a.stride = gate_grad_stride(d, E);
