@@ -46,24 +46,25 @@ __device__ __forceinline__ bool last_to_arrive(unsigned long long* marks, unsign
 // again where there are no more: a loop over a remainder would wait for each).  A load past the caches costs also where it is repeated:
 // with N to fit 512 rows of 512 took 9.2 us a call, with 32 for any number 10.5.
 template <int N>
-__device__ __forceinline__ void add_left(const float* part, int from, int n, int64_t stride, float2& v) {
+__device__ __forceinline__ void add_left(const float* part, int n, int64_t stride, float2& v) {
   unsigned long long q[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) q[i] = left_there(reinterpret_cast<const unsigned long long*>(part + min(from + i, n - 1) * stride));
+  for (int i = 0; i < N; ++i) q[i] = left_there(reinterpret_cast<const unsigned long long*>(part + min(i, n - 1) * stride));
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    v.x += from + i < n ? __uint_as_float(static_cast<uint32_t>(q[i])) : 0.0f;
-    v.y += from + i < n ? __uint_as_float(static_cast<uint32_t>(q[i] >> 32)) : 0.0f;
+    v.x += i < n ? __uint_as_float(static_cast<uint32_t>(q[i])) : 0.0f;
+    v.y += i < n ? __uint_as_float(static_cast<uint32_t>(q[i] >> 32)) : 0.0f;
   }
 }
 
+constexpr int MOST_LEFT = 32;          // parts that sum_left takes
+
 __device__ __forceinline__ float2 sum_left(const float* part, int n, int64_t stride) {
   float2 v = make_float2(0.0f, 0.0f);
-  if (n <= 4) add_left<4>(part, 0, n, stride, v);
-  else if (n <= 8) add_left<8>(part, 0, n, stride, v);
-  else if (n <= 16) add_left<16>(part, 0, n, stride, v);
-  else
-    for (int i = 0; i < n; i += 32) add_left<32>(part, i, n, stride, v);
+  if (n <= 4) add_left<4>(part, n, stride, v);
+  else if (n <= 8) add_left<8>(part, n, stride, v);
+  else if (n <= 16) add_left<16>(part, n, stride, v);
+  else add_left<MOST_LEFT>(part, n, stride, v);
   return v;
 }
 

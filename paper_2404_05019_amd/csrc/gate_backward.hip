@@ -552,6 +552,7 @@ static size_t gate_grad_bytes(int T, int d, int E) {        // (for either type)
 // 512 tokens of 1024, bf16, a call (one launch / two): 8 experts 10.8 / 13.9 us, 16 11.9 / 13.9; 1024 tokens (16 parts), 8 experts
 // 13.1 / 13.8, and 30.9 / 27.4 where the caller waits for each; 256 tokens, 32 experts (16 KB) 15.8 / 13.6.
 constexpr int GATE_GRAD_FEW_PARTS = 8;
+static_assert(GATE_GRAD_FEW_PARTS <= MOST_LEFT);
 constexpr int64_t GATE_GRAD_SMALL_PART = 8 << 10;
 
 static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {

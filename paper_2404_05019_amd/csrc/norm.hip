@@ -353,7 +353,7 @@ static int norm_grad_rows(int d, int dtype) {
 // call of 256 rows of 512, bf16, 9.0 us (two launches 11.4), 4096 of 128 9.3 (11.4), 256 of 1024 11.0 (11.7), 64 of 2048 11.3 (11.3); with
 // 128 KB 512 of 1024 14.9 (11.7).  Where the caller waits for each call two launches are up to 4 us faster (512 rows of 512 22.1 / 26.2).
 constexpr int64_t NORM_GRAD_ONE_LAUNCH = 64 << 10;
-constexpr int64_t NORM_GRAD_FEW_PARTS = 32;
+constexpr int64_t NORM_GRAD_FEW_PARTS = MOST_LEFT;
 
 static int norm_grad_groups(int T, int d, int dtype, bool* one_launch) {
   const int rows = norm_grad_rows(d, dtype);
