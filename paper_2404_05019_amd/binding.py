@@ -55,7 +55,8 @@ class ScmoeError(RuntimeError):
 
 
 _lib = None
-_current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+# (torch without GPU support has neither; the module, its constants and the size functions are there all the same)
+_current_stream, _current_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
 
 
 def lib():
@@ -149,6 +150,8 @@ def _ldw(t):
 
 def _stream(s):
     if s is None:
+        if _current_stream is None or _current_device is None:
+            return torch.cuda.current_stream().cuda_stream
         # (the handle alone: an object of the current stream costs 2.7 us, half of a small call)
         return _current_stream(_current_device())
     return s.cuda_stream if hasattr(s, "cuda_stream") else int(s)
