@@ -375,6 +375,16 @@ def _dense(t, n, dtype=torch.float32):
     return t.data_ptr()
 
 
+def _table(t, rows, cols, dtype=torch.float32):
+    """Address of [rows, cols] of that type without gaps (None: not given).  The rows may have several dimensions, and a flat tensor is
+    taken as it is; a transposed table has as many elements and is refused."""
+    if t is None:
+        return None
+    if t.shape[-1:] != (cols,) and cols != 1 and t.dim() != 1:
+        _refuse(t, "[%d, %d] of %s" % (rows, cols, dtype))
+    return _dense(t, rows * cols, dtype)
+
+
 def _mask(mask, T):
     """Address of one byte per token: torch.bool or torch.uint8."""
     return None if mask is None else _dense(mask, T, torch.bool if mask.dtype is torch.bool else torch.uint8)
@@ -424,7 +434,7 @@ def scmoe_balance_loss(probs, expert_idx, k, coef, load, mean_prob, slope, loss,
     """Loss, items per expert and the loss's slope in every counted token's probabilities."""
     T, E = probs.shape
     wp, nb = _scratch(workspace)
-    _check(lib().scmoe_balance_loss(_dense(probs, T * E), _dense(expert_idx, T * k, torch.int32), _mask(mask, T), T, E, k, coef,
+    _check(lib().scmoe_balance_loss(_table(probs, T, E), _table(expert_idx, T, k, torch.int32), _mask(mask, T), T, E, k, coef,
                                     _dense(load, E, torch.int32), _dense(mean_prob, E), _dense(slope, E), _dense(loss, 1), wp, nb,
                                     _stream(stream)), "scmoe_balance_loss")
 
@@ -446,9 +456,9 @@ def scmoe_gate_backward(x, W_g, probs, expert_idx, gate_w, dgate_w, dx, dW_g, db
         dx_perm = dst_row = None
     (xp, ldx), (dp, ldd), (pp, ldp) = _rows(x, shape, dtype), _rows(dx, shape, dtype), _packed(dx_perm, d, dtype)
     wp, nb = _scratch(workspace)
-    _check(lib().scmoe_gate_backward(xp, ldx, dtype_code(x), _dense(W_g, d * E), _dense(probs, T * E), _dense(expert_idx, T * k, torch.int32),
-                                     _dense(gate_w, T * k), _dense(dgate_w, T * k), _dense(slope, E), _dense(dloss, 1), _mask(mask, T),
-                                     T, d, E, k, normalize, pp, ldp, _dense(dst_row, T * k, torch.int32), dp, ldd, _dense(dW_g, d * E),
+    _check(lib().scmoe_gate_backward(xp, ldx, dtype_code(x), _table(W_g, d, E), _table(probs, T, E), _table(expert_idx, T, k, torch.int32),
+                                     _table(gate_w, T, k), _table(dgate_w, T, k), _dense(slope, E), _dense(dloss, 1), _mask(mask, T),
+                                     T, d, E, k, normalize, pp, ldp, _table(dst_row, T, k, torch.int32), dp, ldd, _table(dW_g, d, E),
                                      _dense(dbias, E), wp, nb, _stream(stream)), "scmoe_gate_backward")
 
 
@@ -461,6 +471,6 @@ def scmoe_combine_backward(dy, y_perm, dst_row, gate_w, k, dy_perm=None, dgate_w
         y_perm = dy
     (gp, ldg), (yp, ldy), (bp, ldb) = _rows(dy, shape, dtype), _packed(y_perm, d, dtype), _rows(base, shape, dtype)
     (pp, ldp), (op, ldo) = _packed(dy_perm, d, dtype), _rows(dbase, shape, dtype)
-    _check(lib().scmoe_combine_backward(gp, ldg, dtype_code(dy), yp, ldy, _dense(dst_row, T * k, torch.int32), _dense(gate_w, T * k), T, d, k,
-                                        bp, ldb, _dense(coef, 2 * T), pp, ldp, _dense(dgate_w, T * k), op, ldo, _dense(dcoef, 2 * T),
+    _check(lib().scmoe_combine_backward(gp, ldg, dtype_code(dy), yp, ldy, _table(dst_row, T, k, torch.int32), _table(gate_w, T, k), T, d, k,
+                                        bp, ldb, _table(coef, T, 2), pp, ldp, _table(dgate_w, T, k), op, ldo, _table(dcoef, T, 2),
                                         _stream(stream)), "scmoe_combine_backward")
