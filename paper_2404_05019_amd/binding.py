@@ -343,68 +343,76 @@ def moe_top2_layer_forward(desc, x, weights, y, workspace, routing=None, stream=
 
 
 def _refuse(t, want):
-    raise TypeError("expected %s on the GPU, got %s of %s on %s" % (want, tuple(t.shape), t.dtype, t.device))
+    raise TypeError("expected %s on the GPU of the call, got %s of %s on %s" % (want, tuple(t.shape), t.dtype, t.device))
 
 
-def _rows(t, shape, dtype):
+def _device(t, stream):
+    """The GPU of the call, that of its stream, where t and every other tensor has to be."""
+    device = t.get_device()
+    if device < 0 or device != (_current_device() if stream is None else getattr(stream, "device_index", device)):
+        _refuse(t, "tensors")
+    return device
+
+
+def _rows(t, shape, dtype, device):
     """Address and row stride of activations of that shape and type (None: not given)."""
     if t is None:
         return None, 0
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
         _refuse(t, "%s of %s" % (tuple(shape), dtype))
     ld, one = t.stride()
     assert one == 1, "rows must be contiguous"
     return t.data_ptr(), ld
 
 
-def _packed(t, d, dtype):
+def _packed(t, d, dtype, device):
     """Address and row stride of packed rows of that width and type."""
     if t is None:
         return None, 0
-    if t.dtype is not dtype or t.dim() != 2 or t.shape[1] != d or not t.is_cuda:
+    if t.dtype is not dtype or t.dim() != 2 or t.shape[1] != d or t.get_device() != device:
         _refuse(t, "rows of %d %s" % (d, dtype))
     return t.data_ptr(), _ld(t)
 
 
-def _dense(t, n, dtype=torch.float32):
+def _dense(t, n, device, dtype=torch.float32):
     """Address of n elements of that type without gaps (None: not given)."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
         _refuse(t, "%d contiguous %s" % (n, dtype))
     return t.data_ptr()
 
 
-def _table(t, rows, cols, dtype=torch.float32):
+def _table(t, rows, cols, device, dtype=torch.float32):
     """Address of [rows, cols] of that type without gaps (None: not given).  The rows may have several dimensions, and a flat tensor is
     taken as it is; a transposed table has as many elements and is refused."""
     if t is None:
         return None
     if t.shape[-1:] != (cols,) and cols != 1 and t.dim() != 1:
         _refuse(t, "[%d, %d] of %s" % (rows, cols, dtype))
-    return _dense(t, rows * cols, dtype)
+    return _dense(t, rows * cols, device, dtype)
 
 
-def _mask(mask, T):
+def _mask(mask, T, device):
     """Address of one byte per token: torch.bool or torch.uint8."""
-    return None if mask is None else _dense(mask, T, torch.bool if mask.dtype is torch.bool else torch.uint8)
+    return None if mask is None else _dense(mask, T, device, torch.bool if mask.dtype is torch.bool else torch.uint8)
 
 
-def _scratch(workspace):
+def _scratch(workspace, device):
     """Address and bytes of a workspace (None: none)."""
     if workspace is None:
         return None, 0
     n = workspace.numel()
-    return _dense(workspace, n, workspace.dtype), n * workspace.element_size()
+    return _dense(workspace, n, device, workspace.dtype), n * workspace.element_size()
 
 
 def scmoe_layer_norm(x, gamma, beta, eps, y, residual=None, sum_out=None, mean=None, rstd=None, stream=None):
     """y = norm(x + residual) * gamma + beta; sum_out takes x + residual, mean and rstd what the backward pass needs."""
     T, d = shape = x.shape
-    dtype = x.dtype
-    (xp, ldx), (rp, ldr), (sp, lds), (yp, ldy) = _rows(x, shape, dtype), _rows(residual, shape, dtype), _rows(sum_out, shape, dtype), _rows(y, shape, dtype)
-    _check(lib().scmoe_layer_norm(xp, ldx, dtype_code(x), rp, ldr, _dense(gamma, d), _dense(beta, d), eps, T, d, sp, lds, yp, ldy,
-                                  _dense(mean, T), _dense(rstd, T), _stream(stream)), "scmoe_layer_norm")
+    dtype, dev = x.dtype, _device(x, stream)
+    (xp, ldx), (rp, ldr), (sp, lds), (yp, ldy) = _rows(x, shape, dtype, dev), _rows(residual, shape, dtype, dev), _rows(sum_out, shape, dtype, dev), _rows(y, shape, dtype, dev)
+    _check(lib().scmoe_layer_norm(xp, ldx, dtype_code(x), rp, ldr, _dense(gamma, d, dev), _dense(beta, d, dev), eps, T, d, sp, lds, yp, ldy,
+                                  _dense(mean, T, dev), _dense(rstd, T, dev), _stream(stream)), "scmoe_layer_norm")
 
 
 def scmoe_layer_norm_backward_workspace_bytes(T, d):
@@ -416,11 +424,11 @@ def scmoe_layer_norm_backward_workspace_bytes(T, d):
 def scmoe_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, workspace=None, dsum=None, stream=None):
     """dx, dgamma and dbeta of scmoe_layer_norm; x is what was normed, dsum the gradient that reaches it beside the norm."""
     T, d = shape = x.shape
-    dtype = x.dtype
-    (gp, ldg), (xp, ldx), (sp, lds), (dp, ldd) = _rows(dy, shape, dtype), _rows(x, shape, dtype), _rows(dsum, shape, dtype), _rows(dx, shape, dtype)
-    wp, nb = _scratch(workspace)
-    _check(lib().scmoe_layer_norm_backward(gp, ldg, xp, ldx, dtype_code(x), _dense(gamma, d), _dense(mean, T), _dense(rstd, T), sp, lds, T, d,
-                                           dp, ldd, _dense(dgamma, d), _dense(dbeta, d), wp, nb, _stream(stream)),
+    dtype, dev = x.dtype, _device(x, stream)
+    (gp, ldg), (xp, ldx), (sp, lds), (dp, ldd) = _rows(dy, shape, dtype, dev), _rows(x, shape, dtype, dev), _rows(dsum, shape, dtype, dev), _rows(dx, shape, dtype, dev)
+    wp, nb = _scratch(workspace, dev)
+    _check(lib().scmoe_layer_norm_backward(gp, ldg, xp, ldx, dtype_code(x), _dense(gamma, d, dev), _dense(mean, T, dev), _dense(rstd, T, dev), sp, lds, T, d,
+                                           dp, ldd, _dense(dgamma, d, dev), _dense(dbeta, d, dev), wp, nb, _stream(stream)),
            "scmoe_layer_norm_backward")
 
 
@@ -433,9 +441,10 @@ def scmoe_balance_loss_workspace_bytes(T, E):
 def scmoe_balance_loss(probs, expert_idx, k, coef, load, mean_prob, slope, loss, workspace, mask=None, stream=None):
     """Loss, items per expert and the loss's slope in every counted token's probabilities."""
     T, E = probs.shape
-    wp, nb = _scratch(workspace)
-    _check(lib().scmoe_balance_loss(_table(probs, T, E), _table(expert_idx, T, k, torch.int32), _mask(mask, T), T, E, k, coef,
-                                    _dense(load, E, torch.int32), _dense(mean_prob, E), _dense(slope, E), _dense(loss, 1), wp, nb,
+    dev = _device(probs, stream)
+    wp, nb = _scratch(workspace, dev)
+    _check(lib().scmoe_balance_loss(_table(probs, T, E, dev), _table(expert_idx, T, k, dev, torch.int32), _mask(mask, T, dev), T, E, k, coef,
+                                    _dense(load, E, dev, torch.int32), _dense(mean_prob, E, dev), _dense(slope, E, dev), _dense(loss, 1, dev), wp, nb,
                                     _stream(stream)), "scmoe_balance_loss")
 
 
@@ -451,26 +460,26 @@ def scmoe_gate_backward(x, W_g, probs, expert_idx, gate_w, dgate_w, dx, dW_g, db
     the packed rows."""
     T, d = shape = x.shape
     E = W_g.shape[1]
-    dtype = x.dtype
+    dtype, dev = x.dtype, _device(x, stream)
     if dx_perm is not None and dx_perm.shape[0] == 0:      # (nothing was kept: an empty tensor has no address)
         dx_perm = dst_row = None
-    (xp, ldx), (dp, ldd), (pp, ldp) = _rows(x, shape, dtype), _rows(dx, shape, dtype), _packed(dx_perm, d, dtype)
-    wp, nb = _scratch(workspace)
-    _check(lib().scmoe_gate_backward(xp, ldx, dtype_code(x), _table(W_g, d, E), _table(probs, T, E), _table(expert_idx, T, k, torch.int32),
-                                     _table(gate_w, T, k), _table(dgate_w, T, k), _dense(slope, E), _dense(dloss, 1), _mask(mask, T),
-                                     T, d, E, k, normalize, pp, ldp, _table(dst_row, T, k, torch.int32), dp, ldd, _table(dW_g, d, E),
-                                     _dense(dbias, E), wp, nb, _stream(stream)), "scmoe_gate_backward")
+    (xp, ldx), (dp, ldd), (pp, ldp) = _rows(x, shape, dtype, dev), _rows(dx, shape, dtype, dev), _packed(dx_perm, d, dtype, dev)
+    wp, nb = _scratch(workspace, dev)
+    _check(lib().scmoe_gate_backward(xp, ldx, dtype_code(x), _table(W_g, d, E, dev), _table(probs, T, E, dev), _table(expert_idx, T, k, dev, torch.int32),
+                                     _table(gate_w, T, k, dev), _table(dgate_w, T, k, dev), _dense(slope, E, dev), _dense(dloss, 1, dev), _mask(mask, T, dev),
+                                     T, d, E, k, normalize, pp, ldp, _table(dst_row, T, k, dev, torch.int32), dp, ldd, _table(dW_g, d, E, dev),
+                                     _dense(dbias, E, dev), wp, nb, _stream(stream)), "scmoe_gate_backward")
 
 
 def scmoe_combine_backward(dy, y_perm, dst_row, gate_w, k, dy_perm=None, dgate_w=None, base=None, coef=None, dbase=None, dcoef=None,
                            stream=None):
     """What reaches the packed rows, the gate weights, the shared expert's rows and the coefficients (each may be None)."""
     T, d = shape = dy.shape
-    dtype = dy.dtype
+    dtype, dev = dy.dtype, _device(dy, stream)
     if y_perm is not None and y_perm.shape[0] == 0:        # (nothing was kept: an empty tensor has no address, and no row is read)
         y_perm = dy
-    (gp, ldg), (yp, ldy), (bp, ldb) = _rows(dy, shape, dtype), _packed(y_perm, d, dtype), _rows(base, shape, dtype)
-    (pp, ldp), (op, ldo) = _packed(dy_perm, d, dtype), _rows(dbase, shape, dtype)
-    _check(lib().scmoe_combine_backward(gp, ldg, dtype_code(dy), yp, ldy, _table(dst_row, T, k, torch.int32), _table(gate_w, T, k), T, d, k,
-                                        bp, ldb, _table(coef, T, 2), pp, ldp, _table(dgate_w, T, k), op, ldo, _table(dcoef, T, 2),
+    (gp, ldg), (yp, ldy), (bp, ldb) = _rows(dy, shape, dtype, dev), _packed(y_perm, d, dtype, dev), _rows(base, shape, dtype, dev)
+    (pp, ldp), (op, ldo) = _packed(dy_perm, d, dtype, dev), _rows(dbase, shape, dtype, dev)
+    _check(lib().scmoe_combine_backward(gp, ldg, dtype_code(dy), yp, ldy, _table(dst_row, T, k, dev, torch.int32), _table(gate_w, T, k, dev), T, d, k,
+                                        bp, ldb, _table(coef, T, 2, dev), pp, ldp, _table(dgate_w, T, k, dev), op, ldo, _table(dcoef, T, 2, dev),
                                         _stream(stream)), "scmoe_combine_backward")

@@ -113,3 +113,26 @@ def test_a_transposed_table_is_refused(library, name, n):
 def test_tensors_that_fit_are_taken(library, name):
     call(name)
     assert library.called == [name]
+
+
+@pytest.mark.parametrize("name,n", [(name, n) for name in CALLS for n in CALLS[name]])
+def test_a_tensor_on_another_gpu_is_refused(library, name, n):
+    """The kernel runs on one GPU, and on another one's memory at best by its grace."""
+    other = OnGpu(torch.zeros(SHAPES[n], dtype=torch.int32 if n in INTS else torch.uint8 if n == "mask" else torch.float32), 1)
+    with pytest.raises(TypeError, match="on the GPU"):
+        call(name, **{n: other})
+    assert library.called == []
+
+
+def test_the_gpu_of_a_call_is_its_stream_s(library, monkeypatch):
+    """The current one, or the one of the stream that is given."""
+    class Stream:
+        cuda_stream, device_index = 5, 1
+    x0, x1 = (OnGpu(torch.zeros(T, D), i) for i in (0, 1))
+    monkeypatch.setattr(B, "_current_stream", lambda device: 0)
+    B.scmoe_layer_norm(x0, None, None, 1e-5, x0)
+    B.scmoe_layer_norm(x1, None, None, 1e-5, x1, stream=Stream)
+    for x, stream in ((x1, None), (x0, Stream)):
+        with pytest.raises(TypeError, match="on the GPU"):
+            B.scmoe_layer_norm(x, None, None, 1e-5, x, stream=stream)
+    assert len(library.called) == 2
