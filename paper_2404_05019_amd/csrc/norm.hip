@@ -348,22 +348,26 @@ static int norm_grad_rows(int d, int dtype) {
   return lanes < 64 ? 8 * (64 / lanes) : d <= 1024 ? 8 : d <= 2048 ? 4 : d <= 4096 ? 2 : 1;
 }
 
-// One workgroup per compute unit, each with a part of 8 d bytes to leave.  Where the parts are few bytes, or would be with up to four
-// turns for each workgroup, the last one adds them up in the same launch: up to 32 parts, which it reads in one go, of 64 KB in all.  A
-// call of 256 rows of 512, bf16, 9.0 us (two launches 11.4), 4096 of 128 9.3 (11.4), 256 of 1024 11.0 (11.7), 64 of 2048 11.3 (11.3); with
-// 128 KB 512 of 1024 14.9 (11.7).  Where the caller waits for each call two launches are up to 4 us faster (512 rows of 512 22.1 / 26.2).
+// One workgroup per compute unit, each with a part of 8 d bytes to leave, which a second launch adds up, but for calls of few rows:
+//  - up to NORM_GRAD_TURNS groups of rows (narrow rows: NORM_GRAD_NARROW_TURNS) are one workgroup's, which writes the sums itself;
+//  - up to MOST_LEFT parts of a narrow row's columns, 64 KB in all, are added up by the last workgroup of the one launch.
+// us a call in a replayed graph / called back to back from Python / waited for one by one, bf16 (fp32 alike), against two launches:
+//   2 turns of one workgroup     64 columns 4.8 / 9.1 / 20.4 (6.3 / 12.0 / 22.6), 2048 6.0 / 9.1 / 21.6 (7.0 / 12.2 / 22.9)
+//   4 turns                      512 columns 6.1 / 9.1 / 21.9 (6.0 / 12.1 / 22.7), 1024 8.6 / 9.0 / 24.3 (7.2 / 12.2 / 23.0)
+//   the last workgroup adds up   32 parts of 64 columns 7.9 / 8.2 / 23.3 (6.4 / 10.8 / 22.1), 16 of 512 7.9 / 8.1 / 23.2 (6.1 / 10.7 / 22.0),
+//                                8 of 1024 9.9 / 9.5 / 25.1 (7.3 / 10.7 / 22.8), 4 of 2048 10.8 / 10.3 / 25.9 (7.0 / 10.8 / 22.5)
+// The arrival costs the device up to 1.8 us and saves the host 2.6 for narrow rows; wider ones cost it more than the host saves.
+constexpr int NORM_GRAD_TURNS = 2, NORM_GRAD_NARROW_TURNS = 4, NORM_GRAD_NARROW = 512;
 constexpr int64_t NORM_GRAD_ONE_LAUNCH = 64 << 10;
-constexpr int64_t NORM_GRAD_FEW_PARTS = MOST_LEFT;
 
 static int norm_grad_groups(int T, int d, int dtype, bool sums, bool* one_launch) {
   const int rows = norm_grad_rows(d, dtype);
   const int64_t most = (static_cast<int64_t>(T) + rows - 1) / rows, groups = most < num_cus() ? most : num_cus();
   *one_launch = false;
   if (!sums) return static_cast<int>(groups);          // (dx alone: 256 rows of 1024 in bf16 3.9 us, on 8 workgroups 7.3)
-  int64_t fit = NORM_GRAD_ONE_LAUNCH / (8 * d);
-  fit = fit < 1 ? 1 : fit < NORM_GRAD_FEW_PARTS ? fit : NORM_GRAD_FEW_PARTS;
-  *one_launch = most <= 4 * fit;
-  return static_cast<int>(*one_launch && groups > fit ? fit : groups);
+  const bool narrow = d <= NORM_GRAD_NARROW, single = most <= (narrow ? NORM_GRAD_NARROW_TURNS : NORM_GRAD_TURNS);
+  *one_launch = single || (narrow && most <= MOST_LEFT && most * 8 * d <= NORM_GRAD_ONE_LAUNCH);
+  return single && groups > 1 ? 1 : static_cast<int>(groups);
 }
 
 static size_t norm_grad_bytes(int T, int d) {          // (fp32 has as many workgroups or more)
