@@ -548,12 +548,17 @@ static size_t gate_grad_bytes(int T, int d, int E) {        // (for either type)
   return s == 1 ? 0 : static_cast<size_t>(s) * (gate_grad_stride(d, E) * 4 + 8 * blocks);   // parts and marks
 }
 
-// A column block's last workgroup adds up its parts in the same launch where they are few and small: as many as it reads in one go.
-// 512 tokens of 1024, bf16, a call (one launch / two): 8 experts 10.8 / 13.9 us, 16 11.9 / 13.9; 1024 tokens (16 parts), 8 experts
-// 13.1 / 13.8, and 30.9 / 27.4 where the caller waits for each; 256 tokens, 32 experts (16 KB) 15.8 / 13.6.
+// A column block's last workgroup adds up its parts in the same launch where they are at most eight, of 8 KB in all.  us a call in a
+// replayed graph / called back to back from Python / waited for one by one, against two launches:
+//   bf16, 4 experts (2 KB a part), 4 parts 10.1 / 9.7 / 26.0 (8.5 / 11.3 / 24.7), 8 parts 10.6 / 10.3 / 26.4 (8.6 / 11.3 / 24.7)
+//         8 (4 KB), 2 parts 10.3 / 10.0 / 26.2 (8.7 / 11.2 / 24.7), 4 parts 10.7 / 10.4 / 26.6 (8.7 / 11.2 / 24.8)
+//         16 (8 KB), 2 parts 11.5 / 11.2 / 27.4 (8.7 / 11.2 / 24.8)
+//   fp32, 4 experts (1 KB), 8 parts 9.2 / 8.9 / 25.1 (7.3 / 11.3 / 23.5); 16 (4 KB), 2 parts 9.2 / 8.9 / 25.1 (7.5 / 11.2 / 23.5),
+//         4 parts 9.7 / 9.3 / 25.7 (7.5 / 11.2 / 23.6); 32 (8 KB), 2 parts 13.3 / 12.9 / 29.1 (10.4 / 11.2 / 26.4)
+// Up to there the host saves about as much as the arrival costs the device; beyond, the device loses more.
 constexpr int GATE_GRAD_FEW_PARTS = 8;
 static_assert(GATE_GRAD_FEW_PARTS <= MOST_LEFT);
-constexpr int64_t GATE_GRAD_SMALL_PART = 8 << 10;
+constexpr int64_t GATE_GRAD_ONE_LAUNCH = 8 << 10;
 
 static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
   const int cols = gate_grad_cols(a.E, dtype);
@@ -635,7 +640,7 @@ extern "C" int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, co
   a.Wg16 = E % 4 == 0 && aligned16(W_g);
   a.parts = static_cast<float*>(workspace); a.stride = gate_grad_stride(d, E);
   a.dWg = dW_g; a.dbias = dbias;
-  if (a.splits > 1 && a.splits <= GATE_GRAD_FEW_PARTS && gate_grad_cols(E, dtype) * E * 4 <= GATE_GRAD_SMALL_PART) {
+  if (a.splits > 1 && a.splits <= GATE_GRAD_FEW_PARTS && static_cast<int64_t>(a.splits) * gate_grad_cols(E, dtype) * E * 4 <= GATE_GRAD_ONE_LAUNCH) {
     a.marks = reinterpret_cast<unsigned long long*>(a.parts + a.splits * a.stride);
     a.call = next_call();
   }

@@ -31,3 +31,13 @@ def test_norm_gradient_of_few_rows(record):  # noqa: F811
         (4, 4096): [1], (5, 4096): [3, 512], (2, 16384): [1], (3, 16384): [3, 2048],
     }
     assert dict(zip(want, launches(record, *[("norm_grad", dict(T=T, d=d)) for T, d in want]))) == want
+
+
+def test_gate_gradient_of_few_tokens(record):  # noqa: F811
+    """Both sides of the rule: parts that a column block's last workgroup adds up, and a second launch for them (64 tokens a part)."""
+    bf16 = dict(dtype=BF16)
+    want = [(dict(T=64, E=16), 1), (dict(T=512, E=4), 1), (dict(T=513, E=4), 2), (dict(T=256, E=8), 1), (dict(T=257, E=8), 2), (dict(T=128, E=16), 1),
+            (dict(T=129, E=16), 2), (dict(T=65, E=32), 2), (dict(T=256, E=4, **bf16), 1), (dict(T=257, E=4, **bf16), 2), (dict(T=128, E=8, **bf16), 1),
+            (dict(T=129, E=8, **bf16), 2), (dict(T=65, E=16, **bf16), 2), (dict(T=64, E=64, **bf16), 1)]
+    got = launches(record, *[("gate_grad", dict(kw, d=256)) for kw, _ in want])
+    assert [len(lines) for lines in got] == [n for _, n in want]
