@@ -220,7 +220,8 @@ template <bool BF16, int EC, int K, bool DISPATCH, bool ST>
 __global__ __launch_bounds__(256, 2) void gate_backward_kernel(GateGradArgs a) {
   using C = GateGradCfg<BF16, EC>;
   constexpr int EP = C::EP, S = C::S, LD = C::LD, NV = C::NV, COLS = C::COLS, KB = C::KB, KS = C::KS;
-  constexpr bool SECOND = DISPATCH && K > 1;
+  constexpr bool SECOND = DISPATCH && K > 1 && (BF16 || EC < 4);   // (rows of the second choice early: fp32 beyond 32 experts has no registers left)
+  constexpr int ITEMS = BF16 || EC < 4 || K < 4 ? K : 1;           // items of a token looked at together (as SECOND: registers)
   __shared__ __attribute__((aligned(16))) unsigned char lds[C::LDS];
   __shared__ float dbs[4][EP];
   __shared__ int last_one;
@@ -337,7 +338,7 @@ __global__ __launch_bounds__(256, 2) void gate_backward_kernel(GateGradArgs a) {
       float g[S], own[S];
 #pragma unroll
       for (int s = 0; s < S; ++s) own[s] = 0.0f;
-#pragma unroll
+#pragma unroll ITEMS
       for (int j = 0; j < K; ++j) {
         const int e = __shfl(n.idx, m * K + j, 64);
         const float v = __shfl(n.add, m * K + j, 64);
