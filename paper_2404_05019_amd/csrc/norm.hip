@@ -139,17 +139,30 @@ struct NormGradRow {
   float mean, rstd;
 };
 
-template <int P, int STEP, bool ST>
+template <int P, int STEP, bool ST, bool DSUM>
 __device__ __forceinline__ void norm_grad_load(const NormGradArgs& a, int64_t row, int lane, int pieces, NormGradRow<P>& r) {
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     const int64_t c = static_cast<int64_t>(min(lane + p * STEP, pieces - 1)) * 16;
     r.x[p] = load16<ST>(a.x + row * a.ldx + c);
     r.y[p] = load16<ST>(a.dy + row * a.lddy + c);
-    if (a.dsum != nullptr) r.s[p] = load16<ST>(a.dsum + row * a.lddsum + c);
+    if (DSUM && a.dsum != nullptr) r.s[p] = load16<ST>(a.dsum + row * a.lddsum + c);
   }
   r.mean = a.mean[row];
   r.rstd = a.rstd[row];
+}
+
+// gamma of the columns of piece c.
+template <int NV>
+__device__ __forceinline__ void norm_grad_gamma(const NormGradArgs& a, int c, float* g) {
+#pragma unroll
+  for (int i = 0; i < NV; i += 4) {
+    const float4 t = a.gamma == nullptr ? make_float4(1.0f, 1.0f, 1.0f, 1.0f) : *reinterpret_cast<const float4*>(a.gamma + c * NV + i);
+    g[i] = t.x;
+    g[i + 1] = t.y;
+    g[i + 2] = t.z;
+    g[i + 3] = t.w;
+  }
 }
 
 // A workgroup has R rows at a time, W waves each, and takes every gridDim.x-th group of R; a lane's columns are the same in all of
@@ -183,6 +196,9 @@ template <bool BF16, int V, int W, int R, bool ST, int L = 64>
 __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(NormGradArgs a) {
   constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = L * W, H = NV / 4, AREAS = W <= 2 ? 2 : 1, ROWS = R * (64 / L);
   constexpr bool AHEAD = P <= 2;
+  // 32 values of x, of dy and of both sums leave no registers for gamma as well, in fp32 neither for dsum: they are read where they are
+  // used (all kept, 2048 rows of 16384 with dsum took 200 us in place of 136 in fp32 and spilled in bf16 too)
+  constexpr bool WIDE = V > 16, LATE = WIDE && !BF16;
   __shared__ float2 s[2][R][W];
   __shared__ int last_one;
   extern __shared__ __attribute__((aligned(16))) float4 cols[];  // R > 1: AREAS of [dgamma, dbeta][half][piece]
@@ -194,19 +210,11 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
   const int64_t step = static_cast<int64_t>(gridDim.x) * ROWS, last = a.T - 1;
   int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + mine;
   NormGradRow<P> n;
-  if (AHEAD) norm_grad_load<P, STEP, ST>(a, row < a.T ? row : last, lane, pieces, n);
-  float g[V], ag[V], ab[V];
+  if (AHEAD) norm_grad_load<P, STEP, ST, !LATE>(a, row < a.T ? row : last, lane, pieces, n);
+  float g[WIDE ? NV : V], ag[V], ab[V];
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const int c = min(lane + p * STEP, pieces - 1);
-#pragma unroll
-    for (int i = 0; i < NV; i += 4) {
-      const float4 t = a.gamma == nullptr ? make_float4(1.0f, 1.0f, 1.0f, 1.0f) : *reinterpret_cast<const float4*>(a.gamma + c * NV + i);
-      g[p * NV + i] = t.x;
-      g[p * NV + i + 1] = t.y;
-      g[p * NV + i + 2] = t.z;
-      g[p * NV + i + 3] = t.w;
-    }
+    if (!WIDE) norm_grad_gamma<NV>(a, min(lane + p * STEP, pieces - 1), g + p * NV);
 #pragma unroll
     for (int i = 0; i < NV; ++i) ag[p * NV + i] = ab[p * NV + i] = 0.0f;
   }
@@ -216,9 +224,9 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
     NormGradRow<P> q;
     if (AHEAD) {
       q = n;
-      norm_grad_load<P, STEP, ST>(a, row + step < a.T ? row + step : last, lane, pieces, n);
+      norm_grad_load<P, STEP, ST, !LATE>(a, row + step < a.T ? row + step : last, lane, pieces, n);
     } else {
-      norm_grad_load<P, STEP, ST>(a, live ? row : last, lane, pieces, q);
+      norm_grad_load<P, STEP, ST, !LATE>(a, live ? row : last, lane, pieces, q);
     }
     if (!live) q.mean = q.rstd = 0.0f;                  // (a row that is there for the barrier adds zeros, whatever the last row holds)
     float s1 = 0.0f, s2 = 0.0f;
@@ -226,11 +234,17 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
     for (int p = 0; p < P; ++p) {
       const bool in = live && lane + p * STEP < pieces;
       float x[NV], y[NV];
-      unpack16<BF16>(zero_unless(in, q.x[p]), x);
-      unpack16<BF16>(zero_unless(in, q.y[p]), y);
+      const uint4 qx = zero_unless(in, q.x[p]), qy = zero_unless(in, q.y[p]);
+      if (WIDE) {                                       // (one copy of them)
+        q.x[p] = qx;
+        q.y[p] = qy;
+      }
+      unpack16<BF16>(qx, x);
+      unpack16<BF16>(qy, y);
+      if (WIDE) norm_grad_gamma<NV>(a, min(lane + p * STEP, pieces - 1), g);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const float xh = (x[i] - q.mean) * q.rstd, gy = y[i] * g[p * NV + i];
+        const float xh = (x[i] - q.mean) * q.rstd, gy = y[i] * g[WIDE ? i : p * NV + i];
         s1 += gy;
         s2 = fmaf(gy, xh, s2);
         ag[p * NV + i] = fmaf(y[i], xh, ag[p * NV + i]);
@@ -248,6 +262,10 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
       float x[NV], y[NV], r[NV];
       unpack16<BF16>(q.x[p], x);
       unpack16<BF16>(q.y[p], y);
+      if (WIDE) norm_grad_gamma<NV>(a, min(c, pieces - 1), g);
+      if (LATE) {
+        if (a.dsum != nullptr) q.s[p] = load16<ST>(a.dsum + (live ? row : last) * a.lddsum + static_cast<int64_t>(min(c, pieces - 1)) * 16);
+      }
       if (a.dsum != nullptr) {
         unpack16<BF16>(q.s[p], r);
       } else {
@@ -257,7 +275,7 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const float xh = (x[i] - q.mean) * q.rstd;
-        r[i] = fmaf(q.rstd, (y[i] * g[p * NV + i] - s1) - xh * s2, r[i]);
+        r[i] = fmaf(q.rstd, (y[i] * g[WIDE ? i : p * NV + i] - s1) - xh * s2, r[i]);
       }
       if (live && c < pieces) store16<ST>(a.dx + row * a.lddx + static_cast<int64_t>(c) * 16, pack16<BF16>(r));
     }

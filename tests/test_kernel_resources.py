@@ -40,7 +40,8 @@ def scratch(tmp_path_factory):
     return kernels
 
 
-@pytest.mark.parametrize("kernel", ["gate_backward_kernel", "combine_backward_kernel", "balance_loss_kernel", "sum_parts_kernel"])
+@pytest.mark.parametrize("kernel", ["gate_backward_kernel", "combine_backward_kernel", "balance_loss_kernel", "sum_parts_kernel", "layer_norm_kernel",
+                                    "layer_norm_backward_kernel"])
 def test_training_kernels_fit_their_registers(scratch, kernel):
     """A register that goes to memory and back waits for the loads that are kept in flight."""
     of = {k: v for k, v in scratch.items() if kernel in k}
