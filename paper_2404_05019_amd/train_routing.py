@@ -28,6 +28,8 @@ class RoutingBlock:
         g.manual_seed(seed)
         normal = lambda *s, scale=1.0: torch.randn(s, generator=g, device=DEV) * scale  # noqa: E731
         self.T, self.d, self.F, self.E, self.k, self.dtype = T, d, F, E, k, dtype
+        # one expert's weight is its probability: as a softmax over the chosen one alone it would be 1, and the gate would not learn
+        self.normalize = int(k > 1)
         self.capacity = B.scmoe_capacity(T, E, k, capacity_factor)
         self.W1, self.W2 = normal(E, F, d, scale=d ** -0.5).to(dtype), normal(E, d, F, scale=F ** -0.5).to(dtype)
         self.gamma, self.beta = torch.ones(d, device=DEV), torch.zeros(d, device=DEV)
@@ -54,7 +56,7 @@ class RoutingBlock:
     def forward(self, x):
         """The block's output for x [T, d]; what the backward pass needs stays in the buffers."""
         B.scmoe_layer_norm(x, self.gamma, self.beta, EPS, self.h, mean=self.mean, rstd=self.rstd)
-        B.scmoe_gate_topk(self.h, self.W_g, self.bias, self.k, self.idx, self.gate_w, self.probs, normalize=1)
+        B.scmoe_gate_topk(self.h, self.W_g, self.bias, self.k, self.idx, self.gate_w, self.probs, normalize=self.normalize)
         B.scmoe_dispatch(self.h, self.idx, self.E, self.k, self.capacity, self.counts, self.offsets, self.dst_row, self.src_token, self.x_perm,
                          self.scratch)
         B.scmoe_expert_ffn(self.x_perm, self.offsets, self.x_perm.shape[0], self.W1, None, self.W2, None, self.hidden, self.y_perm,
@@ -82,7 +84,7 @@ class RoutingBlock:
         B.scmoe_combine_backward(dy, self.y_perm, self.dst_row, self.gate_w, self.k, dy_perm=self.dy_perm, dgate_w=self.dgate_w)
         self._experts_backward()
         B.scmoe_gate_backward(self.h, self.W_g, self.probs, self.idx, self.gate_w, self.dgate_w, self.dh, self.grads[2], self.grads[3],
-                              self.scratch, k=self.k, normalize=1, slope=self.slope, mask=mask, dx_perm=self.dx_perm, dst_row=self.dst_row)
+                              self.scratch, k=self.k, normalize=self.normalize, slope=self.slope, mask=mask, dx_perm=self.dx_perm, dst_row=self.dst_row)
         B.scmoe_layer_norm_backward(self.dh, x, self.gamma, self.mean, self.rstd, self.dx, self.grads[0], self.grads[1], self.scratch)
         return self.dx
 
