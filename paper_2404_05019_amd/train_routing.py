@@ -55,6 +55,7 @@ class RoutingBlock:
 
     def forward(self, x):
         """The block's output for x [T, d]; what the backward pass needs stays in the buffers."""
+        self.loss_slope = None                                    # (of this pass: there is none until the loss was asked for)
         B.scmoe_layer_norm(x, self.gamma, self.beta, EPS, self.h, mean=self.mean, rstd=self.rstd)
         B.scmoe_gate_topk(self.h, self.W_g, self.bias, self.k, self.idx, self.gate_w, self.probs, normalize=self.normalize)
         B.scmoe_dispatch(self.h, self.idx, self.E, self.k, self.capacity, self.counts, self.offsets, self.dst_row, self.src_token, self.x_perm,
@@ -67,6 +68,7 @@ class RoutingBlock:
     def balance_loss(self, coef, mask=None):
         """The loss, on the device; its slope in the probabilities stays for the backward pass."""
         B.scmoe_balance_loss(self.probs, self.idx, self.k, coef, self.load, self.mean_prob, self.slope, self.balance, self.scratch, mask=mask)
+        self.loss_slope = self.slope
         return self.balance
 
     def _experts_backward(self):
@@ -80,11 +82,12 @@ class RoutingBlock:
                 self.dx_perm[at] = torch.autograd.grad(y, x, self.dy_perm[at].float())[0].to(self.dtype)
 
     def backward(self, x, dy, mask=None):
-        """Gradients of the parameters (in `grads`) and of x from the gradient dy of the output, with the balance loss's."""
+        """Gradients of the parameters (in `grads`) and of x from the gradient dy of the output, with the balance loss's if it was asked for
+        since the forward pass."""
         B.scmoe_combine_backward(dy, self.y_perm, self.dst_row, self.gate_w, self.k, dy_perm=self.dy_perm, dgate_w=self.dgate_w)
         self._experts_backward()
         B.scmoe_gate_backward(self.h, self.W_g, self.probs, self.idx, self.gate_w, self.dgate_w, self.dh, self.grads[2], self.grads[3],
-                              self.scratch, k=self.k, normalize=self.normalize, slope=self.slope, mask=mask, dx_perm=self.dx_perm, dst_row=self.dst_row)
+                              self.scratch, k=self.k, normalize=self.normalize, slope=self.loss_slope, mask=mask, dx_perm=self.dx_perm, dst_row=self.dst_row)
         B.scmoe_layer_norm_backward(self.dh, x, self.gamma, self.mean, self.rstd, self.dx, self.grads[0], self.grads[1], self.scratch)
         return self.dx
 

@@ -53,3 +53,20 @@ def test_gradients_of_the_block(k):
     close(y, wy)
     for got, want in zip(block.grads, grads):
         close(got, want)
+
+
+def test_a_pass_without_the_balance_loss():
+    """Nothing of what the memory held before, nor of an earlier pass's loss, is in the gradients."""
+    held = [torch.full((n,), float("nan"), device=DEV) for n in (4, 64, 256, 1 << 20) for _ in range(8)]
+    torch.cuda.synchronize()
+    del held
+    block = RoutingBlock(256, 64, 128, 4, 2, dtype=torch.float32)
+    x, dy = inputs(block)
+    for _ in range(2):
+        y = block.forward(x)
+        block.backward(x, dy)
+        wy, grads = exact(block, x, dy, 0.0)
+        close(y, wy)
+        for got, want in zip(block.grads, grads):
+            close(got, want)
+        block.balance_loss(1000.0)                # (of this pass; the next one does not ask for it)
