@@ -117,12 +117,14 @@ def _check(status, where):
         raise ScmoeError(status, where)
 
 
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 def dtype_code(t):
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
-        return BF16
-    raise TypeError("unsupported activation dtype %s" % t.dtype)
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise TypeError("unsupported activation dtype %s" % t.dtype)
+    return code
 
 
 def _ptr(t):
@@ -346,12 +348,23 @@ def _refuse(t, want):
     raise TypeError("expected %s on the GPU of the call, got %s of %s on %s" % (want, tuple(t.shape), t.dtype, t.device))
 
 
-def _device(t, stream):
-    """The GPU of the call, that of its stream, where t and every other tensor has to be."""
+def _place(t, stream):
+    """The GPU of the call, that of its stream, where t and every other tensor has to be; the stream's handle."""
     device = t.get_device()
-    if device < 0 or device != (_current_device() if stream is None else getattr(stream, "device_index", device)):
+    if stream is None:
+        if device < 0 or device != _current_device():
+            _refuse(t, "tensors")
+        return device, _current_stream(device)
+    if device < 0 or device != getattr(stream, "device_index", device):
         _refuse(t, "tensors")
-    return device
+    return device, _stream(stream)
+
+
+def _view(t):
+    """Address and row stride of the activations that say what the others have to be."""
+    ld, one = t.stride()
+    assert one == 1, "rows must be contiguous"
+    return t.data_ptr(), ld
 
 
 def _rows(t, shape, dtype, device):
@@ -360,9 +373,7 @@ def _rows(t, shape, dtype, device):
         return None, 0
     if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
         _refuse(t, "%s of %s" % (tuple(shape), dtype))
-    ld, one = t.stride()
-    assert one == 1, "rows must be contiguous"
-    return t.data_ptr(), ld
+    return _view(t)
 
 
 def _packed(t, d, dtype, device):
@@ -383,14 +394,16 @@ def _dense(t, n, device, dtype=torch.float32):
     return t.data_ptr()
 
 
-def _table(t, rows, cols, device, dtype=torch.float32):
-    """Address of [rows, cols] of that type without gaps (None: not given).  The rows may have several dimensions, and a flat tensor is
-    taken as it is; a transposed table has as many elements and is refused."""
+def _table(t, shape, device, dtype=torch.float32):
+    """Address of a table of that shape and type without gaps (None: not given).  A flat one is taken as well, and one whose rows have
+    several dimensions; a transposed one, which has as many elements, is refused."""
     if t is None:
         return None
-    if t.shape[-1:] != (cols,) and cols != 1 and t.dim() != 1:
-        _refuse(t, "[%d, %d] of %s" % (rows, cols, dtype))
-    return _dense(t, rows * cols, device, dtype)
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        if t.dim() != 1 and shape[1] != 1 and t.shape[-1:] != shape[1:]:
+            _refuse(t, "%s of %s" % (shape, dtype))
+        return _dense(t, shape[0] * shape[1], device, dtype)
+    return t.data_ptr()
 
 
 def _mask(mask, T, device):
@@ -409,10 +422,10 @@ def _scratch(workspace, device):
 def scmoe_layer_norm(x, gamma, beta, eps, y, residual=None, sum_out=None, mean=None, rstd=None, stream=None):
     """y = norm(x + residual) * gamma + beta; sum_out takes x + residual, mean and rstd what the backward pass needs."""
     T, d = shape = x.shape
-    dtype, dev = x.dtype, _device(x, stream)
-    (xp, ldx), (rp, ldr), (sp, lds), (yp, ldy) = _rows(x, shape, dtype, dev), _rows(residual, shape, dtype, dev), _rows(sum_out, shape, dtype, dev), _rows(y, shape, dtype, dev)
+    dtype, (dev, hs) = x.dtype, _place(x, stream)
+    (xp, ldx), (rp, ldr), (sp, lds), (yp, ldy) = _view(x), _rows(residual, shape, dtype, dev), _rows(sum_out, shape, dtype, dev), _rows(y, shape, dtype, dev)
     _check(lib().scmoe_layer_norm(xp, ldx, dtype_code(x), rp, ldr, _dense(gamma, d, dev), _dense(beta, d, dev), eps, T, d, sp, lds, yp, ldy,
-                                  _dense(mean, T, dev), _dense(rstd, T, dev), _stream(stream)), "scmoe_layer_norm")
+                                  _dense(mean, T, dev), _dense(rstd, T, dev), hs), "scmoe_layer_norm")
 
 
 def scmoe_layer_norm_backward_workspace_bytes(T, d):
@@ -424,11 +437,11 @@ def scmoe_layer_norm_backward_workspace_bytes(T, d):
 def scmoe_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, workspace=None, dsum=None, stream=None):
     """dx, dgamma and dbeta of scmoe_layer_norm; x is what was normed, dsum the gradient that reaches it beside the norm."""
     T, d = shape = x.shape
-    dtype, dev = x.dtype, _device(x, stream)
-    (gp, ldg), (xp, ldx), (sp, lds), (dp, ldd) = _rows(dy, shape, dtype, dev), _rows(x, shape, dtype, dev), _rows(dsum, shape, dtype, dev), _rows(dx, shape, dtype, dev)
+    dtype, (dev, hs) = x.dtype, _place(x, stream)
+    (gp, ldg), (xp, ldx), (sp, lds), (dp, ldd) = _rows(dy, shape, dtype, dev), _view(x), _rows(dsum, shape, dtype, dev), _rows(dx, shape, dtype, dev)
     wp, nb = _scratch(workspace, dev)
     _check(lib().scmoe_layer_norm_backward(gp, ldg, xp, ldx, dtype_code(x), _dense(gamma, d, dev), _dense(mean, T, dev), _dense(rstd, T, dev), sp, lds, T, d,
-                                           dp, ldd, _dense(dgamma, d, dev), _dense(dbeta, d, dev), wp, nb, _stream(stream)),
+                                           dp, ldd, _dense(dgamma, d, dev), _dense(dbeta, d, dev), wp, nb, hs),
            "scmoe_layer_norm_backward")
 
 
@@ -441,11 +454,11 @@ def scmoe_balance_loss_workspace_bytes(T, E):
 def scmoe_balance_loss(probs, expert_idx, k, coef, load, mean_prob, slope, loss, workspace, mask=None, stream=None):
     """Loss, items per expert and the loss's slope in every counted token's probabilities."""
     T, E = probs.shape
-    dev = _device(probs, stream)
+    dev, hs = _place(probs, stream)
     wp, nb = _scratch(workspace, dev)
-    _check(lib().scmoe_balance_loss(_table(probs, T, E, dev), _table(expert_idx, T, k, dev, torch.int32), _mask(mask, T, dev), T, E, k, coef,
+    _check(lib().scmoe_balance_loss(_table(probs, (T, E), dev), _table(expert_idx, (T, k), dev, torch.int32), _mask(mask, T, dev), T, E, k, coef,
                                     _dense(load, E, dev, torch.int32), _dense(mean_prob, E, dev), _dense(slope, E, dev), _dense(loss, 1, dev), wp, nb,
-                                    _stream(stream)), "scmoe_balance_loss")
+                                    hs), "scmoe_balance_loss")
 
 
 def scmoe_gate_backward_workspace_bytes(T, d, E):
@@ -460,26 +473,28 @@ def scmoe_gate_backward(x, W_g, probs, expert_idx, gate_w, dgate_w, dx, dW_g, db
     the packed rows."""
     T, d = shape = x.shape
     E = W_g.shape[1]
-    dtype, dev = x.dtype, _device(x, stream)
+    dtype, (dev, hs) = x.dtype, _place(x, stream)
     if dx_perm is not None and dx_perm.shape[0] == 0:      # (nothing was kept: an empty tensor has no address)
         dx_perm = dst_row = None
-    (xp, ldx), (dp, ldd), (pp, ldp) = _rows(x, shape, dtype, dev), _rows(dx, shape, dtype, dev), _packed(dx_perm, d, dtype, dev)
+    (xp, ldx), (dp, ldd), (pp, ldp) = _view(x), _rows(dx, shape, dtype, dev), _packed(dx_perm, d, dtype, dev)
+    items, gate = (T, k), (d, E)
     wp, nb = _scratch(workspace, dev)
-    _check(lib().scmoe_gate_backward(xp, ldx, dtype_code(x), _table(W_g, d, E, dev), _table(probs, T, E, dev), _table(expert_idx, T, k, dev, torch.int32),
-                                     _table(gate_w, T, k, dev), _table(dgate_w, T, k, dev), _dense(slope, E, dev), _dense(dloss, 1, dev), _mask(mask, T, dev),
-                                     T, d, E, k, normalize, pp, ldp, _table(dst_row, T, k, dev, torch.int32), dp, ldd, _table(dW_g, d, E, dev),
-                                     _dense(dbias, E, dev), wp, nb, _stream(stream)), "scmoe_gate_backward")
+    _check(lib().scmoe_gate_backward(xp, ldx, dtype_code(x), _table(W_g, gate, dev), _table(probs, (T, E), dev), _table(expert_idx, items, dev, torch.int32),
+                                     _table(gate_w, items, dev), _table(dgate_w, items, dev), _dense(slope, E, dev), _dense(dloss, 1, dev), _mask(mask, T, dev),
+                                     T, d, E, k, normalize, pp, ldp, _table(dst_row, items, dev, torch.int32), dp, ldd, _table(dW_g, gate, dev),
+                                     _dense(dbias, E, dev), wp, nb, hs), "scmoe_gate_backward")
 
 
 def scmoe_combine_backward(dy, y_perm, dst_row, gate_w, k, dy_perm=None, dgate_w=None, base=None, coef=None, dbase=None, dcoef=None,
                            stream=None):
     """What reaches the packed rows, the gate weights, the shared expert's rows and the coefficients (each may be None)."""
     T, d = shape = dy.shape
-    dtype, dev = dy.dtype, _device(dy, stream)
+    dtype, (dev, hs) = dy.dtype, _place(dy, stream)
     if y_perm is not None and y_perm.shape[0] == 0:        # (nothing was kept: an empty tensor has no address, and no row is read)
         y_perm = dy
-    (gp, ldg), (yp, ldy), (bp, ldb) = _rows(dy, shape, dtype, dev), _packed(y_perm, d, dtype, dev), _rows(base, shape, dtype, dev)
+    (gp, ldg), (yp, ldy), (bp, ldb) = _view(dy), _packed(y_perm, d, dtype, dev), _rows(base, shape, dtype, dev)
+    items, pairs = (T, k), (T, 2)
     (pp, ldp), (op, ldo) = _packed(dy_perm, d, dtype, dev), _rows(dbase, shape, dtype, dev)
-    _check(lib().scmoe_combine_backward(gp, ldg, dtype_code(dy), yp, ldy, _table(dst_row, T, k, dev, torch.int32), _table(gate_w, T, k, dev), T, d, k,
-                                        bp, ldb, _table(coef, T, 2, dev), pp, ldp, _table(dgate_w, T, k, dev), op, ldo, _table(dcoef, T, 2, dev),
-                                        _stream(stream)), "scmoe_combine_backward")
+    _check(lib().scmoe_combine_backward(gp, ldg, dtype_code(dy), yp, ldy, _table(dst_row, items, dev, torch.int32), _table(gate_w, items, dev), T, d, k,
+                                        bp, ldb, _table(coef, pairs, dev), pp, ldp, _table(dgate_w, items, dev), op, ldo, _table(dcoef, pairs, dev),
+                                        hs), "scmoe_combine_backward")
