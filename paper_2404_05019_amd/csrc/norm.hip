@@ -367,15 +367,16 @@ static int norm_grad_rows(int d, int dtype) {
 }
 
 // One workgroup per compute unit, each with a part of 8 d bytes to leave, which a second launch adds up, but for calls of few rows:
-//  - up to NORM_GRAD_TURNS groups of rows (narrow rows: NORM_GRAD_NARROW_TURNS) are one workgroup's, which writes the sums itself;
+//  - up to four groups of narrow rows, two of rows up to 8192 wide and one of wider ones are one workgroup's, which writes the sums itself;
 //  - up to MOST_LEFT parts of a narrow row's columns, 64 KB in all, are added up by the last workgroup of the one launch.
 // us a call in a replayed graph / called back to back from Python / waited for one by one, bf16 (fp32 alike), against two launches:
 //   2 turns of one workgroup     64 columns 4.8 / 9.1 / 20.4 (6.3 / 12.0 / 22.6), 2048 6.0 / 9.1 / 21.6 (7.0 / 12.2 / 22.9)
+//                                fp32: 8192 columns 6.4 / 8.4 / 21.4 (7.0 / 11.4 / 22.2), 16384 12.5 / 12.2 / 27.8 (10.8 / 11.3 / 26.0)
 //   4 turns                      512 columns 6.1 / 9.1 / 21.9 (6.0 / 12.1 / 22.7), 1024 8.6 / 9.0 / 24.3 (7.2 / 12.2 / 23.0)
 //   the last workgroup adds up   32 parts of 64 columns 7.9 / 8.2 / 23.3 (6.4 / 10.8 / 22.1), 16 of 512 7.9 / 8.1 / 23.2 (6.1 / 10.7 / 22.0),
 //                                8 of 1024 9.9 / 9.5 / 25.1 (7.3 / 10.7 / 22.8), 4 of 2048 10.8 / 10.3 / 25.9 (7.0 / 10.8 / 22.5)
 // The arrival costs the device up to 1.8 us and saves the host 2.6 for narrow rows; wider ones cost it more than the host saves.
-constexpr int NORM_GRAD_TURNS = 2, NORM_GRAD_NARROW_TURNS = 4, NORM_GRAD_NARROW = 512;
+constexpr int NORM_GRAD_NARROW = 512;
 constexpr int64_t NORM_GRAD_ONE_LAUNCH = 64 << 10;
 
 static int norm_grad_groups(int T, int d, int dtype, bool sums, bool* one_launch) {
@@ -383,7 +384,7 @@ static int norm_grad_groups(int T, int d, int dtype, bool sums, bool* one_launch
   const int64_t most = (static_cast<int64_t>(T) + rows - 1) / rows, groups = most < num_cus() ? most : num_cus();
   *one_launch = false;
   if (!sums) return static_cast<int>(groups);          // (dx alone: 256 rows of 1024 in bf16 3.9 us, on 8 workgroups 7.3)
-  const bool narrow = d <= NORM_GRAD_NARROW, single = most <= (narrow ? NORM_GRAD_NARROW_TURNS : NORM_GRAD_TURNS);
+  const bool narrow = d <= NORM_GRAD_NARROW, single = most <= (narrow ? 4 : d <= 8192 ? 2 : 1);
   *one_launch = single || (narrow && most <= MOST_LEFT && most * 8 * d <= NORM_GRAD_ONE_LAUNCH);
   return single && groups > 1 ? 1 : static_cast<int>(groups);
 }

@@ -28,7 +28,8 @@ def test_norm_gradient_of_few_rows(record):  # noqa: F811
         (1, 64): [1], (128, 64): [1], (129, 64): [5], (1024, 64): [32], (1025, 64): [33, 8],      # (32 rows a workgroup in fp32)
         (32, 512): [1], (33, 512): [5], (128, 512): [16], (129, 512): [17, 64],
         (16, 520): [1], (17, 520): [3, 65], (16, 1024): [1], (17, 1024): [3, 128], (256, 1024): [32, 128], (8, 2048): [1], (9, 2048): [3, 256],
-        (4, 4096): [1], (5, 4096): [3, 512], (2, 16384): [1], (3, 16384): [3, 2048],
+        (4, 4096): [1], (5, 4096): [3, 512], (2, 8192): [1], (3, 8192): [3, 1024],
+        (1, 8200): [1], (2, 8200): [2, 1025], (1, 16384): [1], (2, 16384): [2, 2048],
     }
     assert dict(zip(want, launches(record, *[("norm_grad", dict(T=T, d=d)) for T, d in want]))) == want
 
