@@ -117,6 +117,7 @@ static int combine_backward(const CombineGradArgs& a, int dtype, int k, hipStrea
   const int lanes = a.pieces <= 16 ? 16 : a.pieces <= 32 ? 32 : 64;
   const int64_t groups = (static_cast<int64_t>(a.T) + 256 / lanes - 1) / (256 / lanes);
   dim3 grid(static_cast<unsigned>(groups < COMBINE_GRAD_MAX_GROUPS ? groups : COMBINE_GRAD_MAX_GROUPS)), block(256);
+  // (every item counts as kept)
   const int64_t rows = 1 + (a.base ? 1 : 0) + (a.dbase ? 1 : 0) + k * ((a.yp ? 1 : 0) + (a.dyp ? 1 : 0));
   const bool st = a.pieces > 128 && streams_past_caches(rows * a.T * a.pieces * 16);
 #define SCMOE_COMBINE_GRAD_L(K, L, PER, ST)                                                                                    \

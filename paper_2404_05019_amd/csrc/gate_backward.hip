@@ -16,6 +16,8 @@ namespace scmoe {
 
 constexpr int GG_TOK = 16;       // tokens of a wave's step
 static_assert(GG_TOK * SCMOE_MAX_TOPK <= 64, "one register holds a step's items");
+constexpr int GATE_GRAD_FEW_PARTS = 8;   // that the last workgroup of a column block adds up (the rule: GATE_GRAD_ONE_LAUNCH)
+static_assert(GATE_GRAD_FEW_PARTS <= MOST_LEFT);
 
 struct GateGradArgs {
   const unsigned char* x; int64_t ldx;          // strides in bytes
@@ -95,9 +97,6 @@ __device__ __forceinline__ uint32_t word(const uint2& q, int i) { return i == 0 
 
 // Tokens of a step.
 __device__ __forceinline__ int gate_grad_left(const GateGradArgs& a, int64_t t0) { return a.T - t0 < GG_TOK ? static_cast<int>(a.T - t0) : GG_TOK; }
-
-// ST: rows are moved past the caches (streams_past_caches); a choice at run time between the two kinds of store came out of the compiler
-// as one, without the hint.
 
 // What a step reads, as it lies in memory: loaded a step ahead, so nothing here may be looked at (and waited for) before it is due.
 template <bool BF16, int EC>
@@ -216,6 +215,8 @@ __device__ __forceinline__ void gate_grad_add(const Piece (&dp)[4], uint32_t hav
   }
 }
 
+// K: experts per token.  DISPATCH: with the encode's rows.  ST: rows are moved past the caches (streams_past_caches); a choice at run time
+// between the two kinds of store came out of the compiler as one, without the hint.
 template <bool BF16, int EC, int K, bool DISPATCH, bool ST>
 __global__ __launch_bounds__(256, 2) void gate_backward_kernel(GateGradArgs a) {
   using C = GateGradCfg<BF16, EC>;
@@ -557,14 +558,13 @@ static size_t gate_grad_bytes(int T, int d, int E) {        // (for either type)
 //   fp32, 4 experts (1 KB), 8 parts 9.2 / 8.9 / 25.1 (7.3 / 11.3 / 23.5); 16 (4 KB), 2 parts 9.2 / 8.9 / 25.1 (7.5 / 11.2 / 23.5),
 //         4 parts 9.7 / 9.3 / 25.7 (7.5 / 11.2 / 23.6); 32 (8 KB), 2 parts 13.3 / 12.9 / 29.1 (10.4 / 11.2 / 26.4)
 // Up to there the host saves about as much as the arrival costs the device; beyond, the device loses more.
-constexpr int GATE_GRAD_FEW_PARTS = 8;
-static_assert(GATE_GRAD_FEW_PARTS <= MOST_LEFT);
 constexpr int64_t GATE_GRAD_ONE_LAUNCH = 8 << 10;
 
 static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
   const int cols = gate_grad_cols(a.E, dtype);
   dim3 grid(((a.d + cols - 1) / cols * a.splits + 7) / 8 * 8), block(256);
   const bool dispatch = a.dst_row != nullptr;
+  // (every item counts as kept: the host does not know how many were)
   const bool st = streams_past_caches(static_cast<int64_t>(a.T) * a.d * elem_bytes(dtype) * (dispatch ? 2 + a.k : 2));
 #define SCMOE_GATE_GRAD_ST(EC, K, ST)                                                                                                      \
   do {                                                                                                                                     \

@@ -165,9 +165,6 @@ __device__ __forceinline__ void norm_grad_gamma(const NormGradArgs& a, int c, fl
   }
 }
 
-// A workgroup has R rows at a time, W waves each, and takes every gridDim.x-th group of R; a lane's columns are the same in all of
-// them, so dgamma and dbeta are summed in registers and leave as one part per workgroup.  Where there are registers for it the
-// next row is loaded before this one is worked on.
 // Columns 4 i and on of [dgamma, dbeta] of the whole call.
 __device__ __forceinline__ void norm_grad_put(const NormGradArgs& a, int i, const float4& v) {
   float* const to = 4 * i < a.d ? a.dgamma : a.dbeta;
@@ -192,6 +189,9 @@ __device__ __forceinline__ void norm_grad_leave(const NormGradArgs& a, int i, co
   }
 }
 
+// A workgroup has R rows at a time, W waves each, and takes every gridDim.x-th group of R; a lane's columns are the same in all of
+// them, so dgamma and dbeta are summed in registers and leave as one part per workgroup.  Where there are registers for it the
+// next row is loaded before this one is worked on.
 template <bool BF16, int V, int W, int R, bool ST, int L = 64>
 __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(NormGradArgs a) {
   constexpr int NV = BF16 ? 8 : 4, P = V / NV, STEP = L * W, H = NV / 4, AREAS = W <= 2 ? 2 : 1, ROWS = R * (64 / L);

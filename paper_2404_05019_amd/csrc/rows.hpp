@@ -44,8 +44,19 @@ __device__ __forceinline__ void store16(unsigned char* p, const uint4& q) {
   else __builtin_nontemporal_store(u32x4_t{q.x, q.y, q.z, q.w}, reinterpret_cast<u32x4_t*>(p));
 }
 
-// Calls that move more than the 256 MB that the device's last cache holds use streaming loads and stores.  A copy of 1 GB ran at
-// 5.8 TB/s without and 6.3 with them, one of 128 MB at 6.8 without and 6.4 with.
+// Calls that move more than the 256 MB that the device's last cache holds use streaming loads and stores (a copy of 1 GB ran at 5.8 TB/s
+// without and 6.3 with them).  us a call without / with them:
+//                                                              128 MB          256 MB          320 MB          512 MB
+//   norm of 1024 columns, residual, bf16                    23.7 / 25.0     43.8 / 46.9     64.9 / 57.4     99.3 / 92.3
+//   its gradient, fp32                                      27.8 / 28.3     48.2 / 50.2     66.7 / 61.5      104 / 94.3
+//   decode's gradient of 2048 columns, one choice, bf16     23.8 / 25.1     43.9 / 50.9     63.8 / 63.5      107 / 103
+//   gate's gradient with encode of 1024, bf16, 8 experts    31.7 / 34.7     53.7 / 58.0     74.0 / 70.6      120 / 108
+//                                             32 experts    40.6 / 45.5     66.8 / 69.3     85.9 / 82.5      129 / 121
+//                                             64 experts    74.5 / 78.0      129 / 129       156 / 154       233 / 230
+//                                       fp32, 64 experts    64.8 / 67.3      100 / 100       121 / 119       172 / 170
+// Not built with them: norm and its gradient with less than a wave a row (up to 32 pieces of 16 bytes), the decode's gradient up to 128
+// pieces.  Those would gain 3 to 9 % past 256 MB (384 MB of rows of 128 in bf16: norm 74.3 / 69.5, its gradient 78.7 / 73.2, decode's
+// gradient 82.3 / 77.7).
 inline bool streams_past_caches(int64_t bytes) { return bytes > (static_cast<int64_t>(256) << 20); }
 
 __device__ __forceinline__ uint4 zero_unless(bool keep, const uint4& q) {
