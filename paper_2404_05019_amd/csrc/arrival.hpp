@@ -59,12 +59,15 @@ __device__ __forceinline__ void add_left(const float* part, int n, int64_t strid
 
 constexpr int MOST_LEFT = 32;          // parts that sum_left takes
 
+// MOST: the largest n of the caller's, 8 or MOST_LEFT.
+template <int MOST>
 __device__ __forceinline__ float2 sum_left(const float* part, int n, int64_t stride) {
+  static_assert(MOST == 8 || MOST == MOST_LEFT);
   float2 v = make_float2(0.0f, 0.0f);
   if (n <= 4) add_left<4>(part, n, stride, v);
-  else if (n <= 8) add_left<8>(part, n, stride, v);
+  else if (MOST == 8 || n <= 8) add_left<8>(part, n, stride, v);
   else if (n <= 16) add_left<16>(part, n, stride, v);
-  else add_left<MOST_LEFT>(part, n, stride, v);
+  else add_left<MOST>(part, n, stride, v);
   return v;
 }
 

@@ -516,7 +516,7 @@ __global__ __launch_bounds__(256, 2) void gate_backward_kernel(GateGradArgs a) {
   if (a.marks == nullptr || !last_to_arrive(a.marks + static_cast<int64_t>(c0 / COLS) * a.splits, a.call, split, a.splits, &last_one)) return;
   const int64_t first = static_cast<int64_t>(c0) * a.E;
   for (int i = 2 * tid; i < cols * a.E; i += 512) {       // (an even number: columns come in eights)
-    const float2 v = sum_left(a.parts + first + i, a.splits, a.stride);
+    const float2 v = sum_left<GATE_GRAD_FEW_PARTS>(a.parts + first + i, a.splits, a.stride);
     a.dWg[first + i] = v.x;
     a.dWg[first + i + 1] = v.y;
   }

@@ -344,7 +344,7 @@ __global__ __launch_bounds__(64 * W * R, 2) void layer_norm_backward_kernel(Norm
   }
   if (!a.one_launch || gridDim.x == 1 || !last_to_arrive(a.marks, a.call, blockIdx.x, gridDim.x, &last_one)) return;
   for (int i = threadIdx.x; i < a.d; i += 64 * W * R) {
-    const float2 v = sum_left(a.parts + 2 * i, gridDim.x, a.stride);
+    const float2 v = sum_left<MOST_LEFT>(a.parts + 2 * i, gridDim.x, a.stride);
     float* const to = 2 * i < a.d ? a.dgamma : a.dbeta;
     if (to == nullptr) continue;
     to[2 * i < a.d ? 2 * i : 2 * i - a.d] = v.x;
