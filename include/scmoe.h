@@ -532,7 +532,9 @@ int scmoe_gate_backward_workspace_bytes(int32_t T, int32_t d, int32_t E, size_t*
  * dx_perm, dst_row: the gradient of the packed rows (stride ld_perm) and where scmoe_dispatch put each
  * item; both NULL: dx is the gate's gradient alone.
  * dW_g: [d, E] fp32, dbias: [E] or NULL; both overwritten.  dx must not overlap any input.
- * bf16: the products that make dW_g keep fp32 accuracy; dx is rounded once on store.  Sums in an order that
+ * bf16: the products that make dW_g keep fp32 accuracy.  dl W_g^T is made from two bf16 parts each of dl and W_g,
+ * without the product of the low ones: off by at most 3 * 2^-16 of the sum of |dl W_g|, ahead of dx's rounding on
+ * store (2^-8 of dx).  An infinity in x, dl or W_g makes what it reaches an infinity or NaN.  Sums in an order that
  * does not depend on scheduling.
  */
 int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, const float* W_g, const float* probs,

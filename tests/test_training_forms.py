@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 if torch.cuda.is_available():
     from paper_2404_05019_amd import binding as B
     from gpu_util import DEV
-    from test_training_ops import H, NAN, check_gate, close, empty, gen, norm_grad_ref, norm_ref, normal, packed, workspace
+    from test_training_ops import H, NAN, check_gate, close, empty, gen, norm_grad_ref, norm_ref, normal, packed, routing, workspace
 
 CACHES = 256 << 20          # calls that move more bytes load and store past the caches
 
@@ -111,3 +111,25 @@ def test_combine_backward_past_the_caches(k, cg, d, dtype):
         close(dbase, c0 * d64, 0.0, dtype)
         dc0 = d64 * base.double()
         close(dcoef, torch.stack([dc0.sum(1), dc1], 1), 140 * H * torch.stack([dc0.abs().sum(1), size_c1], 1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gate_backward_keeps_infinities_apart(dtype):
+    """An infinity in a token's x reaches its columns of dW_g, one in W_g its column of dx: non-finite there (in bf16 perhaps NaN, where the
+    formula has an infinity), the same bits as without it everywhere else."""
+    T, d, E = 150, 264, 8
+    g = gen(5)
+    x, Wg = normal(g, T, d, dtype=dtype), normal(g, d, E)
+    p, idx, w = routing(g, T, E, 2, 1)
+    dw = normal(g, T, 2)
+    ws, _ = workspace(B.scmoe_gate_backward_workspace_bytes(T, d, E))
+    bad_x, bad_W = x.clone(), Wg.clone()
+    bad_x[77, 9] = float("inf")
+    bad_W[11, 3] = -float("inf")
+    out = [(empty(T, d, dtype), torch.zeros(d, E, device=DEV), torch.zeros(E, device=DEV)) for _ in range(3)]
+    for (a, b), o in zip(((x, Wg), (bad_x, Wg), (x, bad_W)), out):
+        B.scmoe_gate_backward(a, b, p, idx, w, dw, *o, ws, k=2, normalize=1)
+    (dx, dW, db), (dx1, dW1, db1), (dx2, dW2, db2) = out
+    rows, cols = torch.arange(d, device=DEV) != 9, torch.arange(d, device=DEV) != 11
+    assert torch.equal(dx, dx1) and torch.equal(db, db1) and torch.equal(dW[rows], dW1[rows]) and not bool(dW1[9].isfinite().any())
+    assert torch.equal(dW, dW2) and torch.equal(db, db2) and torch.equal(dx[:, cols], dx2[:, cols]) and not bool(dx2[:, 11].isfinite().any())
