@@ -3,6 +3,9 @@
 Only argument marshalling happens here (tensor -> pointer / stride / size); every step of
 the layer runs in the HIP kernels.  torch is used for device memory and streams.  There is
 no CPU fallback: loading fails loudly when the library has not been built.
+
+Autograd does not see these calls: tensors that require gradients are taken as they are, nothing is recorded, and the
+gradients are what the _backward calls write.
 """
 import ctypes as C
 import os
