@@ -550,15 +550,18 @@ static size_t gate_grad_bytes(int T, int d, int E) {        // (for either type)
   return s == 1 ? 0 : static_cast<size_t>(s) * (gate_grad_stride(d, E) * 4 + 8 * blocks);   // parts and marks
 }
 
-// A column block's last workgroup adds up its parts in the same launch where they are at most eight, of 8 KB in all.  us a call in a
-// replayed graph / called back to back from Python / waited for one by one, against two launches:
+// A column block's last workgroup adds up its parts in the same launch where they are at most eight, of up to 4 KB each and 16 KB in all.
+// us a call in a replayed graph / called back to back from Python / waited for one by one, against two launches:
 //   bf16, 4 experts (2 KB a part), 4 parts 10.1 / 9.7 / 26.0 (8.5 / 11.3 / 24.7), 8 parts 10.6 / 10.3 / 26.4 (8.6 / 11.3 / 24.7)
-//         8 (4 KB), 2 parts 10.3 / 10.0 / 26.2 (8.7 / 11.2 / 24.7), 4 parts 10.7 / 10.4 / 26.6 (8.7 / 11.2 / 24.8)
+//         8 (4 KB), 2 parts 10.3 / 10.0 / 26.2 (8.7 / 11.2 / 24.7), 4 parts 10.7 / 10.4 / 26.6 (8.7 / 11.2 / 24.8),
+//         8 parts 11.7 / 11.5 / 27.7 (8.8 / 11.4 / 25.1)
 //         16 (8 KB), 2 parts 11.5 / 11.2 / 27.4 (8.7 / 11.2 / 24.8)
-//   fp32, 4 experts (1 KB), 8 parts 9.2 / 8.9 / 25.1 (7.3 / 11.3 / 23.5); 16 (4 KB), 2 parts 9.2 / 8.9 / 25.1 (7.5 / 11.2 / 23.5),
-//         4 parts 9.7 / 9.3 / 25.7 (7.5 / 11.2 / 23.6); 32 (8 KB), 2 parts 13.3 / 12.9 / 29.1 (10.4 / 11.2 / 26.4)
-// Up to there the host saves about as much as the arrival costs the device; beyond, the device loses more.
-constexpr int64_t GATE_GRAD_ONE_LAUNCH = 8 << 10;
+//   fp32, 4 experts (1 KB), 8 parts 9.2 / 8.9 / 25.1 (7.3 / 11.3 / 23.5); 8 (2 KB), 8 parts 9.6 / 9.4 / 25.5 (7.6 / 11.3 / 23.8)
+//         16 (4 KB), 4 parts 9.7 / 9.3 / 25.7 (7.5 / 11.2 / 23.6), 8 parts 10.7 / 10.5 / 26.7 (7.6 / 11.3 / 23.7)
+//         32 (8 KB), 2 parts 13.3 / 12.9 / 29.1 (10.4 / 11.2 / 26.4)
+// Up to there the arrival costs the device no more (1.1 to 2.2 us) than the second launch costs the host (2.6 to 2.8); beyond it does.
+constexpr int64_t GATE_GRAD_SMALL_PART = 4 << 10;
+constexpr int64_t GATE_GRAD_ONE_LAUNCH = 16 << 10;
 
 static int gate_backward(const GateGradArgs& a, int dtype, hipStream_t stream) {
   const int cols = gate_grad_cols(a.E, dtype);
@@ -641,7 +644,8 @@ extern "C" int scmoe_gate_backward(const void* x, int64_t ldx, int32_t dtype, co
   a.Wg16 = E % 4 == 0 && aligned16(W_g);
   a.parts = static_cast<float*>(workspace); a.stride = gate_grad_stride(d, E);
   a.dWg = dW_g; a.dbias = dbias;
-  if (a.splits > 1 && a.splits <= GATE_GRAD_FEW_PARTS && static_cast<int64_t>(a.splits) * gate_grad_cols(E, dtype) * E * 4 <= GATE_GRAD_ONE_LAUNCH) {
+  const int64_t part = static_cast<int64_t>(gate_grad_cols(E, dtype)) * E * 4;
+  if (a.splits > 1 && a.splits <= GATE_GRAD_FEW_PARTS && part <= GATE_GRAD_SMALL_PART && a.splits * part <= GATE_GRAD_ONE_LAUNCH) {
     a.marks = reinterpret_cast<unsigned long long*>(a.parts + a.splits * a.stride);
     a.call = next_call();
   }

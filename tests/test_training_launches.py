@@ -37,8 +37,8 @@ def test_norm_gradient_of_few_rows(record):  # noqa: F811
 def test_gate_gradient_of_few_tokens(record):  # noqa: F811
     """Both sides of the rule: parts that a column block's last workgroup adds up, and a second launch for them (64 tokens a part)."""
     bf16 = dict(dtype=BF16)
-    want = [(dict(T=64, E=16), 1), (dict(T=512, E=4), 1), (dict(T=513, E=4), 2), (dict(T=256, E=8), 1), (dict(T=257, E=8), 2), (dict(T=128, E=16), 1),
-            (dict(T=129, E=16), 2), (dict(T=65, E=32), 2), (dict(T=256, E=4, **bf16), 1), (dict(T=257, E=4, **bf16), 2), (dict(T=128, E=8, **bf16), 1),
-            (dict(T=129, E=8, **bf16), 2), (dict(T=65, E=16, **bf16), 2), (dict(T=64, E=64, **bf16), 1)]
+    want = [(dict(T=64, E=16), 1), (dict(T=512, E=8), 1), (dict(T=513, E=4), 2), (dict(T=512, E=9), 2), (dict(T=256, E=16), 1), (dict(T=257, E=16), 2),
+            (dict(T=65, E=17), 2), (dict(T=512, E=4, **bf16), 1), (dict(T=513, E=4, **bf16), 2), (dict(T=256, E=8, **bf16), 1),
+            (dict(T=257, E=8, **bf16), 2), (dict(T=65, E=9, **bf16), 2), (dict(T=64, E=64, **bf16), 1)]
     got = launches(record, *[("gate_grad", dict(kw, d=256)) for kw, _ in want])
     assert [len(lines) for lines in got] == [n for _, n in want]
