@@ -418,8 +418,9 @@ def _scratch(workspace, device):
     """Address and bytes of a workspace (None: none)."""
     if workspace is None:
         return None, 0
-    n = workspace.numel()
-    return _dense(workspace, n, device, workspace.dtype), n * workspace.element_size()
+    if not workspace.is_contiguous() or workspace.get_device() != device:
+        _refuse(workspace, "a workspace without gaps")
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def scmoe_layer_norm(x, gamma, beta, eps, y, residual=None, sum_out=None, mean=None, rstd=None, stream=None):
@@ -458,8 +459,10 @@ def scmoe_balance_loss(probs, expert_idx, k, coef, load, mean_prob, slope, loss,
     """Loss, items per expert and the loss's slope in every counted token's probabilities."""
     T, E = probs.shape
     dev, hs = _place(probs, stream)
+    if probs.dtype is not torch.float32 or not probs.is_contiguous():
+        _refuse(probs, "contiguous %s" % torch.float32)
     wp, nb = _scratch(workspace, dev)
-    _check(lib().scmoe_balance_loss(_table(probs, (T, E), dev), _table(expert_idx, (T, k), dev, torch.int32), _mask(mask, T, dev), T, E, k, coef,
+    _check(lib().scmoe_balance_loss(probs.data_ptr(), _table(expert_idx, (T, k), dev, torch.int32), _mask(mask, T, dev), T, E, k, coef,
                                     _dense(load, E, dev, torch.int32), _dense(mean_prob, E, dev), _dense(slope, E, dev), _dense(loss, 1, dev), wp, nb,
                                     hs), "scmoe_balance_loss")
 
