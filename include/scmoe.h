@@ -1,6 +1,7 @@
 /*
- * scmoe.h — C ABI of the MI355X (gfx950) ScMoE library: the forward pass of a block, and what
- * trains its routing part (layer norm, balance loss, gradients of gate, encode and decode).
+ * scmoe.h — C ABI of the MI355X (gfx950) ScMoE library: the forward pass of a block, what
+ * trains its routing part (layer norm, balance loss, gradients of gate, encode and decode), and gated
+ * experts with their training (gated feed-forward block, its gradient, activation checkpoints in 8 bits).
  *
  * One shortcut-connected MoE block (ScMoE paper, Sec. 3.1, Eq. (7)):
  *
@@ -58,6 +59,13 @@ enum { SCMOE_F32 = 0, SCMOE_BF16 = 1 };
  * the exact erf form 0.5 v (1 + erf(v / sqrt 2)) is the default reading. */
 enum { SCMOE_GELU_ERF = 0, SCMOE_GELU_TANH = 1 };
 
+/* A gated feed-forward block takes one more activation, x / (1 + exp(-x)). */
+enum { SCMOE_SILU = 2 };
+
+/* How activations are kept for a backward pass: not at all; in the call's dtype; in 8 bits, as
+ * scmoe_checkpoint_pack lays them out. */
+enum { SCMOE_KEEP_NOTHING = 0, SCMOE_KEEP_FULL = 1, SCMOE_KEEP_8BIT = 2 };
+
 /* How the shared expert's output and the routed output are merged (Sec. 5.2):
  * direct add (Eq. (6)), CG-1 (Eq. (14)-(15)), CG-2 (Eq. (16)-(17)). */
 enum { SCMOE_CG_NONE = 0, SCMOE_CG_1 = 1, SCMOE_CG_2 = 2 };
@@ -68,6 +76,10 @@ enum { SCMOE_CG_NONE = 0, SCMOE_CG_1 = 1, SCMOE_CG_2 = 2 };
 #define SCMOE_MAX_TOPK 4
 /* Upper limit on the width of a normed row. */
 #define SCMOE_MAX_NORM_WIDTH 16384
+/* Upper limit on the model and the hidden width of a gated feed-forward block. */
+#define SCMOE_MAX_GATED_WIDTH (1 << 20)
+/* Upper limit on its packed rows. */
+#define SCMOE_MAX_GATED_ROWS (1 << 30)
 
 /* Shape and options of one layer.  Plain data, host memory, read during the call only. */
 typedef struct scmoe_desc {
@@ -561,6 +573,93 @@ int scmoe_combine_backward(const void* dy, int64_t lddy, int32_t dtype, const vo
                            int32_t d, int32_t k, const void* base, int64_t ldbase, const float* coef,
                            void* dy_perm, int64_t lddyp, float* dgate_w, void* dbase, int64_t lddbase,
                            float* dcoef, void* stream);
+
+/*
+ * Activation checkpoints: rows of `width` values in 8 bits, kept from a forward pass for the backward
+ * pass in half (bf16) or a quarter (fp32) of the memory.  A checkpoint row is `width` codes of one byte
+ * (sign, 4 bits of exponent, 3 of mantissa; largest 448) and then one byte of scale for every 32
+ * columns, the last of them for what is left of the width:
+ *
+ *   s    = the least power of two, of at least 2^-126, with max |x| <= 448 s over the 32 columns;
+ *          its byte is its exponent + 127
+ *   code = x / s rounded to nearest even, restored as code * s
+ *
+ * so a restored value is off by at most 2^-4 of it, or 2^-10 s where it is below 2^-6 s.  A block that
+ * holds an infinity or a NaN has the scale byte 255 and is restored as NaN throughout; values above
+ * 2^128 (1 - 2^-5) may be restored as infinities.  Restored values are exact in bf16 (those below
+ * 2^-126: rounded).
+ * x: [max_rows, width], q: max_rows checkpoint rows of ldq bytes (a multiple of 16, at least width +
+ * ceil(width / 32); scmoe_checkpoint_ld gives the least; bytes behind the scales are left alone).
+ * width: a multiple of 8.  n_rows: one int32 on the DEVICE, the rows to be treated (offsets + E of a
+ * dispatch; at most max_rows are), or NULL: all.  Rows past it are neither read nor written.
+ */
+int scmoe_checkpoint_ld(int32_t width, int64_t* ld);      /* host only; `ld` is a host pointer */
+int scmoe_checkpoint_pack(const void* x, int64_t ldx, int32_t dtype, const int32_t* n_rows,
+                          int32_t max_rows, int32_t width, void* q, int64_t ldq, void* stream);
+int scmoe_checkpoint_unpack(const void* q, int64_t ldq, const int32_t* n_rows, int32_t max_rows,
+                            int32_t width, void* x, int64_t ldx, int32_t dtype, void* stream);
+
+/* Bytes of optional workspace of scmoe_gated_ffn (may be 0).  `out` is a host pointer. */
+int scmoe_gated_ffn_workspace_bytes(int32_t dtype, int32_t d, int32_t F, size_t* out);
+
+/*
+ * Gated experts over packed segments, beside the two-layer ones of scmoe_expert_ffn:
+ *
+ *   for e in 0..E-1, r in [offsets[e], offsets[e+1]):
+ *       (g, u)[r, :]  = W1[e] . x_perm[r, :]                 g: the first F rows of W1[e], u: the others
+ *       hidden[r, :]  = act(g[r, :]) * u[r, :]
+ *       y_perm[r, :]  = W2[e] . hidden[r, :]
+ *
+ * offsets, max_rows, E, hidden and the row strides: as in scmoe_expert_ffn (rows past offsets[E] are not
+ * touched; E = 1 and offsets = {0, T} is a dense block).  W1: [E, 2 F, d] with row stride ldw1, W2:
+ * [E, d, F] with row stride ldw2.  act: SCMOE_SILU, SCMOE_GELU_ERF or SCMOE_GELU_TANH.  d and F are
+ * multiples of 8, up to SCMOE_MAX_GATED_WIDTH, max_rows up to SCMOE_MAX_GATED_ROWS; row strides of up to
+ * 2^21 elements, an expert's W1 and W2 of less than 3.75 GiB each, and no product of more than 2^30 tiles
+ * of 128 x 64 outputs, else SCMOE_ERR_SHAPE.
+ * pre_keep: what stays of g and u for scmoe_gated_ffn_backward.
+ *   SCMOE_KEEP_NOTHING  nothing (serving); pre is not looked at
+ *   SCMOE_KEEP_FULL     pre: [max_rows, 2 F] in dtype, row stride ldpre: g, then u
+ *   SCMOE_KEEP_8BIT     pre: 2 max_rows checkpoint rows of width F (ldpre: bytes of one); g of row r is
+ *                       checkpoint row 2 r, u is 2 r + 1.  The codes are made from the fp32 sums.
+ * fp32 accumulation; bf16: hidden, g, u and y are rounded once each on store, hidden from the fp32 g and
+ * u.  Results are the same from call to call.
+ * workspace: optional device scratch (16-byte aligned) of scmoe_gated_ffn_workspace_bytes bytes; NULL or
+ * less of it: slower where it would be used.
+ */
+int scmoe_gated_ffn(const void* x_perm, int64_t ld_perm, int32_t dtype, const int32_t* offsets,
+                    int32_t max_rows, int32_t E, int32_t d, int32_t F, const void* W1, int64_t ldw1,
+                    const void* W2, int64_t ldw2, int32_t act, void* hidden, int64_t ldh, void* pre,
+                    int64_t ldpre, int32_t pre_keep, void* y_perm, int64_t ldy, void* workspace,
+                    size_t ws_bytes, void* stream);
+
+/* Bytes of workspace scmoe_gated_ffn_backward needs: the gradients of g and u, the hidden rows and the
+ * input rows of max_rows rows, in dtype.  `out` is a host pointer. */
+int scmoe_gated_ffn_backward_workspace_bytes(int32_t dtype, int32_t max_rows, int32_t E, int32_t d,
+                                             int32_t F, size_t* out);
+
+/*
+ * Gradient of scmoe_gated_ffn; arguments named there mean the same.  dy_perm: [max_rows, d], the
+ * gradient of y_perm.  With g and u as they were kept (in 8 bits: as they are restored):
+ *
+ *   dh = W2[e]^T . dy_perm[r, :],  du = dh * act(g),  dg = dh * u * act'(g)
+ *   dx_perm[r, :] = W1[e]^T . (dg, du)
+ *   dW1[e] = sum over the segment's rows of (dg, du)[r, :]^T x[r, :],   dW2[e] = sum of dy_perm[r, :]^T (act(g) u)
+ *
+ * x: the input rows, kept like this by the caller: SCMOE_KEEP_FULL: x_perm, stride in elements;
+ * SCMOE_KEEP_8BIT: max_rows checkpoint rows of width d, stride in bytes.  x is needed for dW1 alone and
+ * W1 for dx_perm alone.  dx_perm, dW1, dW2: each may be NULL, not all of them.  dW1: [E, 2 F, d], dW2:
+ * [E, d, F], in dtype, without gaps, overwritten (an expert without rows: zeros; max_rows 0: all zeros,
+ * and only offsets is looked at).  Rows of dx_perm past offsets[E] are not touched, and what lies past
+ * offsets[E] in dy_perm, x and pre reaches nothing.  dx_perm may be the buffer of dy_perm only where dW2
+ * is NULL.  fp32 accumulation in an order that does not depend on scheduling; bf16: dg, du and act(g) u
+ * are rounded on their way to the second products.
+ */
+int scmoe_gated_ffn_backward(const void* dy_perm, int64_t lddy, int32_t dtype, const void* x, int64_t ldx,
+                             int32_t x_keep, const void* pre, int64_t ldpre, int32_t pre_keep,
+                             const int32_t* offsets, int32_t max_rows, int32_t E, int32_t d, int32_t F,
+                             const void* W1, int64_t ldw1, const void* W2, int64_t ldw2, int32_t act,
+                             void* dx_perm, int64_t lddx, void* dW1, void* dW2, void* workspace,
+                             size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -16,7 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libscmoe.so")
 
 F32, BF16 = 0, 1
-GELU_ERF, GELU_TANH = 0, 1
+GELU_ERF, GELU_TANH, SILU = 0, 1, 2
+KEEP_NOTHING, KEEP_FULL, KEEP_8BIT = 0, 1, 2
 CG_NONE, CG_1, CG_2 = 0, 1, 2
 MAX_EXPERTS = 64
 
@@ -30,7 +31,9 @@ EXPORTS = ["scmoe_status_string", "scmoe_last_hip_error", "scmoe_set_gemm_varian
            "moe_top2_layer_forward",
            "scmoe_layer_norm", "scmoe_layer_norm_backward_workspace_bytes", "scmoe_layer_norm_backward",
            "scmoe_balance_loss_workspace_bytes", "scmoe_balance_loss", "scmoe_gate_backward_workspace_bytes",
-           "scmoe_gate_backward", "scmoe_combine_backward"]
+           "scmoe_gate_backward", "scmoe_combine_backward",
+           "scmoe_checkpoint_ld", "scmoe_checkpoint_pack", "scmoe_checkpoint_unpack", "scmoe_gated_ffn_workspace_bytes", "scmoe_gated_ffn",
+           "scmoe_gated_ffn_backward_workspace_bytes", "scmoe_gated_ffn_backward"]
 
 
 class Desc(C.Structure):
@@ -112,6 +115,14 @@ def lib():
                                              i64, vp, vp, vp, sz, vp]
         _lib.scmoe_combine_backward.argtypes = [vp, i64, i32, vp, i64, vp, vp, i32, i32, i32, vp, i64, vp, vp, i64, vp, vp, i64, vp,
                                                 vp]
+        _lib.scmoe_checkpoint_ld.argtypes = [i32, C.POINTER(i64)]
+        _lib.scmoe_checkpoint_pack.argtypes = [vp, i64, i32, vp, i32, i32, vp, i64, vp]
+        _lib.scmoe_checkpoint_unpack.argtypes = [vp, i64, vp, i32, i32, vp, i64, i32, vp]
+        _lib.scmoe_gated_ffn_workspace_bytes.argtypes = [i32, i32, i32, C.POINTER(sz)]
+        _lib.scmoe_gated_ffn.argtypes = [vp, i64, i32, vp, i32, i32, i32, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp, i64, vp, sz, vp]
+        _lib.scmoe_gated_ffn_backward_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, C.POINTER(sz)]
+        _lib.scmoe_gated_ffn_backward.argtypes = [vp, i64, i32, vp, i64, i32, vp, i64, i32, vp, i32, i32, i32, i32, vp, i64, vp, i64, i32, vp, i64,
+                                                  vp, vp, vp, sz, vp]
     return _lib
 
 
@@ -504,3 +515,100 @@ def scmoe_combine_backward(dy, y_perm, dst_row, gate_w, k, dy_perm=None, dgate_w
     _check(lib().scmoe_combine_backward(gp, ldg, dtype_code(dy), yp, ldy, _table(dst_row, items, dev, torch.int32), _table(gate_w, items, dev), T, d, k,
                                         bp, ldb, _table(coef, pairs, dev), pp, ldp, _table(dgate_w, items, dev), op, ldo, _table(dcoef, pairs, dev),
                                         hs), "scmoe_combine_backward")
+
+
+def scmoe_checkpoint_ld(width):
+    """Bytes of a checkpoint row of that width, the least stride of the rows."""
+    out = C.c_int64(0)
+    _check(lib().scmoe_checkpoint_ld(width, C.byref(out)), "scmoe_checkpoint_ld")
+    return out.value
+
+
+def _kept_rows(t, rows, width, device):
+    """Address and stride in bytes of at least that many checkpoint rows."""
+    if t.dtype is not torch.uint8 or t.dim() != 2 or t.shape[0] < rows or t.shape[1] < width + -(-width // 32) or t.get_device() != device:
+        _refuse(t, "%d checkpoint rows of %d values" % (rows, width))
+    return t.data_ptr(), _ld(t)
+
+
+def scmoe_checkpoint_pack(x, q, n_rows=None, stream=None):
+    """Rows of x into the checkpoint rows q (torch.uint8); n_rows: how many of them, on the GPU."""
+    rows, width = x.shape
+    dev, hs = _place(x, stream)
+    (xp, ldx), (qp, ldq) = _view(x), _kept_rows(q, rows, width, dev)
+    _check(lib().scmoe_checkpoint_pack(xp, ldx, dtype_code(x), _dense(n_rows, 1, dev, torch.int32), rows, width, qp, ldq, hs), "scmoe_checkpoint_pack")
+
+
+def scmoe_checkpoint_unpack(q, x, n_rows=None, stream=None):
+    """The values of the checkpoint rows q into x; n_rows: how many of them, on the GPU."""
+    rows, width = x.shape
+    dev, hs = _place(x, stream)
+    (xp, ldx), (qp, ldq) = _view(x), _kept_rows(q, rows, width, dev)
+    _check(lib().scmoe_checkpoint_unpack(qp, ldq, _dense(n_rows, 1, dev, torch.int32), rows, width, xp, ldx, dtype_code(x), hs),
+           "scmoe_checkpoint_unpack")
+
+
+def _kept(t, rows, width, parts, dtype, device):
+    """Address, stride and kind of kept activations of `parts` widths a row: in dtype, or in 8 bits (torch.uint8)."""
+    if t is None:
+        return None, 0, KEEP_NOTHING
+    if t.dtype is torch.uint8:
+        return (*_kept_rows(t, rows * parts, width, device), KEEP_8BIT)
+    return (*_packed_rows(t, rows, width * parts, dtype, device), KEEP_FULL)
+
+
+def _packed_rows(t, rows, width, dtype, device):
+    """Address and row stride of at least that many packed rows (None: not given)."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] < rows or t.shape[1] != width or t.get_device() != device:
+        _refuse(t, "%d rows of %d %s" % (rows, width, dtype))
+    return t.data_ptr(), _ld(t)
+
+
+def _experts(t, shape, dtype, device):
+    """Address and row stride of weights [E, out, in] (None: not given)."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or tuple(t.shape) != shape or t.get_device() != device:
+        _refuse(t, "%s of %s" % (shape, dtype))
+    return t.data_ptr(), _ldw(t)
+
+
+def scmoe_gated_ffn_workspace_bytes(dtype, d, F):
+    out = C.c_size_t(0)
+    _check(lib().scmoe_gated_ffn_workspace_bytes(dtype, d, F, C.byref(out)), "scmoe_gated_ffn_workspace_bytes")
+    return out.value
+
+
+def scmoe_gated_ffn(x_perm, offsets, max_rows, W1, W2, hidden, y_perm, act=SILU, pre=None, workspace=None, stream=None):
+    """y_perm = W2 (act(g) u) with (g, u) = W1 x_perm, expert by expert.  pre keeps g and u for the backward pass: rows of 2 F in
+    the type of x_perm, or two checkpoint rows of F (torch.uint8) for every row."""
+    E, d, F = W2.shape
+    dtype, (dev, hs) = x_perm.dtype, _place(x_perm, stream)
+    (xp, ldx), (yp, ldy), (hp, ldh) = (_packed_rows(t, max_rows, w, dtype, dev) for t, w in ((x_perm, d), (y_perm, d), (hidden, F)))
+    (w1, ld1), (w2, ld2) = _experts(W1, (E, 2 * F, d), dtype, dev), _experts(W2, (E, d, F), dtype, dev)
+    pp, ldp, keep = _kept(pre, max_rows, F, 2, dtype, dev)
+    wp, nb = _scratch(workspace, dev)
+    _check(lib().scmoe_gated_ffn(xp, ldx, dtype_code(x_perm), _dense(offsets, E + 1, dev, torch.int32), max_rows, E, d, F, w1, ld1, w2, ld2, act, hp, ldh,
+                                 pp, ldp, keep, yp, ldy, wp, nb, hs), "scmoe_gated_ffn")
+
+
+def scmoe_gated_ffn_backward_workspace_bytes(dtype, max_rows, E, d, F):
+    out = C.c_size_t(0)
+    _check(lib().scmoe_gated_ffn_backward_workspace_bytes(dtype, max_rows, E, d, F, C.byref(out)), "scmoe_gated_ffn_backward_workspace_bytes")
+    return out.value
+
+
+def scmoe_gated_ffn_backward(dy_perm, x, pre, offsets, max_rows, W1, W2, act=SILU, dx_perm=None, dW1=None, dW2=None, workspace=None, stream=None):
+    """dx_perm, dW1 and dW2 (each may be None) of scmoe_gated_ffn.  x: its input rows, pre: what it kept; each in the type of dy_perm
+    or in 8 bits (torch.uint8)."""
+    E, d, F = W2.shape
+    dtype, (dev, hs) = dy_perm.dtype, _place(dy_perm, stream)
+    (gp, ldg), (dp, ldd) = (_packed_rows(t, max_rows, d, dtype, dev) for t in (dy_perm, dx_perm))
+    (w1, ld1), (w2, ld2) = _experts(W1, (E, 2 * F, d), dtype, dev), _experts(W2, (E, d, F), dtype, dev)
+    (xp, ldx, xk), (pp, ldp, pk) = _kept(x, max_rows, d, 1, dtype, dev), _kept(pre, max_rows, F, 2, dtype, dev)
+    wp, nb = _scratch(workspace, dev)
+    _check(lib().scmoe_gated_ffn_backward(gp, ldg, dtype_code(dy_perm), xp, ldx, xk, pp, ldp, pk, _dense(offsets, E + 1, dev, torch.int32), max_rows, E, d, F,
+                                          w1, ld1, w2, ld2, act, dp, ldd, _dense(dW1, 2 * E * F * d, dev, dtype), _dense(dW2, E * d * F, dev, dtype), wp, nb,
+                                          hs), "scmoe_gated_ffn_backward")

@@ -1,0 +1,574 @@
+// The products of the gated feed-forward block and of its gradient, on the matrix cores (bf16 and fp32): one kernel, whose operands may
+// lie along k or across it, over the packed segments of the experts.
+//
+//   GATE  [g; u] = W1[e] x       both operands along k; act(g) u on store, g and u beside it where they are kept
+//   DOWN  y = W2[e] h            both along k
+//   DH    dh = W2[e]^T dy        W2 across k; on store the gradients of g and u, and h again, from the kept g and u
+//   DX    dx = W1[e]^T [dg; du]  W1 across k
+//   DW    dW1[e] = [dg; du]^T x, dW2[e] = dy^T h     both across k, which is the rows of the segment
+//
+// A tile of BM x BN is one workgroup's; its operands come through NS stages in LDS, copied there directly (16 bytes a lane).
+//  * Along k, a stage holds rows of 128 bytes of k (64 bf16 or 32 fp32), 16-byte chunks swizzled (swz); a fragment is 16 rows, lane
+//    (l16, lq) holding chunk 4 s + lq of row l16 for step s: 32 k of bf16 for one instruction, 16 of fp32 for four, which take element c
+//    of every chunk (the order of k inside a step is the same for both operands).
+//  * Across k, it holds the 64 (32) rows of k as they lie in memory, all columns of the tile, and the fragments are transposed on the way
+//    out of LDS: bf16 by ds_read_b64_tr_b16, in which 16 lanes read four rows of 16 columns and lane i gets column i of them; fp32 by four
+//    reads of 4 bytes.  Units of 16 columns are swizzled by the row, so that the rows a read touches lie in different banks.
+//    Nothing is transposed in memory.
+//  * Rows past a segment, columns past a matrix and k past its end read zeros (offsets outside the buffer), in both operands, so that what
+//    lies there (another expert's rows, NaN) reaches nothing.
+//  * Persistent workgroups, as in ffn_mfma.hip, whose schedule, barrier and two-group refill of a stage these kernels share.
+#pragma once
+#include "checkpoint.hpp"
+#include "gated_act.hpp"
+#include "mfma_common.hpp"
+#include <atomic>
+
+namespace scmoe {
+
+enum { G_GATE = 0, G_DOWN = 1, G_DH = 2, G_DX = 3, G_DW = 4 };
+enum { KEEP_NONE = 0, KEEP_FULL = 1, KEEP_8BIT = 2 };
+
+// One product; strides in elements.  A: [rows, Kd] (DW: [rows, M]).  B: [E, N, Kd], GATE [E, 2 N, Kd]; DH, DX [E, Kd, N]; DW [rows, N].
+struct GatedJob {
+  const unsigned char* A; int64_t lda;
+  const unsigned char* B; int64_t ldb;
+  unsigned char* C; int64_t ldc;       // [rows, N]: hidden, y, h again, dx;  DW: [E, M, N]
+  int M, N, Kd;
+  int mt, nt;                          // tiles of a DW matrix down and across; of the others across
+  int tiles;                           // DW: E mt nt
+};
+struct GatedArgs {
+  GatedJob j[2];                       // DW: two products in a launch (the second may have no tiles)
+  const int32_t* offsets;
+  int E, act;
+  unsigned char* pre; int64_t ldpre;   // GATE: written, DH: read: [rows, 2 F], or checkpoint rows 2 r, 2 r + 1 (strides in bytes)
+  unsigned char* dpre; int64_t lddpre; // DH: gradients of g and u, [rows, 2 F]
+};
+
+template <bool F32_, int BM_, int BN_, int WM_, int WN_, int NS_>
+struct GatedCfg {
+  static constexpr bool F32 = F32_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NS = NS_;
+  static constexpr int EB = F32 ? 4 : 2, VE = 16 / EB, BK = 128 / EB, KS = 2;      // KS: k steps of 64 bytes in a stage
+  static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+  static constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NJ = TN / 16;
+  static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
+  static constexpr int APW = A_BYTES / 1024 / WAVES, BPW = B_BYTES / 1024 / WAVES;  // copies of a wave and k-tile
+  static constexpr int LDS = NS * STAGE;
+  static constexpr int WG_PER_CU = (160 * 1024 / LDS) < (8 / WAVES) ? (160 * 1024 / LDS) : (8 / WAVES);
+  static_assert(TM % 32 == 0 && TN == 64 && APW % 2 == 0 && WG_PER_CU >= 1 && NS >= 2, "tile shape");
+};
+
+// Swizzle of an operand across k: a read takes rows k of 8 consecutive ones at a time of two (bf16: lanes' groups of 16 on rows
+// 8 lq + 0..3) or of four (fp32: rows 4 lq + c) groups.  ROWB: bytes of a row in LDS; the result is added (xor) to the unit of 16 columns.
+template <bool F32, int ROWB>
+__host__ __device__ constexpr int across_swz(int k) {
+  if (F32) return (k >> 2) & 3;
+  return ROWB >= 256 ? (k & 3) | (((k >> 3) & 1) << 2) : ((k >> 1) & 1) | (((k >> 3) & 1) << 1);
+}
+
+typedef unsigned int g_u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int g_u32x2 __attribute__((ext_vector_type(2)));
+
+// Sixteen columns of four rows each of k, transposed (see above).
+__device__ __forceinline__ g_u32x2 lds_read_transposed(uint32_t at) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef __bf16 v4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(g_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16(reinterpret_cast<__attribute__((address_space(3))) v4*>(static_cast<uintptr_t>(at))));
+#else
+  return g_u32x2{0, 0};
+#endif
+}
+
+// The largest value over the four lanes that hold 16 columns each of a row's 32 (lanes l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ uint32_t max_over_lq(uint32_t v) {
+  const g_u32x2 a = __builtin_bit_cast(g_u32x2, __builtin_amdgcn_permlane32_swap(v, v, false, false));
+  v = max(a[0], a[1]);
+  const g_u32x2 b = __builtin_bit_cast(g_u32x2, __builtin_amdgcn_permlane16_swap(v, v, false, false));
+  return max(b[0], b[1]);
+}
+
+template <bool F32>
+__device__ __forceinline__ void store4(unsigned char* p, const float* v) {
+  if constexpr (F32) *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
+  else *reinterpret_cast<uint2*>(p) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
+}
+template <bool F32>
+__device__ __forceinline__ void load4(const unsigned char* p, float* v) {
+  if constexpr (F32) {
+    const f32x4_t t = *reinterpret_cast<const f32x4_t*>(p);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = t[q];
+  } else {
+    const uint2 t = *reinterpret_cast<const uint2*>(p);
+    v[0] = __uint_as_float(t.x << 16);
+    v[1] = __uint_as_float(t.x & 0xffff0000u);
+    v[2] = __uint_as_float(t.y << 16);
+    v[3] = __uint_as_float(t.y & 0xffff0000u);
+  }
+}
+
+template <class CFG, int MODE, int KEEP>
+__global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void gated_kernel(const GatedArgs p) {
+  constexpr bool F32 = CFG::F32;
+  constexpr int BM = CFG::BM, BN = CFG::BN, EB = CFG::EB, VE = CFG::VE, BK = CFG::BK, KS = CFG::KS, NS = CFG::NS;
+  constexpr int MI = CFG::MI, NJ = CFG::NJ, TM = CFG::TM, TN = CFG::TN, STAGE = CFG::STAGE, A_BYTES = CFG::A_BYTES;
+  constexpr int APW = CFG::APW, BPW = CFG::BPW, LPW = APW + BPW, H = MI / 2;
+  constexpr bool A_ACROSS = MODE == G_DW, B_ACROSS = MODE >= G_DH;
+  constexpr int BNF = MODE == G_GATE ? BN / 2 : BN;             // columns of the output that a tile has
+  constexpr int A_ROWB = BM / 2 * EB, B_ROWB = BN * EB;         // across k: bytes of an LDS row (A: of half the tile's columns, see issue_a)
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, lq = lane >> 4;
+  const int wave_m = wave / CFG::WN, wave_n = wave % CFG::WN;
+
+  // ---- what this workgroup does: tiles slot, slot + nslots, ... of its XCD's share ---------------------------
+  const int xcd = blockIdx.x & 7, nslots = gridDim.x >> 3;
+  int it = blockIdx.x >> 3;
+  constexpr int GM = MODE == G_GATE || MODE == G_DH ? 6 : 4;
+  TileSchedule<BM, BNF, GM> sched(MODE == G_DW ? 0 : p.j[0].nt, MODE == G_DW ? 0 : p.E, p.offsets, 0, 1, false, 1, xcd, nslots);
+  // DW: as many tiles for every expert; dealt like the schedule's
+  const int dw_all = p.j[0].tiles + p.j[1].tiles;
+  constexpr int RR = decltype(sched)::RR;
+  const int dw_dealt = dw_all / (8 * RR) * RR, dw_rest = dw_all - 8 * dw_dealt, dw_share = (dw_rest + 7) >> 3;
+  int items = sched.ngemm;
+  if (MODE == G_DW) {
+    int more = dw_rest - xcd * dw_share;
+    more = more < 0 ? 0 : more > dw_share ? dw_share : more;
+    items = dw_dealt + more;
+  }
+
+  // ---- the tile in hand -----------------------------------------------------------------------------------
+  int e = 0, row0 = 0, row_end = 0, n0 = 0, nk = 0, k_all = 0, which = 0;   // DW: row0, row_end are rows of the output
+  const unsigned char* abase = nullptr;
+  const unsigned char* bbase = nullptr;
+  int64_t lda = 0, ldb = 0;
+  uint32_t aoff[APW], boff[BPW];
+  // Place of this lane's 16 bytes of copy i: row and first column (along k: of the k-tile's row; across: of the tile).
+  auto a_row = [&](int i) {                      // along k: LDS row = tile row that copy i begins with
+    constexpr int HP = APW / 2, HALF = TM / 2;
+    const int q = (wave * HP + i % HP) * 8;
+    return (q / HALF) * TM + (i / HP) * HALF + q % HALF;
+  };
+  auto a_k = [&](int i) { return ((wave * (APW / 2) + i % (APW / 2)) * 1024) / A_ROWB + lane / (A_ROWB / 16); };   // across
+  auto b_k = [&](int i) { return ((wave * BPW + i) * 1024) / B_ROWB + lane / (B_ROWB / 16); };
+  auto setup = [&](int item) {
+    const GatedJob* jb = &p.j[0];
+    if constexpr (MODE == G_DW) {
+      int t = item < dw_dealt ? ((item / RR) * 8 + xcd) * RR + item % RR : 8 * dw_dealt + xcd * dw_share + item - dw_dealt;
+      which = t >= p.j[0].tiles ? 1 : 0;
+      if (which) { t -= p.j[0].tiles; jb = &p.j[1]; }
+      const int per = jb->mt * jb->nt;
+      e = t / per;
+      int m;
+      sched.nt = jb->nt;
+      sched.raster(t - e * per, jb->mt, m, n0);
+      row0 = m * BM;
+      row_end = jb->M;
+      const int s = p.offsets[e];
+      k_all = p.offsets[e + 1] - s;
+      abase = jb->A + static_cast<int64_t>(s) * jb->lda * EB;
+      bbase = jb->B + static_cast<int64_t>(s) * jb->ldb * EB;
+    } else {
+      int l, part;
+      sched.item(item, l, part);
+      sched.locate(l, e, row0, row_end, n0);
+      k_all = jb->Kd;
+      abase = jb->A + static_cast<int64_t>(row0) * jb->lda * EB;
+      bbase = jb->B + static_cast<int64_t>(e) * (MODE == G_GATE ? 2 * jb->N : MODE == G_DOWN ? jb->N : jb->Kd) * jb->ldb * EB;
+    }
+    nk = (k_all + BK - 1) / BK;
+    lda = jb->lda;
+    ldb = jb->ldb;
+#pragma unroll
+    for (int i = 0; i < APW; ++i) {
+      if constexpr (A_ACROSS) {
+        const int k = a_k(i), c = (lane % (A_ROWB / 16)) ^ (across_swz<F32, A_ROWB>(k) * (16 / VE));
+        const int lc = c * VE, col = row0 + (lc / (TM / 2)) * TM + (i / (APW / 2)) * (TM / 2) + lc % (TM / 2);
+        aoff[i] = col < row_end ? static_cast<uint32_t>((static_cast<int64_t>(k) * lda + col) * EB) : BUFFER_NOWHERE;
+      } else {
+        const int r = a_row(i) + lane / 8, kc = (lane % 8) ^ swz<8>(r);
+        aoff[i] = row0 + r < row_end ? static_cast<uint32_t>(static_cast<int64_t>(r) * lda * EB + kc * 16) : BUFFER_NOWHERE;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < BPW; ++i) {
+      if constexpr (B_ACROSS) {
+        const int k = b_k(i), c = (lane % (B_ROWB / 16)) ^ (across_swz<F32, B_ROWB>(k) * (16 / VE));
+        const int col = n0 + c * VE;
+        boff[i] = col < jb->N ? static_cast<uint32_t>((static_cast<int64_t>(k) * ldb + col) * EB) : BUFFER_NOWHERE;
+      } else {
+        const int r = (wave * BPW + i) * 8 + lane / 8, kc = (lane % 8) ^ swz<8>(r);
+        int n = n0 + r, row = n;
+        if constexpr (MODE == G_GATE) {            // 64 columns of a wave: 32 of g, and the same 32 of u
+          const int in = r % TN;
+          n = n0 + (r / TN) * (TN / 2) + in % (TN / 2);
+          row = n + (in / (TN / 2)) * jb->N;
+        }
+        boff[i] = n < jb->N ? static_cast<uint32_t>(static_cast<int64_t>(row - n0) * ldb * EB + kc * 16) : BUFFER_NOWHERE;
+      }
+    }
+    if constexpr (!B_ACROSS) bbase += static_cast<int64_t>(n0) * ldb * EB;
+  };
+  // k of this lane's 16 bytes inside the k-tile
+  auto in_k = [&](int kt, int k) { return kt * BK + k < k_all; };
+  auto issue_a = [&](int kt, int stage, auto half_c) {
+    constexpr int h = decltype(half_c)::value;
+    const bool tail = (kt + 1) * BK > k_all;
+#pragma unroll
+    for (int i = h * (APW / 2); i < (h + 1) * (APW / 2); ++i) {
+      uint32_t off = aoff[i];
+      if constexpr (A_ACROSS) {
+        if (tail && !in_k(kt, a_k(i))) off = BUFFER_NOWHERE;
+        // (the columns of the waves' first halves, then of their second halves: each BK rows of A_ROWB bytes)
+        buffer_to_lds16(abase + static_cast<int64_t>(kt) * BK * lda * EB, smem + stage * STAGE + h * (A_BYTES / 2) + (wave * (APW / 2) + i % (APW / 2)) * 1024, off, 0);
+      } else {
+        const int r = a_row(i) + lane / 8;
+        if (tail && !in_k(kt, ((lane % 8) ^ swz<8>(r)) * VE)) off = BUFFER_NOWHERE;
+        buffer_to_lds16(abase, smem + stage * STAGE + a_row(i) * 128, off, static_cast<uint32_t>(kt) * 128);
+      }
+    }
+  };
+  auto issue_b = [&](int kt, int stage) {
+    const bool tail = (kt + 1) * BK > k_all;
+    unsigned char* const sb = smem + stage * STAGE + A_BYTES + wave * BPW * 1024;
+#pragma unroll
+    for (int i = 0; i < BPW; ++i) {
+      uint32_t off = boff[i];
+      if constexpr (B_ACROSS) {
+        if (tail && !in_k(kt, b_k(i))) off = BUFFER_NOWHERE;
+        buffer_to_lds16(bbase + static_cast<int64_t>(kt) * BK * ldb * EB, sb + i * 1024, off, 0);
+      } else {
+        const int r = (wave * BPW + i) * 8 + lane / 8;
+        if (tail && !in_k(kt, ((lane % 8) ^ swz<8>(r)) * VE)) off = BUFFER_NOWHERE;
+        buffer_to_lds16(bbase, sb + i * 1024, off, static_cast<uint32_t>(kt) * 128);
+      }
+    }
+  };
+  auto issue_ba0 = [&](int kt, int stage) {
+    issue_b(kt, stage);
+    issue_a(kt, stage, std::integral_constant<int, 0>{});
+  };
+  auto issue_a1 = [&](int kt, int stage) { issue_a(kt, stage, std::integral_constant<int, 1>{}); };
+  auto issue_prologue = [&]() {
+#pragma unroll
+    for (int t = 0; t < NS; ++t)
+      if (t < nk) {
+        issue_ba0(t, t);
+        issue_a1(t, t);
+      }
+  };
+  auto wait_vm = [&](auto n_c) {
+    constexpr int n = decltype(n_c)::value;
+    static_assert(n < 64, "vmcnt field");
+    __builtin_amdgcn_s_waitcnt((n & 15) | ((n >> 4) << 14) | 0x0F70);
+  };
+  auto wait_tiles = [&](int tiles, auto extra_c) {      // at most so many k-tiles, and `extra` copies, still in flight
+    constexpr int x = decltype(extra_c)::value;
+    if (NS > 2 && tiles >= 2) wait_vm(std::integral_constant<int, 2 * LPW + x < 63 ? 2 * LPW + x : 63>{});
+    else if (tiles >= 1) wait_vm(std::integral_constant<int, LPW + x>{});
+    else wait_vm(std::integral_constant<int, x>{});
+  };
+
+  // ---- fragments -----------------------------------------------------------------------------------------
+  unsigned lds0 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(SCMOE_LDS_PTR(smem)));
+  asm volatile("" : "+s"(lds0));
+  constexpr int UNITB = 16 * EB;                          // bytes of 16 columns
+  // Along k: address of (row l16, chunk of step s), the row block an immediate.  Across k: of this lane's first row of the step, the unit
+  // (16 columns) swizzled per subtile: the swizzle of a lane's rows is the same throughout.
+  const int kin = F32 ? lq * 4 : lq * 8 + (l16 >> 2);
+  const unsigned in_unit = F32 ? l16 * 4 : (l16 & 3) * 8;
+  unsigned xa[A_ACROSS ? H : KS], wb[B_ACROSS ? NJ : KS];
+  if constexpr (A_ACROSS) {
+#pragma unroll
+    for (int i = 0; i < H; ++i) xa[i] = lds0 + kin * A_ROWB + (((wave_m * (TM / 2) / 16 + i) ^ across_swz<F32, A_ROWB>(kin)) * UNITB) + in_unit;
+  } else {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) xa[s] = lds0 + (wave_m * TM + l16) * 128 + (((s * 4 + lq) ^ swz<8>(l16)) << 4);
+  }
+  if constexpr (B_ACROSS) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) wb[j] = lds0 + A_BYTES + kin * B_ROWB + (((wave_n * TN / 16 + j) ^ across_swz<F32, B_ROWB>(kin)) * UNITB) + in_unit;
+  } else {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) wb[s] = lds0 + A_BYTES + (wave_n * TN + l16) * 128 + (((s * 4 + lq) ^ swz<8>(l16)) << 4);
+  }
+  typedef const __attribute__((address_space(3))) g_u32x4* lds16_ptr;
+  typedef const __attribute__((address_space(3))) uint32_t* lds4_ptr;
+  auto read_along = [&](unsigned at) { return *reinterpret_cast<lds16_ptr>(static_cast<uintptr_t>(at)); };
+  auto read_across = [&](unsigned at, auto rowb_c) {
+    constexpr int rowb = decltype(rowb_c)::value;
+    g_u32x4 v;
+    if constexpr (F32) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] = *reinterpret_cast<lds4_ptr>(static_cast<uintptr_t>(at + c * rowb));
+    } else {
+      const g_u32x2 lo = lds_read_transposed(at), hi = lds_read_transposed(at + 4 * rowb);
+      v = g_u32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
+    return v;
+  };
+  constexpr int KROWS = BK / KS;                          // rows of k in a step
+  f32x4_t acc[MI][NJ];
+  g_u32x4 wf[2][NJ], xf[2][H];
+  static_assert((NS * KS) % 2 == 0, "the weight-fragment buffers alternate over the unrolled k loop");
+  auto load_frags = [&](int R, int hs) {                  // half-step hs: step hs % KS, row-subtile half hs / KS
+    const int s = hs % KS, half = hs / KS, st = R * STAGE, wbuf = (R * KS + s) & 1, xbuf = hs & 1;
+#pragma unroll
+    for (int t = 0; t < (H > NJ ? H : NJ); ++t) {
+      if (half == 0 && t < NJ) {
+        if constexpr (B_ACROSS) wf[wbuf][t] = read_across(wb[t] + st + s * KROWS * B_ROWB, std::integral_constant<int, B_ROWB>{});
+        else wf[wbuf][t] = read_along(wb[s] + st + t * 16 * 128);
+      }
+      if (t < H) {
+        if constexpr (A_ACROSS) xf[xbuf][t] = read_across(xa[t] + st + half * (A_BYTES / 2) + s * KROWS * A_ROWB, std::integral_constant<int, A_ROWB>{});
+        else xf[xbuf][t] = read_along(xa[s] + st + (half * H + t) * 16 * 128);
+      }
+    }
+  };
+  auto mfma_step = [&](int R, int hs) {
+    const int s = hs % KS, half = hs / KS, wbuf = (R * KS + s) & 1, xbuf = hs & 1;
+#pragma unroll
+    for (int c = 0; c < (F32 ? 4 : 1); ++c)
+#pragma unroll
+      for (int i = 0; i < H; ++i)
+#pragma unroll
+        for (int jj = 0; jj < NJ; ++jj) {
+          const int j = (i & 1) ? NJ - 1 - jj : jj;       // there and back: one operand changes at a time
+          f32x4_t& a = acc[half * H + i][j];
+          if constexpr (F32) a = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(wf[wbuf][j][c]), __uint_as_float(xf[xbuf][i][c]), a, 0, 0, 0);
+          else a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, wf[wbuf][j]), __builtin_bit_cast(bf16x8_t, xf[xbuf][i]), a, 0, 0, 0);
+        }
+  };
+  // issue order of a half-step: a matrix instruction, then reads for the next half-step
+  auto interleave = [&](auto next_hs_c) {
+    constexpr int RA = A_ACROSS ? (F32 ? 4 : 2) : 1, RB = B_ACROSS ? (F32 ? 4 : 2) : 1;
+    constexpr int reads = H * RA + (decltype(next_hs_c)::value / KS ? 0 : NJ * RB);
+    constexpr int mfmas = H * NJ * (F32 ? 4 : 1), per = (reads + mfmas - 1) / mfmas, groups = reads / per;
+#pragma unroll
+    for (int q = 0; q < groups; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, per, 0);
+    }
+    if constexpr (reads % per != 0) __builtin_amdgcn_sched_group_barrier(0x100, reads % per, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, mfmas - groups, 0);
+  };
+
+  if (it >= items) return;
+  setup(it);
+  issue_prologue();
+  for (;;) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    wait_vm(std::integral_constant<int, 0>{});
+    lds_barrier();
+    constexpr int HS = 2 * KS;
+    using X0 = std::integral_constant<int, 0>;
+    using XA1 = std::integral_constant<int, APW / 2>;
+    // One k-tile (the order of its half-steps, copies and barriers is gemm_bf16_kernel's): W and the first halves of the rows are
+    // refilled with k-tile kt + NS while the second halves are multiplied, these behind a second barrier.
+    auto k_tile = [&](auto stage_c, auto steady_c, int kt) {
+      constexpr int stage = decltype(stage_c)::value;
+      constexpr bool steady = decltype(steady_c)::value;
+      constexpr int next = stage + 1 == NS ? 0 : stage + 1;
+      static_for<0, HS>([&](auto hs_c) {
+        constexpr int hs = decltype(hs_c)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (hs == KS - 1) {
+          if constexpr (steady) wait_tiles(NS - 1, X0{});
+          else wait_tiles(nk - 1 - kt < NS - 1 ? nk - 1 - kt : NS - 1, X0{});
+          lds_barrier();
+          if (steady || kt + NS < nk) issue_ba0(kt + NS, stage);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (hs == HS - 1) {
+          if (steady || kt + 1 < nk) {
+            if (steady || kt + NS < nk) wait_tiles(NS - 1, X0{});
+            else wait_tiles(nk - 2 - kt, XA1{});
+            lds_barrier();
+            if (steady || kt + NS < nk) issue_a1(kt + NS, stage);
+            __builtin_amdgcn_sched_barrier(0);
+            load_frags(next, 0);
+          }
+          mfma_step(stage, hs);
+          if constexpr (steady) interleave(std::integral_constant<int, 0>{});
+        } else {
+          load_frags(stage, hs + 1);
+          mfma_step(stage, hs);
+          interleave(std::integral_constant<int, hs + 1>{});
+        }
+      });
+    };
+    using std::bool_constant;
+    using std::integral_constant;
+    if (nk > 0) {
+      load_frags(0, 0);
+      int kt = 0;
+      for (; kt + 2 * NS <= nk; kt += NS) static_for<0, NS>([&](auto s) { k_tile(s, bool_constant<true>{}, kt + decltype(s)::value); });
+      for (; kt < nk; kt += NS)
+        static_for<0, NS>([&](auto s) {
+          if (kt + decltype(s)::value < nk) k_tile(s, bool_constant<false>{}, kt + decltype(s)::value);
+        });
+    }
+    lds_barrier();                                  // every wave holds its last fragments: LDS is free
+
+    const GatedJob& jc = p.j[MODE == G_DW ? which : 0];
+    const int ce = e, crow0 = row0, crow_end = row_end, cn0 = n0;
+    unsigned char* const cC = jc.C;
+    const int64_t cldc = jc.ldc;
+    const int cN = jc.N;
+    const int itn = MODE == G_DW ? it + nslots : sched.next(it);
+    const bool more = itn < items;
+    if (more) {
+      setup(itn);
+      issue_prologue();
+    }
+
+    // ---- store: acc[i][j][q] is row l16 of subtile i, column 4 lq + q of subtile j -----------------------------
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int r = crow0 + wave_m * TM + i * 16 + l16;
+      const bool in = r < crow_end;
+      if constexpr (MODE == G_GATE) {
+        constexpr int J2 = NJ / 2;
+        static_assert(J2 * 16 == CKPT_BLOCK, "a wave has one block of g and of u");
+        const int f0 = cn0 + wave_n * (TN / 2);
+#pragma unroll
+        for (int j = 0; j < J2; ++j) {
+          const int f = f0 + j * 16 + 4 * lq;
+          float h[4], g[4], u[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            g[q] = acc[i][j][q];
+            u[q] = acc[i][J2 + j][q];
+            h[q] = gated_act<F32>(g[q], p.act) * u[q];
+          }
+          if (in && f < cN) {
+            store4<F32>(cC + (static_cast<int64_t>(r) * cldc + f) * EB, h);
+            if constexpr (KEEP == KEEP_FULL) {
+              store4<F32>(p.pre + (static_cast<int64_t>(r) * p.ldpre + f) * EB, g);
+              store4<F32>(p.pre + (static_cast<int64_t>(r) * p.ldpre + cN + f) * EB, u);
+            }
+          }
+        }
+        if constexpr (KEEP == KEEP_8BIT) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int j = 0; j < J2; ++j)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) most = max(most, magnitude(acc[i][t * J2 + j][q]));
+            most = max_over_lq(most);
+            const uint32_t byte = ckpt_scale_byte(most);
+            const float inv = ckpt_inverse(byte);
+            unsigned char* const row = p.pre + (2 * static_cast<int64_t>(r) + t) * p.ldpre;
+#pragma unroll
+            for (int j = 0; j < J2; ++j) {
+              const int f = f0 + j * 16 + 4 * lq;
+              const f32x4_t& a = acc[i][t * J2 + j];
+              if (in && f < cN) *reinterpret_cast<uint32_t*>(row + f) = ckpt_encode4(a[0], a[1], a[2], a[3], inv);
+            }
+            if (in && lq == 0 && f0 < cN) row[cN + f0 / CKPT_BLOCK] = static_cast<unsigned char>(byte);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const int n = cn0 + wave_n * TN + j * 16 + 4 * lq;
+          float v[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[q] = acc[i][j][q];
+          if (!in || n >= cN) continue;
+          if constexpr (MODE == G_DH) {
+            float g[4], u[4], h[4], dg[4], du[4];
+            if constexpr (KEEP == KEEP_8BIT) {
+              const unsigned char* row = p.pre + 2 * static_cast<int64_t>(r) * p.ldpre;
+              ckpt_decode4(*reinterpret_cast<const uint32_t*>(row + n), ckpt_scale(row[cN + n / CKPT_BLOCK]), g);
+              row += p.ldpre;
+              ckpt_decode4(*reinterpret_cast<const uint32_t*>(row + n), ckpt_scale(row[cN + n / CKPT_BLOCK]), u);
+            } else {
+              load4<F32>(p.pre + (static_cast<int64_t>(r) * p.ldpre + n) * EB, g);
+              load4<F32>(p.pre + (static_cast<int64_t>(r) * p.ldpre + cN + n) * EB, u);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float a, s;
+              gated_act_slope<F32>(g[q], p.act, a, s);
+              h[q] = a * u[q];
+              du[q] = v[q] * a;
+              dg[q] = v[q] * u[q] * s;
+            }
+            store4<F32>(cC + (static_cast<int64_t>(r) * cldc + n) * EB, h);
+            store4<F32>(p.dpre + (static_cast<int64_t>(r) * p.lddpre + n) * EB, dg);
+            store4<F32>(p.dpre + (static_cast<int64_t>(r) * p.lddpre + cN + n) * EB, du);
+          } else {
+            const int64_t at = MODE == G_DW ? (static_cast<int64_t>(ce) * jc.M + r) * cldc + n : static_cast<int64_t>(r) * cldc + n;
+            store4<F32>(cC + at * EB, v);
+          }
+        }
+      }
+    }
+    it = itn;
+    if (!more) break;
+  }
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------
+
+template <class CFG, int MODE, int KEEP>
+static int launch_gated_cfg(GatedArgs a, int64_t max_rows, hipStream_t stream) {
+  static std::atomic<bool> attr_set[64];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = -1;
+  if (dev < 0 || !attr_set[dev].load(std::memory_order_acquire)) {
+    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(&gated_kernel<CFG, MODE, KEEP>), hipFuncAttributeMaxDynamicSharedMemorySize, CFG::LDS);
+    if (err != hipSuccess) return hip_fail(err);
+    if (dev >= 0) attr_set[dev].store(true, std::memory_order_release);
+  }
+  constexpr int BNF = MODE == G_GATE ? CFG::BN / 2 : CFG::BN;
+  int64_t tiles = 0;
+  for (GatedJob& j : a.j) {
+    if (j.C == nullptr) continue;                       // (no second product)
+    j.nt = (j.N + BNF - 1) / BNF;
+    if (MODE == G_DW) {
+      j.mt = (j.M + CFG::BM - 1) / CFG::BM;
+      j.tiles = a.E * j.mt * j.nt;                       // (check_gated: they fit)
+      tiles += j.tiles;
+    } else {
+      // sum_e ceil(c_e / BM) is at most rows / BM and one more for every segment that can hold a row
+      tiles += (max_rows / CFG::BM + (a.E < max_rows ? a.E : max_rows)) * j.nt;
+    }
+  }
+  int64_t slots = (tiles + 7) / 8;
+  const int resident = (num_cus() / 8) * CFG::WG_PER_CU;
+  if (slots > resident) slots = resident;
+  if (slots < 1) slots = 1;
+  hipLaunchKernelGGL((gated_kernel<CFG, MODE, KEEP>), dim3(static_cast<unsigned>(8 * slots)), dim3(CFG::THREADS), CFG::LDS, stream, a);
+  return launch_status();
+}
+
+// One launch of a product (DW: of one or two), of either type.
+int launch_gated_bf16(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream);
+int launch_gated_f32(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream);
+
+template <class CFG>
+static int launch_gated_mode(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream) {
+  switch (mode) {
+    case G_GATE:
+      return keep == KEEP_NONE ? launch_gated_cfg<CFG, G_GATE, KEEP_NONE>(a, max_rows, stream)
+             : keep == KEEP_FULL ? launch_gated_cfg<CFG, G_GATE, KEEP_FULL>(a, max_rows, stream)
+                                 : launch_gated_cfg<CFG, G_GATE, KEEP_8BIT>(a, max_rows, stream);
+    case G_DH:
+      return keep == KEEP_FULL ? launch_gated_cfg<CFG, G_DH, KEEP_FULL>(a, max_rows, stream) : launch_gated_cfg<CFG, G_DH, KEEP_8BIT>(a, max_rows, stream);
+    case G_DOWN: return launch_gated_cfg<CFG, G_DOWN, KEEP_NONE>(a, max_rows, stream);
+    case G_DX: return launch_gated_cfg<CFG, G_DX, KEEP_NONE>(a, max_rows, stream);
+    default: return launch_gated_cfg<CFG, G_DW, KEEP_NONE>(a, max_rows, stream);
+  }
+}
+
+}  // namespace scmoe

@@ -1,0 +1,548 @@
+"""The gated feed-forward block, its gradient and the activation checkpoints against the same formulas in 64 bits.
+
+Tolerances count roundings, element by element, as bounds that are carried through the formulas in 64 bits: H = 2^-24 for every fp32
+operation; a sum of n products is off by at most n H times the sum of their magnitudes, in any order; a value stored in bf16 by 2^-8 of
+itself.  The activation and its slope: 8 operations, and e^x of an x that is off by H |x| in itself; in bf16 the distribution function
+comes from a polynomial that is off by up to 2^-16 (what tests/test_gelu_error.py finds on the host, 4.7e-5 at 4.24, is 1.1e-5 times
+that argument), and the other two from the hardware's exponential and reciprocal, one more H each."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+if torch.cuda.is_available():
+    from paper_2404_05019_amd import binding as B
+    from gpu_util import DEV
+
+H = 2.0 ** -24
+NAN = float("nan")
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+STORE = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+ACTS = ["silu", "gelu", "gelu_tanh"]
+
+
+def mode(act):
+    return {"silu": B.SILU, "gelu": B.GELU_ERF, "gelu_tanh": B.GELU_TANH}[act]
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def normal(g, *shape, scale=1.0, dtype="f32"):
+    return (torch.randn(shape, generator=g, device=DEV) * scale).to(TYPES[dtype])
+
+
+def padded(t, pad=8, fill=NAN):
+    """The same values in rows `pad` elements longer, with `fill` between them."""
+    store = torch.full((*t.shape[:-1], t.shape[-1] + pad), fill, dtype=t.dtype, device=t.device)
+    store[..., :t.shape[-1]] = t
+    return store[..., :t.shape[-1]]
+
+
+def close(got, want, slack, dtype="f32"):
+    """|got - want| <= one rounding to the type of what is rounded + slack, everywhere; non-finite values the same."""
+    got, want = got.double(), want.double()
+    off = (got - want).abs()
+    most = STORE[dtype] * (want.abs() + slack) + slack + 1e-38
+    same = (got == want) | (got.isnan() & want.isnan())
+    ok = same | (off <= most)
+    assert bool(ok.all()), "%d of %d differ; worst %.3g times the bound" % (int((~ok).sum()), ok.numel(), float((off / most)[~ok].nan_to_num(1e9).max()))
+
+
+# ---- the formulas in 64 bits, and how far 32 bits may be off ------------------------------------------
+
+
+def act64(g, act):
+    """Activation, slope, and bounds of their errors as functions of an exact argument, in units of 1 (fp32 library) and of the fast forms."""
+    if act == "silu":
+        p = torch.sigmoid(g)
+        return g * p, p * (1 + g * (1 - p))
+    if act == "gelu":
+        p = torch.special.ndtr(g)
+        return g * p, p + g * torch.exp(-0.5 * g * g) / math.sqrt(2 * math.pi)
+    c, b = 2 * math.sqrt(2 / math.pi), 0.044715
+    p = torch.sigmoid(c * (g + b * g ** 3))
+    return g * p, p + g * p * (1 - p) * c * (1 + 3 * b * g * g)
+
+
+def act_errors(g, act, dtype):
+    """Bounds on the error of activation and slope for an exact argument.  The exponent t of e^t is made of up to four operations and is off
+    by 4 H |t|, which moves p = 1 / (1 + e^-t) by p (1 - p) 4 H |t|; p itself and the products: 8 H of each term."""
+    t = {"silu": g.abs(), "gelu": 0.5 * g * g, "gelu_tanh": 1.6 * (g.abs() + 0.045 * g.abs() ** 3)}[act]
+    if act == "gelu":
+        dp = 8 * H if dtype == "f32" else 2.0 ** -16
+        phi = torch.exp(-0.5 * g * g) / math.sqrt(2 * math.pi)
+        return g.abs() * dp, dp + 8 * H * g.abs() + (8 + 4 * t) * H * g.abs() * phi
+    p = torch.sigmoid(t)
+    pq = p * (1 - p)
+    dp = 8 * H + 4 * H * t * pq
+    inner = torch.ones_like(g) if act == "silu" else 1.6 * (1 + 0.135 * g * g)
+    return g.abs() * dp, dp + g.abs() * inner * (2 * dp * 1.0 + 8 * H)
+
+
+def forward64(x, W1, W2, act, dtype):
+    """y, pre, h and the bounds on each of one segment."""
+    F, d = W2.shape[1], W2.shape[0]
+    x, W1, W2 = x.double(), W1.double(), W2.double()
+    pre = x @ W1.t()
+    dpre = d * H * (x.abs() @ W1.abs().t())
+    g, u, dg, du = pre[:, :F], pre[:, F:], dpre[:, :F], dpre[:, F:]
+    a, _ = act64(g, act)
+    ea, _ = act_errors(g, act, dtype)
+    h = a * u
+    dh = (1.13 * dg + ea) * (u.abs() + du) + a.abs() * du + 2 * H * h.abs()
+    dh = dh + STORE[dtype] * (h.abs() + dh)
+    y = h @ W2.t()
+    dy = dh @ W2.abs().t() + F * H * (h.abs() @ W2.abs().t())
+    return y, pre, h, dy, dpre
+
+
+def backward64(dy, x, pre, W1, W2, act, dtype):
+    """dx, dW1, dW2 of one segment from exact dy, x and pre, and the bounds on each."""
+    F, d, n = W2.shape[1], W2.shape[0], dy.shape[0]
+    dy, x, pre, W1, W2 = (t.double() for t in (dy, x, pre, W1, W2))
+    g, u = pre[:, :F], pre[:, F:]
+    a, s = act64(g, act)
+    ea, es = act_errors(g, act, dtype)
+    dh = dy @ W2
+    e = d * H * (dy.abs() @ W2.abs())
+    h, both = a * u, torch.cat([dh * u * s, dh * a], 1)
+    eh = ea * u.abs() + 2 * H * h.abs()
+    eb = torch.cat([u.abs() * (e * s.abs() + (dh.abs() + e) * es), e * a.abs() + (dh.abs() + e) * ea], 1) + 4 * H * both.abs()
+    eh, eb = eh + STORE[dtype] * (h.abs() + eh), eb + STORE[dtype] * (both.abs() + eb)
+    dx, dW1, dW2 = both @ W1, both.t() @ x, dy.t() @ h
+    ex = eb @ W1.abs() + 2 * F * H * ((both.abs() + eb) @ W1.abs())
+    e1 = eb.t() @ x.abs() + n * H * ((both.abs() + eb).t() @ x.abs())
+    e2 = dy.abs().t() @ eh + n * H * (dy.abs().t() @ (h.abs() + eh))
+    return dx, dW1, dW2, ex, e1, e2
+
+
+def offsets_of(counts):
+    return torch.tensor([0] + list(torch.tensor(counts).cumsum(0)), dtype=torch.int32, device=DEV)
+
+
+class Block:
+    """Weights, rows and buffers of a call, with gaps full of NaN and `spare` rows behind the last segment."""
+
+    def __init__(self, counts, d, F, dtype, act, spare=3, pad=8, seed=0):
+        g = gen(seed + d + F)
+        self.counts, self.d, self.F, self.dtype, self.act, self.E = counts, d, F, dtype, act, len(counts)
+        self.K = sum(counts)
+        self.rows = self.K + spare
+        tt = TYPES[dtype]
+        self.offsets = offsets_of(counts)
+        self.x, self.dy = normal(g, self.rows, d, dtype=dtype), normal(g, self.rows, d, dtype=dtype)
+        self.x[self.K:], self.dy[self.K:] = NAN, NAN
+        self.x, self.dy = padded(self.x, pad), padded(self.dy, 2 * pad)
+        self.W1 = padded(normal(g, self.E, 2 * F, d, scale=d ** -0.5, dtype=dtype), pad)
+        self.W2 = padded(normal(g, self.E, d, F, scale=F ** -0.5, dtype=dtype), 3 * pad)
+        buf = lambda n, w, p: torch.full((n, w + p), NAN, dtype=tt, device=DEV)[:, :w]  # noqa: E731
+        self.hidden, self.y, self.dx = buf(self.rows, F, pad), buf(self.rows, d, pad), buf(self.rows, d, 2 * pad)
+        self.pre = buf(self.rows, 2 * F, pad)
+        self.pre8 = torch.full((2 * self.rows, B.scmoe_checkpoint_ld(F) + 16), 0x5A, dtype=torch.uint8, device=DEV)
+        self.x8 = torch.full((self.rows, B.scmoe_checkpoint_ld(d) + 32), 0xA5, dtype=torch.uint8, device=DEV)
+        self.dW1 = torch.full((self.E, 2 * F, d), NAN, dtype=tt, device=DEV)
+        self.dW2 = torch.full((self.E, d, F), NAN, dtype=tt, device=DEV)
+        code = B.dtype_code(self.x)
+        need = max(16, B.scmoe_gated_ffn_workspace_bytes(code, d, F), B.scmoe_gated_ffn_backward_workspace_bytes(code, self.rows, self.E, d, F))
+        self.guarded = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device=DEV)     # (NaN in either type)
+        self.workspace = self.guarded[:need]
+
+    def segments(self):
+        at = 0
+        for e, c in enumerate(self.counts):
+            yield e, slice(at, at + c)
+            at += c
+
+    def forward(self, pre=None, **kw):
+        B.scmoe_gated_ffn(self.x, self.offsets, self.rows, self.W1, self.W2, self.hidden, self.y, mode(self.act), pre=pre, workspace=self.workspace, **kw)
+
+    def backward(self, x, pre, **kw):
+        args = dict(dx_perm=self.dx, dW1=self.dW1, dW2=self.dW2)
+        args.update(kw)
+        B.scmoe_gated_ffn_backward(self.dy, x, pre, self.offsets, self.rows, self.W1, self.W2, mode(self.act), workspace=self.workspace, **args)
+
+    def guard(self):
+        assert bool((self.guarded[self.workspace.numel():] == 0xFF).all()), "written behind the workspace"
+
+    def untouched(self, t, rows=None, byte=None):
+        """Rows behind the last segment and the gaps between rows are as they were."""
+        rows = self.K if rows is None else rows
+        whole = torch.empty(0, dtype=t.dtype, device=DEV).set_(t.untyped_storage()).reshape(t.shape[0], t.stride(0))
+        same = (lambda v: bool(v.isnan().all())) if byte is None else (lambda v: bool((v == byte).all()))
+        assert same(whole[rows:]) and same(whole[:, t.shape[1]:])
+
+
+def check_forward(b, keep="full"):
+    for e, at in b.segments():
+        if at.stop == at.start:
+            continue
+        y, pre, h, sy, spre = forward64(b.x[at], b.W1[e], b.W2[e], b.act, b.dtype)
+        close(b.y[at], y, sy, b.dtype)
+        if keep == "full":
+            close(b.pre[at], pre, spre, b.dtype)
+    b.untouched(b.y)
+
+
+def check_backward(b, x, pre, which=("dx", "dW1", "dW2")):
+    b.guard()
+    for e, at in b.segments():
+        if at.stop == at.start:
+            assert all(bool((w[e] == 0).all()) for w, n in ((b.dW1, "dW1"), (b.dW2, "dW2")) if n in which)
+            continue
+        dx, dW1, dW2, ex, e1, e2 = backward64(b.dy[at], x[at], pre[at], b.W1[e], b.W2[e], b.act, b.dtype)
+        if "dx" in which:
+            close(b.dx[at], dx, ex, b.dtype)
+        if "dW1" in which:
+            close(b.dW1[e], dW1, e1, b.dtype)
+        if "dW2" in which:
+            close(b.dW2[e], dW2, e2, b.dtype)
+    if "dx" in which:
+        b.untouched(b.dx)
+
+
+# (rows of the segments, model width, hidden width): one row; empty segments first, last and between; rows and widths on both sides of every
+# tile edge, and down to the least width
+SHAPES = [([1], 8, 8), ([1, 0, 0, 1], 64, 96), ([0, 0], 64, 64), ([0, 5, 0, 130, 1, 0], 72, 136), ([127, 1, 128, 129], 128, 64), ([64, 63], 264, 40),
+          ([33, 260], 200, 1000), ([300], 512, 256), ([3, 2, 1, 0, 7, 16, 17, 31], 1000, 344), ([257, 513], 192, 328)]
+SMALL = [([1], 8, 8), ([0, 5, 0, 130, 1, 0], 72, 136), ([33, 260], 200, 1000), ([127, 1, 128, 129], 128, 64)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts,d,F", SHAPES)
+def test_forward(counts, d, F, dtype):
+    b = Block(counts, d, F, dtype, "silu")
+    b.forward(pre=b.pre)
+    check_forward(b)
+    b.untouched(b.pre)
+    y = b.y.clone()
+    b.y.fill_(NAN)
+    b.forward()                                     # nothing kept: the same
+    assert torch.equal(b.y[:b.K], y[:b.K])
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts,d,F", SMALL)
+def test_forward_activations(counts, d, F, dtype, act):
+    b = Block(counts, d, F, dtype, act, seed=5)
+    b.x[:b.K] *= 3
+    b.forward(pre=b.pre)
+    check_forward(b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts,d,F", SHAPES)
+def test_backward(counts, d, F, dtype):
+    b = Block(counts, d, F, dtype, "silu", seed=1)
+    b.forward(pre=b.pre)
+    b.backward(b.x, b.pre)
+    check_backward(b, b.x, b.pre)
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts,d,F", SMALL)
+def test_backward_activations(counts, d, F, dtype, act):
+    b = Block(counts, d, F, dtype, act, seed=2)
+    b.x[:b.K] *= 3
+    b.forward(pre=b.pre)
+    b.backward(b.x, b.pre)
+    check_backward(b, b.x, b.pre)
+
+
+# ---- checkpoints ------------------------------------------------------------------------------------
+
+
+def pack64(x):
+    """Codes' values and scales' bytes from the definition, in 64 bits on the host."""
+    x = x.double().cpu()
+    n, w = x.shape
+    blocks = torch.nn.functional.pad(x, (0, -w % 32)).reshape(n, -1, 32)
+    top = blocks.abs().amax(2, keepdim=True)
+    bad = ~torch.isfinite(blocks).all(2, keepdim=True)
+    top = torch.where(bad, torch.ones_like(top), top)
+    exponent = torch.full_like(top, -126.0)
+    for k in range(-125, 128):
+        exponent = torch.where(top > 448.0 * 2.0 ** (k - 1), torch.full_like(top, float(k)), exponent)
+    s = torch.exp2(exponent)
+    z = blocks / s
+    step = torch.exp2(torch.floor(torch.log2(z.abs().clamp(min=2.0 ** -6))) - 3)
+    v = torch.where(bad, torch.full_like(z, NAN), torch.round(z / step) * step * s)
+    return v.reshape(n, -1)[:, :w], torch.where(bad, torch.full_like(exponent, 128.0), exponent)[:, :, 0] + 127
+
+
+def ckpt(x, extra=0, n_rows=None):
+    q = torch.full((x.shape[0], B.scmoe_checkpoint_ld(x.shape[1]) + extra), 0x5A, dtype=torch.uint8, device=DEV)
+    B.scmoe_checkpoint_pack(x, q, n_rows=n_rows)
+    return q
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,w", [(1, 8), (1, 32), (3, 40), (5, 1000), (129, 264), (1, 16384), (700, 96)])
+def test_checkpoint(n, w, dtype):
+    g = gen(n + w)
+    x = padded(normal(g, n, w, dtype=dtype) * torch.exp2(torch.randint(-40, 40, (n, w), generator=g, device=DEV).float() * (torch.arange(n, device=DEV) % 2)[:, None]).to(TYPES[dtype]), 16)
+    x[0, :4] = torch.tensor([448.0, -448.0, 0.0, -0.0], device=DEV)
+    q = ckpt(x, 16)
+    want, scales = pack64(x)
+    blocks = -(-w // 32)
+    assert torch.equal(q[:, w:w + blocks].cpu().double(), scales)
+    assert bool((q[:, w + blocks:] == 0x5A).all())
+    back = torch.full((n, w + 8), NAN, dtype=TYPES[dtype], device=DEV)[:, :w]
+    B.scmoe_checkpoint_unpack(q, back)
+    assert torch.equal(back.double().cpu(), want)
+    off = (back.double() - x.double()).abs().cpu()
+    s = torch.exp2(scales - 127).repeat_interleave(32, 1)[:, :w]
+    assert bool((off <= torch.maximum(2.0 ** -4 * x.double().abs().cpu(), 2.0 ** -10 * s)).all())
+
+
+def test_checkpoint_of_borders():
+    """Blocks whose largest value lies on either side of where the scale changes, ties, zeros, the least and the largest numbers."""
+    rows = []
+    for top in (448.0, math.nextafter(448.0, 1e9), 1.75, 1.7500001, 1.7499999, 1.0, 3.4e38, 2.0 ** -126, 2.0 ** -149, 448 * 2.0 ** -126, 449 * 2.0 ** -126, 0.0):
+        r = torch.linspace(-1, 1, 32, dtype=torch.float64) * top
+        r[5:13] = torch.tensor([17, 19, 21, 23, 25, 27, 29, 31], dtype=torch.float64) / 32 * top / 2
+        rows.append(r)
+    x = torch.stack(rows).float().to(DEV)
+    q, back = ckpt(x), torch.empty_like(x)
+    B.scmoe_checkpoint_unpack(q, back)
+    want, scales = pack64(x)
+    assert torch.equal(q[:, 32].cpu().double(), scales[:, 0])
+    assert torch.equal(back.double().cpu(), want.float().double())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [NAN, float("inf"), -float("inf")])
+def test_checkpoint_of_what_is_not_finite(bad, dtype):
+    """Its block is NaN, the ones beside it are as they would be."""
+    x = normal(gen(3), 4, 104, dtype=dtype)
+    x[1, 40], x[2, 103] = bad, bad
+    want, _ = pack64(x)
+    back = torch.empty_like(x)
+    B.scmoe_checkpoint_unpack(ckpt(x), back)
+    assert bool(back[1, 32:64].isnan().all()) and bool(back[2, 96:].isnan().all()) and int(back.isnan().sum()) == 40
+    assert torch.equal(back.double().cpu().nan_to_num(7.0), want.nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [0, 1, 6, 9, 200])
+def test_checkpoint_of_some_rows(n, dtype):
+    x = normal(gen(4), 9, 72, dtype=dtype)
+    count = torch.tensor([n], dtype=torch.int32, device=DEV)
+    q = ckpt(x, n_rows=count)
+    n = min(n, 9)
+    assert bool((q[n:] == 0x5A).all()) and torch.equal(q[:n], ckpt(x)[:n])
+    back = torch.full_like(x, NAN)
+    B.scmoe_checkpoint_unpack(ckpt(x), back, n_rows=count)
+    assert bool(back[n:].isnan().all()) and not bool(back[:n].isnan().any())
+
+
+def restored(q, rows, w, dtype="f32"):
+    out = torch.empty(rows, w, dtype=TYPES[dtype], device=DEV)
+    B.scmoe_checkpoint_unpack(q, out)
+    return out
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts,d,F", SHAPES)
+def test_checkpoints_of_a_step(counts, d, F, dtype, act):
+    """The forward pass keeps what packing its exact sums would keep, up to a step of the code where a sum lies next to a border; the
+    backward pass gives the gradient at what was kept."""
+    b = Block(counts, d, F, dtype, act, seed=3)
+    b.forward(pre=b.pre8)
+    check_forward(b, keep="8bit")
+    blocks = -(-F // 32)
+    assert bool((b.pre8[2 * b.K:] == 0x5A).all()) and bool((b.pre8[:, F + blocks:] == 0x5A).all())
+    pre = restored(b.pre8[:2 * b.K], 2 * b.K, F).reshape(b.K, 2 * F) if b.K else torch.empty(0, 2 * F, device=DEV)
+    for e, at in b.segments():
+        if at.stop > at.start:
+            _, want, _, _, slack = forward64(b.x[at], b.W1[e], b.W2[e], act, dtype)
+            # half a step: 2^-4 of the value, or 2^-10 s; s is at most 2 max / 448 of the block (and at least 2^-126), its maximum off by the slack as well
+            most = torch.nn.functional.pad((want.abs() + slack).reshape(-1, F), (0, -F % 32)).reshape(want.shape[0] * 2, -1, 32).amax(2).repeat_interleave(32, 1)[:, :F]
+            small = (2.0 ** -10 * (most / 224 + 2.0 ** -126)).reshape(want.shape)
+            off = (pre[at].double() - want).abs()
+            assert bool((off <= torch.maximum(2.0 ** -4 * (want.abs() + slack), small) + slack).all())
+    B.scmoe_checkpoint_pack(b.x, b.x8, n_rows=b.offsets[-1:])
+    assert bool((b.x8[b.K:] == 0xA5).all())
+    x = restored(b.x8[:b.K], b.K, d) if b.K else torch.empty(0, d, device=DEV)
+    b.backward(b.x8, b.pre8)
+    check_backward(b, x, pre)
+    # each of the two alone in 8 bits
+    b.backward(b.x, b.pre8)
+    check_backward(b, b.x, pre)
+    b.forward(pre=b.pre)
+    b.backward(b.x8, b.pre)
+    check_backward(b, x, b.pre)
+
+
+# ---- parts of a call, values that are not finite, graphs, streams --------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("which", [("dx",), ("dW1",), ("dW2",), ("dx", "dW2"), ("dW1", "dW2")])
+def test_some_of_the_gradients(which, dtype):
+    """What is not asked for is not needed either."""
+    b = Block([5, 0, 140], 136, 72, dtype, "gelu", seed=4)
+    b.forward(pre=b.pre)
+    out = {n: getattr(b, "dx" if n == "dx" else n) for n in which}
+    b.backward(b.x if "dW1" in which else None, b.pre, **{n: out.get({"dx_perm": "dx"}.get(n, n)) for n in ("dx_perm", "dW1", "dW2")})
+    check_backward(b, b.x, b.pre, which)
+    for n in ("dx", "dW1", "dW2"):
+        if n not in which:
+            assert bool(getattr(b, n).isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_rows(dtype):
+    b = Block([0, 0, 0], 64, 40, dtype, "silu", spare=0)
+    b.forward()
+    b.backward(b.x, b.pre)
+    assert bool((b.dW1 == 0).all()) and bool((b.dW2 == 0).all())
+
+
+@pytest.mark.parametrize("keep", ["full", "8bit"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [NAN, float("inf")])
+def test_a_row_that_is_not_finite(bad, dtype, keep):
+    """It reaches its own rows and its expert's gradients alone."""
+    counts, d, F = [60, 70, 5], 72, 136
+    b, c = (Block(counts, d, F, dtype, "silu", seed=6) for _ in range(2))
+    b.x[62, 3] = bad                                            # a row of expert 1
+    grads = []
+    for k in (b, c):
+        pre = k.pre if keep == "full" else k.pre8
+        x = k.x
+        if keep == "8bit":
+            x = k.x8
+            B.scmoe_checkpoint_pack(k.x, x, n_rows=k.offsets[-1:])
+        k.forward(pre=pre)
+        k.backward(x, pre)
+        grads.append((k.y, k.dx, k.dW1, k.dW2))
+    rows = [r for r in range(b.K) if r != 62]
+    for got, want in zip(grads[0][:2], grads[1][:2]):
+        assert torch.equal(got[rows], want[rows]) and not bool(got[62].isfinite().any())
+    for got, want in zip(grads[0][2:], grads[1][2:]):
+        assert torch.equal(got[[0, 2]], want[[0, 2]])
+    assert not bool(grads[0][3][1].isfinite().any())
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_pre_activations(act, dtype):
+    """Where the activation is flat its value is 0 or its argument, its slope 0 or 1: no infinity times zero."""
+    b = Block([4], 8, 8, dtype, act, spare=0)
+    big = torch.tensor([1e4, -1e4, 1e10, -1e10, 3e19, -3e19, 200.0, -200.0], device=DEV).to(TYPES[dtype])
+    b.pre[:, :8], b.pre[:, 8:] = big, 1.0
+    b.dy.fill_(0.0)
+    b.dy[:, 0] = 1.0
+    b.W2.fill_(0.0)
+    b.W2[0, 0] = 1.0                                             # dh = 1 everywhere
+    b.x.fill_(0.0)
+    b.x[0, 0] = 1.0                                              # dW1[:, 0] = (dg, du) of row 0
+    b.backward(b.x, b.pre)
+    a, s = (big > 0) * big.float(), (big > 0).float()
+    assert torch.equal(b.dW1[0, :8, 0].float(), s) and torch.equal(b.dW1[0, 8:, 0], a.to(TYPES[dtype]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("keep", ["full", "8bit"])
+def test_results_are_the_same_from_call_to_call_and_in_graphs(dtype, keep):
+    b = Block([100, 0, 333, 40], 264, 520, dtype, "silu", seed=7)
+    pre, x = (b.pre, b.x) if keep == "full" else (b.pre8, b.x8)
+
+    def step():
+        if keep == "8bit":
+            B.scmoe_checkpoint_pack(b.x, b.x8, n_rows=b.offsets[-1:])
+        b.forward(pre=pre)
+        b.backward(x, pre)
+
+    def results():
+        torch.cuda.synchronize()
+        return [t.clone() for t in (b.y[:b.K], b.dx[:b.K], b.dW1, b.dW2)]
+
+    step()
+    first = results()
+    step()
+    assert all(torch.equal(p, q) for p, q in zip(first, results()))
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    base = b.x.clone()
+    for k in range(4):                                           # other rows, another load, eager calls in between
+        b.x.copy_(base * (1 + k))
+        b.offsets.copy_(offsets_of([[100, 0, 333, 40], [473, 0, 0, 0], [0, 1, 1, 1], [1, 200, 0, 272]][k]))
+        b.K = int(b.offsets[-1])
+        step()
+        want = results()
+        for t in (b.y, b.dx, b.dW1, b.dW2):
+            t.fill_(NAN)
+        graph.replay()
+        assert all(torch.equal(p, q) for p, q in zip(want, results()))
+
+
+def test_two_calls_at_once_on_two_streams():
+    """Each with its own workspace."""
+    blocks = [Block([200, 90, 130], 200, 264, "bf16", "silu", seed=s) for s in (8, 9)]
+    want = []
+    for b in blocks:
+        b.forward(pre=b.pre)
+        b.backward(b.x, b.pre)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in (b.y[:b.K], b.dx[:b.K], b.dW1, b.dW2)])
+    streams = [torch.cuda.Stream() for _ in blocks]
+    for _ in range(5):
+        for b, s in zip(blocks, streams):
+            b.forward(pre=b.pre, stream=s)
+            B.scmoe_gated_ffn_backward(b.dy, b.x, b.pre, b.offsets, b.rows, b.W1, b.W2, B.SILU, b.dx, b.dW1, b.dW2, workspace=b.workspace, stream=s)
+    torch.cuda.synchronize()
+    for b, w in zip(blocks, want):
+        assert all(torch.equal(p, q) for p, q in zip(w, (b.y[:b.K], b.dx[:b.K], b.dW1, b.dW2)))
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_gradients_against_differences(act):
+    """fp32: what the outputs of the forward call, weighted by dy, change by along a direction, against the gradient along it.  A central
+    difference with step t is off by t^2 times the third derivative (here under 1e-5 of the change) and by the roundings of the two
+    outputs over 2 t: 2^-24 times some tens of operations times the sum of |y dy|, over 2 t = 2^-5."""
+    b = Block([40, 0, 25], 64, 96, "f32", act, spare=0, pad=0, seed=10)
+    b.forward(pre=b.pre)
+    b.backward(b.x, b.pre)
+    for t, grad in ((b.x, b.dx), (b.W1, b.dW1), (b.W2, b.dW2)):
+        g, base = gen(11), t.clone()
+        way = torch.randn(t.shape, generator=g, device=DEV) * base.abs().mean()
+        step = 2.0 ** -6
+        sums, size = [], 0.0
+        for sign in (1, -1):
+            t.copy_(base + sign * step * way)
+            real = (t - base).double()                           # (the step that was taken, after its rounding)
+            b.forward()
+            sums.append(((b.y.double() * b.dy.double()).sum(), real))
+            size = float((b.y.double() * b.dy.double()).abs().sum())
+        t.copy_(base)
+        got = float(sums[0][0] - sums[1][0])
+        want = float((grad.double() * (sums[0][1] - sums[1][1])).sum())
+        terms = float((grad.double() * (sums[0][1] - sums[1][1])).abs().sum())
+        assert abs(got - want) <= 64 * H * size + 1e-3 * step * terms + 64 * H * terms
+
+
+def test_what_torch_differentiates():
+    """The same block as a function of torch in 64 bits."""
+    b = Block([33, 20], 64, 40, "f32", "gelu_tanh", spare=0, seed=12)
+    b.forward(pre=b.pre)
+    b.backward(b.x, b.pre)
+    for e, at in b.segments():
+        x, W1, W2 = (t.detach().double().requires_grad_(True) for t in (b.x[at], b.W1[e], b.W2[e]))
+        pre = x @ W1.t()
+        y = (torch.nn.functional.gelu(pre[:, :40], approximate="tanh") * pre[:, 40:]) @ W2.t()
+        grads = torch.autograd.grad(y, (x, W1, W2), b.dy[at].double())
+        for got, want in zip((b.dx[at], b.dW1[e], b.dW2[e]), grads):
+            # (sums of up to 80 terms after two products of 64: some hundred roundings of the largest terms)
+            assert float((got.double() - want).abs().max()) <= 1024 * H * float(want.abs().max())
