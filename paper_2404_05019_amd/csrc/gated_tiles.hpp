@@ -21,7 +21,7 @@
 #pragma once
 #include "checkpoint.hpp"
 #include "gated_act.hpp"
-#include "mfma_common.hpp"
+#include "rows.hpp"
 #include <atomic>
 
 namespace scmoe {
@@ -55,7 +55,9 @@ struct GatedCfg {
   static constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NJ = TN / 16;
   static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
   static constexpr int APW = A_BYTES / 1024 / WAVES, BPW = B_BYTES / 1024 / WAVES;  // copies of a wave and k-tile
-  static constexpr int LDS = NS * STAGE;
+  static constexpr int PATCH = F32 ? 0 : 4096;                                       // of a wave, for the epilogue
+  static constexpr int LDS = NS * STAGE + WAVES * PATCH;
+  static_assert(LDS <= 160 * 1024, "LDS budget");
   static constexpr int WG_PER_CU = (160 * 1024 / LDS) < (8 / WAVES) ? (160 * 1024 / LDS) : (8 / WAVES);
   static_assert(TM % 32 == 0 && TN == 64 && APW % 2 == 0 && WG_PER_CU >= 1 && NS >= 2, "tile shape");
 };
@@ -70,15 +72,23 @@ __host__ __device__ constexpr int across_swz(int k) {
 
 typedef unsigned int g_u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int g_u32x2 __attribute__((ext_vector_type(2)));
+typedef short g_i16x4 __attribute__((ext_vector_type(4)));
 
-// Sixteen columns of four rows each of k, transposed (see above).
-__device__ __forceinline__ g_u32x2 lds_read_transposed(uint32_t at) {
+// Sixteen columns of four rows each of k, transposed (see above).  The second pointer is for the compiler alone: two that are said not to
+// overlap give the read a scope of its own, without which it would wait for every copy in flight to LDS (vmcnt(0)) ahead of it, once a
+// k-tile; the kernel waits for the copies that it needs (gradient of both weights, 32768 rows, d = 2048, F = 8192, E = 16: 3836 us with
+// that wait, 2544 without).
+__device__ __forceinline__ g_u32x2 lds_read_transposed(__attribute__((address_space(3))) g_i16x4* __restrict at,
+                                                       __attribute__((address_space(3))) g_i16x4* __restrict /*elsewhere*/) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  typedef __bf16 v4 __attribute__((ext_vector_type(4)));
-  return __builtin_bit_cast(g_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16(reinterpret_cast<__attribute__((address_space(3))) v4*>(static_cast<uintptr_t>(at))));
+  return __builtin_bit_cast(g_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at));
 #else
   return g_u32x2{0, 0};
 #endif
+}
+__device__ __forceinline__ g_u32x2 lds_read_transposed(uint32_t at) {
+  typedef __attribute__((address_space(3))) g_i16x4* lds8_ptr;
+  return lds_read_transposed(reinterpret_cast<lds8_ptr>(static_cast<uintptr_t>(at)), reinterpret_cast<lds8_ptr>(static_cast<uintptr_t>(at + 64)));
 }
 
 // The largest value over the four lanes that hold 16 columns each of a row's 32 (lanes l, l ^ 16, l ^ 32, l ^ 48).
@@ -146,14 +156,21 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
   const unsigned char* bbase = nullptr;
   int64_t lda = 0, ldb = 0;
   uint32_t aoff[APW], boff[BPW];
+  // A copy of the lane that what is worked out from it does not outlive its use: nothing of a tile's start or end takes registers of the
+  // k loop.
+  auto lane_here = [&]() {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    return l;
+  };
   // Place of this lane's 16 bytes of copy i: row and first column (along k: of the k-tile's row; across: of the tile).
   auto a_row = [&](int i) {                      // along k: LDS row = tile row that copy i begins with
     constexpr int HP = APW / 2, HALF = TM / 2;
     const int q = (wave * HP + i % HP) * 8;
     return (q / HALF) * TM + (i / HP) * HALF + q % HALF;
   };
-  auto a_k = [&](int i) { return ((wave * (APW / 2) + i % (APW / 2)) * 1024) / A_ROWB + lane / (A_ROWB / 16); };   // across
-  auto b_k = [&](int i) { return ((wave * BPW + i) * 1024) / B_ROWB + lane / (B_ROWB / 16); };
+  auto a_k = [&](int i, int ln) { return ((wave * (APW / 2) + i % (APW / 2)) * 1024) / A_ROWB + ln / (A_ROWB / 16); };   // across
+  auto b_k = [&](int i, int ln) { return ((wave * BPW + i) * 1024) / B_ROWB + ln / (B_ROWB / 16); };
   auto setup = [&](int item) {
     const GatedJob* jb = &p.j[0];
     if constexpr (MODE == G_DW) {
@@ -182,25 +199,26 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     nk = (k_all + BK - 1) / BK;
     lda = jb->lda;
     ldb = jb->ldb;
+    const int ln = lane_here();
 #pragma unroll
     for (int i = 0; i < APW; ++i) {
       if constexpr (A_ACROSS) {
-        const int k = a_k(i), c = (lane % (A_ROWB / 16)) ^ (across_swz<F32, A_ROWB>(k) * (16 / VE));
+        const int k = a_k(i, ln), c = (ln % (A_ROWB / 16)) ^ (across_swz<F32, A_ROWB>(k) * (16 / VE));
         const int lc = c * VE, col = row0 + (lc / (TM / 2)) * TM + (i / (APW / 2)) * (TM / 2) + lc % (TM / 2);
         aoff[i] = col < row_end ? static_cast<uint32_t>((static_cast<int64_t>(k) * lda + col) * EB) : BUFFER_NOWHERE;
       } else {
-        const int r = a_row(i) + lane / 8, kc = (lane % 8) ^ swz<8>(r);
+        const int r = a_row(i) + ln / 8, kc = (ln % 8) ^ swz<8>(r);
         aoff[i] = row0 + r < row_end ? static_cast<uint32_t>(static_cast<int64_t>(r) * lda * EB + kc * 16) : BUFFER_NOWHERE;
       }
     }
 #pragma unroll
     for (int i = 0; i < BPW; ++i) {
       if constexpr (B_ACROSS) {
-        const int k = b_k(i), c = (lane % (B_ROWB / 16)) ^ (across_swz<F32, B_ROWB>(k) * (16 / VE));
+        const int k = b_k(i, ln), c = (ln % (B_ROWB / 16)) ^ (across_swz<F32, B_ROWB>(k) * (16 / VE));
         const int col = n0 + c * VE;
         boff[i] = col < jb->N ? static_cast<uint32_t>((static_cast<int64_t>(k) * ldb + col) * EB) : BUFFER_NOWHERE;
       } else {
-        const int r = (wave * BPW + i) * 8 + lane / 8, kc = (lane % 8) ^ swz<8>(r);
+        const int r = (wave * BPW + i) * 8 + ln / 8, kc = (ln % 8) ^ swz<8>(r);
         int n = n0 + r, row = n;
         if constexpr (MODE == G_GATE) {            // 64 columns of a wave: 32 of g, and the same 32 of u
           const int in = r % TN;
@@ -212,39 +230,41 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     }
     if constexpr (!B_ACROSS) bbase += static_cast<int64_t>(n0) * ldb * EB;
   };
-  // k of this lane's 16 bytes inside the k-tile
-  auto in_k = [&](int kt, int k) { return kt * BK + k < k_all; };
+  // The last k-tile may be cut short: what lies past the end is not read (zeros).
+  auto a_off = [&](int i, int kt, int ln) {
+    const int k = A_ACROSS ? a_k(i, ln) : ((ln % 8) ^ swz<8>(a_row(i) + ln / 8)) * VE;
+    return kt * BK + k < k_all ? aoff[i] : BUFFER_NOWHERE;
+  };
+  auto b_off = [&](int i, int kt, int ln) {
+    const int k = B_ACROSS ? b_k(i, ln) : ((ln % 8) ^ swz<8>((wave * BPW + i) * 8 + ln / 8)) * VE;
+    return kt * BK + k < k_all ? boff[i] : BUFFER_NOWHERE;
+  };
   auto issue_a = [&](int kt, int stage, auto half_c) {
     constexpr int h = decltype(half_c)::value;
-    const bool tail = (kt + 1) * BK > k_all;
+    const unsigned char* const base = A_ACROSS ? abase + static_cast<int64_t>(kt) * (BK * EB) * lda : abase;
+    const uint32_t soff = A_ACROSS ? 0u : static_cast<uint32_t>(kt) * 128;
+    // (across: the columns of the waves' first halves, then of their second halves, BK rows of A_ROWB bytes each)
+    auto to = [&](int i) { return smem + stage * STAGE + (A_ACROSS ? h * (A_BYTES / 2) + (wave * (APW / 2) + i % (APW / 2)) * 1024 : a_row(i) * 128); };
+    if ((kt + 1) * BK <= k_all) {
 #pragma unroll
-    for (int i = h * (APW / 2); i < (h + 1) * (APW / 2); ++i) {
-      uint32_t off = aoff[i];
-      if constexpr (A_ACROSS) {
-        if (tail && !in_k(kt, a_k(i))) off = BUFFER_NOWHERE;
-        // (the columns of the waves' first halves, then of their second halves: each BK rows of A_ROWB bytes)
-        buffer_to_lds16(abase + static_cast<int64_t>(kt) * BK * lda * EB, smem + stage * STAGE + h * (A_BYTES / 2) + (wave * (APW / 2) + i % (APW / 2)) * 1024, off, 0);
-      } else {
-        const int r = a_row(i) + lane / 8;
-        if (tail && !in_k(kt, ((lane % 8) ^ swz<8>(r)) * VE)) off = BUFFER_NOWHERE;
-        buffer_to_lds16(abase, smem + stage * STAGE + a_row(i) * 128, off, static_cast<uint32_t>(kt) * 128);
-      }
+      for (int i = h * (APW / 2); i < (h + 1) * (APW / 2); ++i) buffer_to_lds16(base, to(i), aoff[i], soff);
+    } else {
+      const int ln = lane_here();
+#pragma unroll
+      for (int i = h * (APW / 2); i < (h + 1) * (APW / 2); ++i) buffer_to_lds16(base, to(i), a_off(i, kt, ln), soff);
     }
   };
   auto issue_b = [&](int kt, int stage) {
-    const bool tail = (kt + 1) * BK > k_all;
-    unsigned char* const sb = smem + stage * STAGE + A_BYTES + wave * BPW * 1024;
+    const unsigned char* const base = B_ACROSS ? bbase + static_cast<int64_t>(kt) * (BK * EB) * ldb : bbase;
+    const uint32_t soff = B_ACROSS ? 0u : static_cast<uint32_t>(kt) * 128;
+    unsigned char* const to = smem + stage * STAGE + A_BYTES + wave * BPW * 1024;
+    if ((kt + 1) * BK <= k_all) {
 #pragma unroll
-    for (int i = 0; i < BPW; ++i) {
-      uint32_t off = boff[i];
-      if constexpr (B_ACROSS) {
-        if (tail && !in_k(kt, b_k(i))) off = BUFFER_NOWHERE;
-        buffer_to_lds16(bbase + static_cast<int64_t>(kt) * BK * ldb * EB, sb + i * 1024, off, 0);
-      } else {
-        const int r = (wave * BPW + i) * 8 + lane / 8;
-        if (tail && !in_k(kt, ((lane % 8) ^ swz<8>(r)) * VE)) off = BUFFER_NOWHERE;
-        buffer_to_lds16(bbase, sb + i * 1024, off, static_cast<uint32_t>(kt) * 128);
-      }
+      for (int i = 0; i < BPW; ++i) buffer_to_lds16(base, to + i * 1024, boff[i], soff);
+    } else {
+      const int ln = lane_here();
+#pragma unroll
+      for (int i = 0; i < BPW; ++i) buffer_to_lds16(base, to + i * 1024, b_off(i, kt, ln), soff);
     }
   };
   auto issue_ba0 = [&](int kt, int stage) {
@@ -423,12 +443,176 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     const int cN = jc.N;
     const int itn = MODE == G_DW ? it + nslots : sched.next(it);
     const bool more = itn < items;
+    // bf16: an output row's 16-byte pieces as a wave stores them, 8 rows at a time: lane l has piece l % 8 of row l / 8, and of row
+    // 8 + l / 8, of a subtile of 16 rows
+    const int le = lane_here(), pr = le >> 3, pc = le & 7;
+    const int l16 = le & 15, lq = le >> 4;
+    const int pn = cn0 + wave_n * TN + pc * 8;                 // its first column
+    // DH: g and u of a subtile's pieces (8 bits: codes, and the block's scale), a subtile ahead of their use
+    g_u32x4 kg[2][2], ku[2][2];
+    auto load_kept = [&](int i) {
+      if constexpr (MODE == G_DH && !F32) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          // (rows past the segment and columns past the matrix: the last ones again, for no store)
+          const int rk = crow0 + wave_m * TM + i * 16 + t * 8 + pr, r = rk < crow_end ? rk : crow_end - 1, n = pn < cN ? pn : cN - 8;
+          if constexpr (KEEP == KEEP_8BIT) {
+            const unsigned char* row = p.pre + 2 * static_cast<int64_t>(r) * p.ldpre;
+            const uint2 a = *reinterpret_cast<const uint2*>(row + n), b = *reinterpret_cast<const uint2*>(row + p.ldpre + n);
+            kg[i & 1][t] = g_u32x4{a.x, a.y, row[cN + n / CKPT_BLOCK], row[p.ldpre + cN + n / CKPT_BLOCK]};
+            ku[i & 1][t] = g_u32x4{b.x, b.y, 0, 0};
+          } else {
+            const unsigned char* row = p.pre + (static_cast<int64_t>(r) * p.ldpre + n) * 2;
+            kg[i & 1][t] = *reinterpret_cast<const g_u32x4*>(row);
+            ku[i & 1][t] = *reinterpret_cast<const g_u32x4*>(row + static_cast<int64_t>(cN) * 2);
+          }
+        }
+      }
+    };
+    load_kept(0);
     if (more) {
       setup(itn);
       issue_prologue();
     }
 
     // ---- store: acc[i][j][q] is row l16 of subtile i, column 4 lq + q of subtile j -----------------------------
+    // bf16: rows are put together in the wave's patch of LDS, a subtile of 16 rows at a time, and leave it as whole lines.
+    unsigned char* const patch = smem + NS * STAGE + wave * CFG::PATCH;
+    if constexpr (!F32) {
+      auto out16 = [&](unsigned char* at, g_u32x4 v) { *reinterpret_cast<g_u32x4*>(at) = v; };
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const int rbase = crow0 + wave_m * TM + i * 16;
+        if (rbase >= crow_end) break;                          // (wave-uniform)
+        wave_lds_order();                                      // (the patch has been read)
+        __builtin_amdgcn_sched_barrier(0);                     // (a subtile at a time: several take registers that are not there)
+        if constexpr (MODE == G_DH) {
+          if (i + 1 < MI) load_kept(i + 1);
+          // dh in fp32: 16 rows of 256 bytes, chunks swizzled by the row
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) *reinterpret_cast<f32x4_t*>(patch + l16 * 256 + (((j * 4 + lq) ^ l16) << 4)) = acc[i][j];
+          wave_lds_order();
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int rr = t * 8 + pr, r = rbase + rr;
+            float dh[8], g[8], u[8], h[8];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const f32x4_t v = *reinterpret_cast<const f32x4_t*>(patch + rr * 256 + (((pc * 2 + c) ^ rr) << 4));
+#pragma unroll
+              for (int q = 0; q < 4; ++q) dh[c * 4 + q] = v[q];
+            }
+            const g_u32x4 wg = kg[i & 1][t], wu = ku[i & 1][t];
+            if constexpr (KEEP == KEEP_8BIT) {
+              const float sg = ckpt_scale(wg[2]), su = ckpt_scale(wg[3]);
+              ckpt_decode4(wg[0], sg, g);
+              ckpt_decode4(wg[1], sg, g + 4);
+              ckpt_decode4(wu[0], su, u);
+              ckpt_decode4(wu[1], su, u + 4);
+            } else {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                g[2 * q] = __uint_as_float(wg[q] << 16);
+                g[2 * q + 1] = __uint_as_float(wg[q] & 0xffff0000u);
+                u[2 * q] = __uint_as_float(wu[q] << 16);
+                u[2 * q + 1] = __uint_as_float(wu[q] & 0xffff0000u);
+              }
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              float a, s;
+              gated_act_slope<F32>(g[q], p.act, a, s);
+              h[q] = a * u[q];
+              g[q] = dh[q] * u[q] * s;
+              u[q] = dh[q] * a;
+            }
+            auto pack8 = [&](const float* v) { return g_u32x4{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])}; };
+            const g_u32x4 oh = pack8(h), og = pack8(g), ou = pack8(u);
+            if (r < crow_end && pn < cN) {
+              out16(cC + (static_cast<int64_t>(r) * cldc + pn) * 2, oh);
+              unsigned char* const to = p.dpre + (static_cast<int64_t>(r) * p.lddpre + pn) * 2;
+              out16(to, og);
+              out16(to + static_cast<int64_t>(cN) * 2, ou);
+            }
+          }
+        } else if constexpr (MODE == G_GATE) {
+          // 32 columns a wave: hidden, g, u in 16 rows of 64 bytes each (in 8 bits: of 32), one behind the other
+          constexpr int J2 = NJ / 2;
+          static_assert(J2 * 16 == CKPT_BLOCK, "a wave has one block of g and of u");
+          const int f0 = cn0 + wave_n * (TN / 2);
+          uint32_t byte[2] = {0, 0};
+          float inv[2] = {0.0f, 0.0f};
+          if constexpr (KEEP == KEEP_8BIT) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              uint32_t most = 0;
+#pragma unroll
+              for (int j = 0; j < J2; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) most = max(most, magnitude(acc[i][t * J2 + j][q]));
+              byte[t] = ckpt_scale_byte(max_over_lq(most));
+              inv[t] = ckpt_inverse(byte[t]);
+            }
+          }
+          const int sw = (l16 >> 1) & 3;                       // 64-byte rows: chunks of 16 bytes, swizzled
+#pragma unroll
+          for (int j = 0; j < J2; ++j) {
+            float h[4];
+            const f32x4_t g = acc[i][j], u = acc[i][J2 + j];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) h[q] = gated_act<F32>(g[q], p.act) * u[q];
+            const int at = l16 * 64 + (((j * 2 + (lq >> 1)) ^ sw) << 4) + (lq & 1) * 8;
+            *reinterpret_cast<uint2*>(patch + at) = make_uint2(cvt_pk_bf16(h[0], h[1]), cvt_pk_bf16(h[2], h[3]));
+            if constexpr (KEEP == KEEP_FULL) {
+              *reinterpret_cast<uint2*>(patch + 1024 + at) = make_uint2(cvt_pk_bf16(g[0], g[1]), cvt_pk_bf16(g[2], g[3]));
+              *reinterpret_cast<uint2*>(patch + 2048 + at) = make_uint2(cvt_pk_bf16(u[0], u[1]), cvt_pk_bf16(u[2], u[3]));
+            } else if constexpr (KEEP == KEEP_8BIT) {
+              *reinterpret_cast<uint32_t*>(patch + 1024 + l16 * 32 + j * 16 + lq * 4) = ckpt_encode4(g[0], g[1], g[2], g[3], inv[0]);
+              *reinterpret_cast<uint32_t*>(patch + 1536 + l16 * 32 + j * 16 + lq * 4) = ckpt_encode4(u[0], u[1], u[2], u[3], inv[1]);
+            }
+          }
+          wave_lds_order();
+          {
+            const int rr = le >> 2, c = le & 3, r = rbase + rr, f = f0 + c * 8;
+            const int at = rr * 64 + ((c ^ ((rr >> 1) & 3)) << 4);
+            if (r < crow_end && f < cN) {
+              out16(cC + (static_cast<int64_t>(r) * cldc + f) * 2, *reinterpret_cast<const g_u32x4*>(patch + at));
+              if constexpr (KEEP == KEEP_FULL) {
+                unsigned char* const to = p.pre + (static_cast<int64_t>(r) * p.ldpre + f) * 2;
+                out16(to, *reinterpret_cast<const g_u32x4*>(patch + 1024 + at));
+                out16(to + static_cast<int64_t>(cN) * 2, *reinterpret_cast<const g_u32x4*>(patch + 2048 + at));
+              }
+            }
+          }
+          if constexpr (KEEP == KEEP_8BIT) {
+            // lane l: 16 codes, half l % 2 of row l / 2 % 16 of g (lanes 0 .. 31) or u
+            const int t = le >> 5, rr = (le >> 1) & 15, c = le & 1, r = rbase + rr, f = f0 + c * 16;
+            unsigned char* const row = p.pre + (2 * static_cast<int64_t>(r) + t) * p.ldpre;
+            if (r < crow_end && f < cN) {
+              const unsigned char* const from = patch + 1024 + t * 512 + rr * 32 + c * 16;
+              if (f + 16 <= cN) *reinterpret_cast<g_u32x4*>(row + f) = *reinterpret_cast<const g_u32x4*>(from);
+              else *reinterpret_cast<uint2*>(row + f) = *reinterpret_cast<const uint2*>(from);      // (the width is a multiple of 8)
+            }
+            if (lq < 2 && rbase + l16 < crow_end && f0 < cN)
+              p.pre[(2 * static_cast<int64_t>(rbase + l16) + lq) * p.ldpre + cN + f0 / CKPT_BLOCK] = static_cast<unsigned char>(lq == 0 ? byte[0] : byte[1]);
+          }
+        } else {
+          unsigned char* const half = patch + (i & 1) * 2048;   // 16 rows of 128 bytes
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+            *reinterpret_cast<uint2*>(half + l16 * 128 + (((2 * j + (lq >> 1)) ^ swz<8>(l16)) << 4) + (lq & 1) * 8) =
+                make_uint2(cvt_pk_bf16(acc[i][j][0], acc[i][j][1]), cvt_pk_bf16(acc[i][j][2], acc[i][j][3]));
+          wave_lds_order();
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int rr = t * 8 + pr, r = rbase + rr;
+            const g_u32x4 v = *reinterpret_cast<const g_u32x4*>(half + rr * 128 + ((pc ^ swz<8>(rr)) << 4));
+            const int64_t row = MODE == G_DW ? static_cast<int64_t>(ce) * jc.M + r : r;
+            if (r < crow_end && pn < cN) out16(cC + (row * cldc + pn) * 2, v);
+          }
+        }
+      }
+    } else {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       const int r = crow0 + wave_m * TM + i * 16 + l16;
@@ -512,6 +696,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
           }
         }
       }
+    }
     }
     it = itn;
     if (!more) break;
