@@ -153,6 +153,8 @@ struct FfnArgs {
 bool ffn_is_tiled(int dtype, int d, int F, int max_rows, int E, int64_t mean_rows, int64_t all_rows);
 // One expert-FFN call, whichever kernel it takes.
 int ffn_forward(const FfnArgs& a, int dtype, hipStream_t stream);
+// Its second product alone: y = W2 . hidden + b2.
+int ffn_second(const FfnArgs& a, int dtype, hipStream_t stream);
 // The shared expert `se` (one dense segment) and the routed experts `rt`.  Both tiled: their
 // first GEMMs share a launch; the second GEMMs are one product with rt.joint_offsets, else one
 // launch if neither decodes, else two: the shared expert's first (the routed one may decode into

@@ -1239,6 +1239,16 @@ int ffn_forward(const FfnArgs& a, int dtype, hipStream_t stream) {
   return launch_variant<false>(second_gemm(a, sk), a.max_rows, a.max_rows, stream);
 }
 
+int ffn_second(const FfnArgs& a, int dtype, hipStream_t stream) {
+  if (!is_tiled(a, dtype)) {
+    const DirectJob second = direct_second(a);
+    return launch_gemm_direct(&second, 1, dtype, stream);
+  }
+  SplitK sk;
+  const int st = prepare_splitk(a, sk, stream);
+  return st == SCMOE_OK ? launch_variant<false>(second_gemm(a, sk), a.max_rows, a.max_rows, stream) : st;
+}
+
 int ffn_forward_pair(const FfnArgs& se, const FfnArgs& rt, int dtype, hipStream_t stream) {
   if (se.d != rt.d || se.F != rt.F || se.E != 1 || (se.gather != nullptr) != (rt.joint_offsets != nullptr) || se.gelu_mode != rt.gelu_mode) return SCMOE_ERR_ARG;
   if (se.max_rows <= 0) return ffn_forward(rt, dtype, stream);

@@ -7,15 +7,25 @@ namespace scmoe {
 using GatedA = GatedCfg<false, 256, 256, 2, 4, 2>;   // 8 waves of 128 x 64, 128 KiB LDS, one workgroup per CU
 using GatedU = GatedCfg<false, 128, 128, 2, 2, 2>;   // 4 waves of 64 x 64, 64 KiB LDS, two workgroups per CU
 
+using GatedS = GatedCfg<false, 64, 64, 4, 1, 3>;     // 4 waves of 16 x 64, 64 KiB LDS, two workgroups per CU
+
 // Which tiles: by rounds of workgroups, an expert's last row tile counted as half full.  A 256 x 256 tile is one workgroup's, alone on its
 // compute unit; of the 128 x 128 ones a unit has two, which take 1.5 times as long for their share of the work.  A last, partly filled
-// round costs between half a round and a whole one: its workgroups have the caches to themselves.  us, large / small tiles:
-//   16384 rows, d = 1024, F = 4096, E = 8      GATE 342 / 371, DH 238 / 271, DX 236 / 305, DW 390 / 491, DOWN 120 / 149
-//   8192 rows, d = 384, F = 1536, E = 8        DH 40.6 / 39.2, DX 71 / 37, DW 63 / 42
-//   5003 rows, d = 1000, F = 2728, E = 32      GATE 127 / 141, DOWN 92 / 85
-//   2000 rows, d = 768, F = 2048, E = 64       GATE 144 / 129, DH 70 / 55, DX 113 / 97, DW 142 / 174, DOWN 70 / 63
-static bool large_tiles(const GatedArgs& a, int mode, int64_t max_rows) {
-  const int64_t cus = num_cus();
+// round costs between half a round and a whole one: its workgroups have the caches to themselves.  us, large / middle / small tiles
+// (GATE, DOWN: of a forward call; DH, DX, DW: of a gradient):
+//   16384 rows, d = 1024, F = 4096, E = 8      GATE 368 / 397 / 597, DH 794 / 809 / 910, DX 787 / 865 / 1084, DW 799 / 890 / 1187
+//   8192 rows, d = 384, F = 1536, E = 8        GATE 56 / 51 / 67, DH 119 / 119 / 127, DX 150 / 119 / 129, DW 138 / 120 / 137
+//   5003 rows, d = 1000, F = 2728, E = 32      GATE 273 / 283 / 341, DH 476 / 469 / 508, DX 476 / 476 / 531, DW 476 / 504 / 725
+//   2000 rows, d = 768, F = 2048, E = 64       GATE 157 / 145 / 152, DH 334 / 334 / 335, DX 336 / 334 / 329, DW 333 / 366 / 524
+//   64 rows, d = 2048, F = 8192, E = 16        GATE 345 / 311 / 319, DH 660 / 665 / 677, DX 797 / 668 / 699, DW 667 / 744 / 1136
+// 64 x 64 tiles where the 128 x 128 ones would leave half of the compute units without work, or a quarter with a short K; their rows of an
+// operand across k are 128 bytes long, which streams weights worse, and a gradient of weights (all tiles are written, whatever the rows)
+// always has tiles enough:
+//   1 row, d = 2048, F = 8192, E = 16          GATE 60 / 38 / 33, DH 447 / 426 / 421, DX 581 / 427 / 388
+//   500 rows, d = 1000, F = 2728, E = 8        GATE 74 / 70 / 71, DH 148 / 134 / 133, DX 198 / 133 / 122
+//   2000 rows, d = 512, F = 1024, E = 8        GATE 35 / 29 / 28, DH 72 / 57 / 49, DX 80 / 57 / 49, DW 57 / 57 / 65
+static int tiles_for(const GatedArgs& a, int mode, int64_t max_rows) {
+  const double cus = num_cus();
   double tiles[2] = {0, 0};
   for (int q = 0; q < 2; ++q) {
     const int B = q == 0 ? 256 : 128, BN = mode == G_GATE ? B / 2 : B;
@@ -26,15 +36,20 @@ static bool large_tiles(const GatedArgs& a, int mode, int64_t max_rows) {
       else tiles[q] += across * (static_cast<double>(max_rows) / B + 0.5 * static_cast<double>(a.E < max_rows ? a.E : max_rows));
     }
   }
+  if (mode != G_DW && tiles[1] < (a.j[0].Kd < 2048 ? 0.75 : 0.5) * cus) return 64;
   auto rounds = [](double t) {
     const double whole = floor(t), rest = t - whole;
     return whole < 1.0 ? 1.0 : rest > 0.0 ? whole + 0.5 + 0.5 * rest : whole;
   };
-  return 4.0 * rounds(tiles[0] / static_cast<double>(cus)) <= 2.0 * 1.5 * rounds(tiles[1] / (2.0 * static_cast<double>(cus)));
+  return 4.0 * rounds(tiles[0] / cus) <= 2.0 * 1.5 * rounds(tiles[1] / (2.0 * cus)) ? 256 : 128;
 }
 
 int launch_gated_bf16(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream) {
-  return large_tiles(a, mode, max_rows) ? launch_gated_mode<GatedA>(a, mode, keep, max_rows, stream) : launch_gated_mode<GatedU>(a, mode, keep, max_rows, stream);
+  switch (tiles_for(a, mode, max_rows)) {
+    case 256: return launch_gated_mode<GatedA>(a, mode, keep, max_rows, stream);
+    case 128: return launch_gated_mode<GatedU>(a, mode, keep, max_rows, stream);
+    default: return launch_gated_mode<GatedS>(a, mode, keep, max_rows, stream);
+  }
 }
 
 }  // namespace scmoe

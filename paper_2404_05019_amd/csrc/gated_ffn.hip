@@ -42,6 +42,15 @@ static bool kept_ok(const void* p, int64_t ld, int64_t width, int keep, int dtyp
   return keep == SCMOE_KEEP_8BIT ? ckpt_view_ok(p, ld, width) && ld <= GATED_MOST_LD : gated_view_ok(p, ld, width, dtype);
 }
 
+// Where y = W2 h is the second product of the experts without a gate (ffn_mfma.hip, ffn_direct.hip): in bf16 where its tiled kernel takes
+// the widths, and for few rows, when its other kernel streams the weights; else this block's own.  us of a forward call, so / with DOWN:
+// bf16, 16384 rows, d = 1024, F = 4096, E = 8 372 / 394; 1 row, d = 2048, F = 8192, E = 16 41 / 73; 1 row, d = 1000, F = 2728, E = 8 21 / 26; 30 rows
+// 45 / 52; but 500 rows 73 / 64, 5003 rows, E = 32 272 / 208.  fp32, 1 row, d = 1024, F = 4096, E = 8 84 / 95; but 40 rows 161 / 148, 4096, F = 2048 417 / 381.
+static bool second_is_the_experts(int dtype, int64_t rows, int E, int d, int F) {
+  if (dtype == SCMOE_F32) return rows <= E;
+  return ffn_mfma_supported(d, F) || rows <= 64 || (rows <= 16 * static_cast<int64_t>(E) && rows <= 1024);
+}
+
 struct GatedWs { int64_t ldp, ldh; size_t dpre, hidden, x, total; };
 static GatedWs gated_ws(int dtype, int64_t rows, int d, int F) {
   GatedWs w;
@@ -62,7 +71,7 @@ extern "C" int scmoe_gated_ffn_workspace_bytes(int32_t dtype, int32_t d, int32_t
   using namespace scmoe;
   if (!out) return SCMOE_ERR_NULL;
   const int st = check_gated(dtype, 0, 1, d, F, SCMOE_SILU);
-  if (st == SCMOE_OK) *out = 0;
+  if (st == SCMOE_OK) *out = dtype == SCMOE_BF16 && ffn_mfma_supported(d, F) ? ffn_mfma_scratch_bytes() : 0;
   return st;
 }
 
@@ -71,7 +80,6 @@ extern "C" int scmoe_gated_ffn(const void* x_perm, int64_t ld_perm, int32_t dtyp
                                int64_t ldh, void* pre, int64_t ldpre, int32_t pre_keep, void* y_perm, int64_t ldy, void* workspace,
                                size_t ws_bytes, void* stream) {
   using namespace scmoe;
-  (void)ws_bytes;
   int st = check_gated(dtype, max_rows, E, d, F, act);
   if (st != SCMOE_OK) return st;
   if (pre_keep != SCMOE_KEEP_NOTHING && pre_keep != SCMOE_KEEP_FULL && pre_keep != SCMOE_KEEP_8BIT) return SCMOE_ERR_ARG;
@@ -88,6 +96,13 @@ extern "C" int scmoe_gated_ffn(const void* x_perm, int64_t ld_perm, int32_t dtyp
   a.j[0] = gated_job(x_perm, ld_perm, W1, ldw1, hidden, ldh, 0, F, d);
   st = launch_gated(a, G_GATE, pre_keep, max_rows, dtype, s);
   if (st != SCMOE_OK) return st;
+  if (second_is_the_experts(dtype, max_rows, E, d, F)) {
+    FfnArgs f{};
+    f.offsets = offsets; f.max_rows = max_rows; f.E = E; f.d = d; f.F = F;
+    f.W2 = W2; f.ldw2 = ldw2; f.hidden = hidden; f.ldh = ldh; f.y = y_perm; f.ldy = ldy;
+    f.scratch = workspace; f.scratch_bytes = ws_bytes;
+    return ffn_second(f, dtype, s);
+  }
   a.j[0] = gated_job(hidden, ldh, W2, ldw2, y_perm, ldy, 0, d, F);
   return launch_gated(a, G_DOWN, KEEP_NONE, max_rows, dtype, s);
 }

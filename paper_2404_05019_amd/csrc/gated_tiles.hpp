@@ -47,25 +47,28 @@ struct GatedArgs {
 };
 
 template <bool F32_, int BM_, int BN_, int WM_, int WN_, int NS_>
-struct GatedCfg {
+struct GatedCfg {                      // NS_: stages
   static constexpr bool F32 = F32_;
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NS = NS_;
   static constexpr int EB = F32 ? 4 : 2, VE = 16 / EB, BK = 128 / EB, KS = 2;      // KS: k steps of 64 bytes in a stage
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
   static constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NJ = TN / 16;
+  static constexpr int NH = MI > 1 ? 2 : 1;                                          // halves of a wave's rows that a stage is refilled by
   static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
   static constexpr int APW = A_BYTES / 1024 / WAVES, BPW = B_BYTES / 1024 / WAVES;  // copies of a wave and k-tile
   static constexpr int PATCH = F32 ? 0 : 4096;                                       // of a wave, for the epilogue
   static constexpr int LDS = NS * STAGE + WAVES * PATCH;
   static_assert(LDS <= 160 * 1024, "LDS budget");
-  static constexpr int WG_PER_CU = (160 * 1024 / LDS) < (8 / WAVES) ? (160 * 1024 / LDS) : (8 / WAVES);
-  static_assert(TM % 32 == 0 && TN == 64 && APW % 2 == 0 && WG_PER_CU >= 1 && NS >= 2, "tile shape");
+  static constexpr int MOST_WG = (MI > 1 ? 8 : 16) / WAVES;                          // by registers: two waves a SIMD, small tiles four
+  static constexpr int WG_PER_CU = (160 * 1024 / LDS) < MOST_WG ? (160 * 1024 / LDS) : MOST_WG;
+  static_assert(TM % (16 * NH) == 0 && TN == 64 && APW % NH == 0 && WG_PER_CU >= 1 && NS >= 2, "tile shape");
 };
 
 // Swizzle of an operand across k: a read takes rows k of 8 consecutive ones at a time of two (bf16: lanes' groups of 16 on rows
 // 8 lq + 0..3) or of four (fp32: rows 4 lq + c) groups.  ROWB: bytes of a row in LDS; the result is added (xor) to the unit of 16 columns.
 template <bool F32, int ROWB>
 __host__ __device__ constexpr int across_swz(int k) {
+  static_assert(ROWB >= (F32 ? 256 : 128), "four units of 16 columns");
   if (F32) return (k >> 2) & 3;
   return ROWB >= 256 ? (k & 3) | (((k >> 3) & 1) << 2) : ((k >> 1) & 1) | (((k >> 3) & 1) << 1);
 }
@@ -124,10 +127,10 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
   constexpr bool F32 = CFG::F32;
   constexpr int BM = CFG::BM, BN = CFG::BN, EB = CFG::EB, VE = CFG::VE, BK = CFG::BK, KS = CFG::KS, NS = CFG::NS;
   constexpr int MI = CFG::MI, NJ = CFG::NJ, TM = CFG::TM, TN = CFG::TN, STAGE = CFG::STAGE, A_BYTES = CFG::A_BYTES;
-  constexpr int APW = CFG::APW, BPW = CFG::BPW, LPW = APW + BPW, H = MI / 2;
+  constexpr int APW = CFG::APW, BPW = CFG::BPW, LPW = APW + BPW, NH = CFG::NH, H = MI / NH, APH = APW / NH;
   constexpr bool A_ACROSS = MODE == G_DW, B_ACROSS = MODE >= G_DH;
   constexpr int BNF = MODE == G_GATE ? BN / 2 : BN;             // columns of the output that a tile has
-  constexpr int A_ROWB = BM / 2 * EB, B_ROWB = BN * EB;         // across k: bytes of an LDS row (A: of half the tile's columns, see issue_a)
+  constexpr int A_ROWB = BM / NH * EB, B_ROWB = BN * EB;        // across k: bytes of an LDS row (A: of a half of the tile's columns, see issue_a)
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -165,11 +168,11 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
   };
   // Place of this lane's 16 bytes of copy i: row and first column (along k: of the k-tile's row; across: of the tile).
   auto a_row = [&](int i) {                      // along k: LDS row = tile row that copy i begins with
-    constexpr int HP = APW / 2, HALF = TM / 2;
-    const int q = (wave * HP + i % HP) * 8;
-    return (q / HALF) * TM + (i / HP) * HALF + q % HALF;
+    constexpr int HALF = TM / NH;
+    const int q = (wave * APH + i % APH) * 8;
+    return (q / HALF) * TM + (i / APH) * HALF + q % HALF;
   };
-  auto a_k = [&](int i, int ln) { return ((wave * (APW / 2) + i % (APW / 2)) * 1024) / A_ROWB + ln / (A_ROWB / 16); };   // across
+  auto a_k = [&](int i, int ln) { return ((wave * APH + i % APH) * 1024) / A_ROWB + ln / (A_ROWB / 16); };   // across
   auto b_k = [&](int i, int ln) { return ((wave * BPW + i) * 1024) / B_ROWB + ln / (B_ROWB / 16); };
   auto setup = [&](int item) {
     const GatedJob* jb = &p.j[0];
@@ -204,7 +207,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     for (int i = 0; i < APW; ++i) {
       if constexpr (A_ACROSS) {
         const int k = a_k(i, ln), c = (ln % (A_ROWB / 16)) ^ (across_swz<F32, A_ROWB>(k) * (16 / VE));
-        const int lc = c * VE, col = row0 + (lc / (TM / 2)) * TM + (i / (APW / 2)) * (TM / 2) + lc % (TM / 2);
+        const int lc = c * VE, col = row0 + (lc / (TM / NH)) * TM + (i / APH) * (TM / NH) + lc % (TM / NH);
         aoff[i] = col < row_end ? static_cast<uint32_t>((static_cast<int64_t>(k) * lda + col) * EB) : BUFFER_NOWHERE;
       } else {
         const int r = a_row(i) + ln / 8, kc = (ln % 8) ^ swz<8>(r);
@@ -244,14 +247,14 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     const unsigned char* const base = A_ACROSS ? abase + static_cast<int64_t>(kt) * (BK * EB) * lda : abase;
     const uint32_t soff = A_ACROSS ? 0u : static_cast<uint32_t>(kt) * 128;
     // (across: the columns of the waves' first halves, then of their second halves, BK rows of A_ROWB bytes each)
-    auto to = [&](int i) { return smem + stage * STAGE + (A_ACROSS ? h * (A_BYTES / 2) + (wave * (APW / 2) + i % (APW / 2)) * 1024 : a_row(i) * 128); };
+    auto to = [&](int i) { return smem + stage * STAGE + (A_ACROSS ? h * (A_BYTES / NH) + (wave * APH + i % APH) * 1024 : a_row(i) * 128); };
     if ((kt + 1) * BK <= k_all) {
 #pragma unroll
-      for (int i = h * (APW / 2); i < (h + 1) * (APW / 2); ++i) buffer_to_lds16(base, to(i), aoff[i], soff);
+      for (int i = h * APH; i < (h + 1) * APH; ++i) buffer_to_lds16(base, to(i), aoff[i], soff);
     } else {
       const int ln = lane_here();
 #pragma unroll
-      for (int i = h * (APW / 2); i < (h + 1) * (APW / 2); ++i) buffer_to_lds16(base, to(i), a_off(i, kt, ln), soff);
+      for (int i = h * APH; i < (h + 1) * APH; ++i) buffer_to_lds16(base, to(i), a_off(i, kt, ln), soff);
     }
   };
   auto issue_b = [&](int kt, int stage) {
@@ -271,7 +274,9 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     issue_b(kt, stage);
     issue_a(kt, stage, std::integral_constant<int, 0>{});
   };
-  auto issue_a1 = [&](int kt, int stage) { issue_a(kt, stage, std::integral_constant<int, 1>{}); };
+  auto issue_a1 = [&](int kt, int stage) {
+    if constexpr (NH > 1) issue_a(kt, stage, std::integral_constant<int, 1>{});
+  };
   auto issue_prologue = [&]() {
 #pragma unroll
     for (int t = 0; t < NS; ++t)
@@ -287,7 +292,8 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
   };
   auto wait_tiles = [&](int tiles, auto extra_c) {      // at most so many k-tiles, and `extra` copies, still in flight
     constexpr int x = decltype(extra_c)::value;
-    if (NS > 2 && tiles >= 2) wait_vm(std::integral_constant<int, 2 * LPW + x < 63 ? 2 * LPW + x : 63>{});
+    if (NS > 3 && tiles >= 3) wait_vm(std::integral_constant<int, 3 * LPW + x < 63 ? 3 * LPW + x : 63>{});
+    else if (NS > 2 && tiles >= 2) wait_vm(std::integral_constant<int, 2 * LPW + x < 63 ? 2 * LPW + x : 63>{});
     else if (tiles >= 1) wait_vm(std::integral_constant<int, LPW + x>{});
     else wait_vm(std::integral_constant<int, x>{});
   };
@@ -303,7 +309,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
   unsigned xa[A_ACROSS ? H : KS], wb[B_ACROSS ? NJ : KS];
   if constexpr (A_ACROSS) {
 #pragma unroll
-    for (int i = 0; i < H; ++i) xa[i] = lds0 + kin * A_ROWB + (((wave_m * (TM / 2) / 16 + i) ^ across_swz<F32, A_ROWB>(kin)) * UNITB) + in_unit;
+    for (int i = 0; i < H; ++i) xa[i] = lds0 + kin * A_ROWB + (((wave_m * H + i) ^ across_swz<F32, A_ROWB>(kin)) * UNITB) + in_unit;
   } else {
 #pragma unroll
     for (int s = 0; s < KS; ++s) xa[s] = lds0 + (wave_m * TM + l16) * 128 + (((s * 4 + lq) ^ swz<8>(l16)) << 4);
@@ -343,7 +349,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
         else wf[wbuf][t] = read_along(wb[s] + st + t * 16 * 128);
       }
       if (t < H) {
-        if constexpr (A_ACROSS) xf[xbuf][t] = read_across(xa[t] + st + half * (A_BYTES / 2) + s * KROWS * A_ROWB, std::integral_constant<int, A_ROWB>{});
+        if constexpr (A_ACROSS) xf[xbuf][t] = read_across(xa[t] + st + half * (A_BYTES / NH) + s * KROWS * A_ROWB, std::integral_constant<int, A_ROWB>{});
         else xf[xbuf][t] = read_along(xa[s] + st + (half * H + t) * 16 * 128);
       }
     }
@@ -386,11 +392,12 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
       for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     wait_vm(std::integral_constant<int, 0>{});
     lds_barrier();
-    constexpr int HS = 2 * KS;
+    constexpr int HS = NH * KS;
     using X0 = std::integral_constant<int, 0>;
-    using XA1 = std::integral_constant<int, APW / 2>;
-    // One k-tile (the order of its half-steps, copies and barriers is gemm_bf16_kernel's): W and the first halves of the rows are
-    // refilled with k-tile kt + NS while the second halves are multiplied, these behind a second barrier.
+    using XA1 = std::integral_constant<int, (NH - 1) * APH>;
+    // One k-tile (the order of its half-steps, copies and barriers is gemm_bf16_kernel's): B and the first halves of the rows are
+    // refilled with k-tile kt + NS while the second halves are multiplied, these behind a second barrier.  Without halves the whole stage
+    // is refilled ahead of the last step, when its fragments are in registers.
     auto k_tile = [&](auto stage_c, auto steady_c, int kt) {
       constexpr int stage = decltype(stage_c)::value;
       constexpr bool steady = decltype(steady_c)::value;
@@ -398,7 +405,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
       static_for<0, HS>([&](auto hs_c) {
         constexpr int hs = decltype(hs_c)::value;
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (hs == KS - 1) {
+        if constexpr (NH > 1 && hs == KS - 1) {
           if constexpr (steady) wait_tiles(NS - 1, X0{});
           else wait_tiles(nk - 1 - kt < NS - 1 ? nk - 1 - kt : NS - 1, X0{});
           lds_barrier();
@@ -407,10 +414,19 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
         }
         if constexpr (hs == HS - 1) {
           if (steady || kt + 1 < nk) {
-            if (steady || kt + NS < nk) wait_tiles(NS - 1, X0{});
-            else wait_tiles(nk - 2 - kt, XA1{});
+            if constexpr (NH > 1) {
+              if (steady || kt + NS < nk) wait_tiles(NS - 1, X0{});
+              else wait_tiles(nk - 2 - kt, XA1{});
+            } else {
+              // k-tile kt + 1 must have landed; in flight may be those after it, up to kt + NS - 1
+              if constexpr (steady) wait_tiles(NS - 2, X0{});
+              else wait_tiles(nk - 2 - kt < NS - 2 ? nk - 2 - kt : NS - 2, X0{});
+            }
             lds_barrier();
-            if (steady || kt + NS < nk) issue_a1(kt + NS, stage);
+            if (steady || kt + NS < nk) {
+              if constexpr (NH > 1) issue_a1(kt + NS, stage);
+              else issue_ba0(kt + NS, stage);
+            }
             __builtin_amdgcn_sched_barrier(0);
             load_frags(next, 0);
           }
