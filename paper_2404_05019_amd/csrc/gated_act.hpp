@@ -11,6 +11,8 @@ namespace scmoe {
 //   GELU, tanh  p = 1 / (1 + e^(-2 c (g + b g^3))): a = g p, s = p + g p (1 - p) 2 c (1 + 3 b g^2)
 // EXACT (fp32 storage): the library's exponential and error function and a division.  Otherwise (bf16) the hardware's exponential and
 // reciprocal (1 ulp each) and the polynomial of gelu.hpp, 2^-16 and better of what is rounded to 2^-8 on store.
+// ACT is a parameter of the kernels: as an argument every element had a branch of its own, and its exponential and reciprocal waited for
+// by themselves (gradient TODO).
 // g^2 is held below 1e8, where the products with p (1 - p) = 0 would be infinity times zero; an infinite g still gives what the
 // formula gives.
 template <bool EXACT>
@@ -19,44 +21,46 @@ __device__ __forceinline__ float sigmoid_of(float t_log2e, float t) {     // 1 /
   else return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-t_log2e));
 }
 
-template <bool EXACT>
-__device__ __forceinline__ float gated_act(float g, int mode) {
+template <bool EXACT, int ACT>
+__device__ __forceinline__ float gated_act(float g) {
   constexpr float LOG2E = 1.4426950408889634f;
-  if (mode == SCMOE_SILU) return g * sigmoid_of<EXACT>(g * LOG2E, g);
-  if (mode == SCMOE_GELU_TANH) {
+  if constexpr (ACT == SCMOE_SILU) {
+    return g * sigmoid_of<EXACT>(g * LOG2E, g);
+  } else if constexpr (ACT == SCMOE_GELU_TANH) {
     const float t = g * fmaf(0.07135481627f, g * g, 1.5957691216057308f);
     return g * sigmoid_of<EXACT>(t * LOG2E, t);
+  } else if constexpr (EXACT) {
+    return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
+  } else {
+    return gelu_erf_fast(g);
   }
-  if constexpr (EXACT) return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
-  else return gelu_erf_fast(g);
 }
 
-template <bool EXACT>
-__device__ __forceinline__ void gated_act_slope(float g, int mode, float& a, float& s) {
+template <bool EXACT, int ACT>
+__device__ __forceinline__ void gated_act_slope(float g, float& a, float& s) {
   constexpr float LOG2E = 1.4426950408889634f;
-  if (mode == SCMOE_SILU) {
+  if constexpr (ACT == SCMOE_SILU) {
     const float p = sigmoid_of<EXACT>(g * LOG2E, g);
     a = g * p;
     s = p * fmaf(g, 1.0f - p, 1.0f);
-    return;
-  }
-  if (mode == SCMOE_GELU_TANH) {
+  } else if constexpr (ACT == SCMOE_GELU_TANH) {
     const float g2 = fminf(g * g, 1e8f);
     const float t = g * fmaf(0.07135481627f, g2, 1.5957691216057308f);
     const float p = sigmoid_of<EXACT>(t * LOG2E, t);
     a = g * p;
     s = fmaf(a * (1.0f - p), fmaf(0.21406444881f, g2, 1.5957691216057308f), p);
-    return;
-  }
-  const float g2 = g * g;
-  if constexpr (EXACT) {
-    const float p = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
-    a = g * p;
-    s = fmaf(g * 0.3989422804014327f, expf(-0.5f * g2), p);
   } else {
-    const float p = normal_cdf_fast(g);
+    const float g2 = g * g;
+    float p, e;
+    if constexpr (EXACT) {
+      p = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
+      e = expf(-0.5f * g2);
+    } else {
+      p = normal_cdf_fast(g);
+      e = __builtin_amdgcn_exp2f(-0.5f * LOG2E * g2);
+    }
     a = g * p;
-    s = fmaf(g * 0.3989422804014327f, __builtin_amdgcn_exp2f(-0.5f * LOG2E * g2), p);
+    s = fmaf(g * 0.3989422804014327f, e, p);
   }
 }
 

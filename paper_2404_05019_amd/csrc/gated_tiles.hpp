@@ -94,6 +94,19 @@ __device__ __forceinline__ g_u32x2 lds_read_transposed(uint32_t at) {
   return lds_read_transposed(reinterpret_cast<lds8_ptr>(static_cast<uintptr_t>(at)), reinterpret_cast<lds8_ptr>(static_cast<uintptr_t>(at + 64)));
 }
 
+// Stores of 16, 8, 4 and 1 bytes to base + off; an offset of BUFFER_NOWHERE stores nothing.  No branch: behind stores under a condition,
+// which it cannot count, the compiler would make every later load's wait one for these stores as well.
+template <class V>
+__device__ __forceinline__ void buffer_put(unsigned char* base, uint32_t off, V v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_make_buffer_rsrc(base, 0, static_cast<uint32_t>(BUFFER_SPAN), 0x00020000);
+  if constexpr (sizeof(V) == 16) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(g_u32x4, v), r, off, 0, 0);
+  else if constexpr (sizeof(V) == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(g_u32x2, v), r, off, 0, 0);
+  else if constexpr (sizeof(V) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), r, off, 0, 0);
+  else __builtin_amdgcn_raw_buffer_store_b8(v, r, off, 0, 0);
+#endif
+}
+
 // The largest value over the four lanes that hold 16 columns each of a row's 32 (lanes l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ uint32_t max_over_lq(uint32_t v) {
   const g_u32x2 a = __builtin_bit_cast(g_u32x2, __builtin_amdgcn_permlane32_swap(v, v, false, false));
@@ -122,7 +135,7 @@ __device__ __forceinline__ void load4(const unsigned char* p, float* v) {
   }
 }
 
-template <class CFG, int MODE, int KEEP>
+template <class CFG, int MODE, int KEEP, int ACT>
 __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void gated_kernel(const GatedArgs p) {
   constexpr bool F32 = CFG::F32;
   constexpr int BM = CFG::BM, BN = CFG::BN, EB = CFG::EB, VE = CFG::VE, BK = CFG::BK, KS = CFG::KS, NS = CFG::NS;
@@ -242,13 +255,14 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     const int k = B_ACROSS ? b_k(i, ln) : ((ln % 8) ^ swz<8>((wave * BPW + i) * 8 + ln / 8)) * VE;
     return kt * BK + k < k_all ? boff[i] : BUFFER_NOWHERE;
   };
-  auto issue_a = [&](int kt, int stage, auto half_c) {
+  // whole_c: the k-tile is known to be whole
+  auto issue_a = [&](int kt, int stage, auto half_c, auto whole_c) {
     constexpr int h = decltype(half_c)::value;
     const unsigned char* const base = A_ACROSS ? abase + static_cast<int64_t>(kt) * (BK * EB) * lda : abase;
     const uint32_t soff = A_ACROSS ? 0u : static_cast<uint32_t>(kt) * 128;
     // (across: the columns of the waves' first halves, then of their second halves, BK rows of A_ROWB bytes each)
     auto to = [&](int i) { return smem + stage * STAGE + (A_ACROSS ? h * (A_BYTES / NH) + (wave * APH + i % APH) * 1024 : a_row(i) * 128); };
-    if ((kt + 1) * BK <= k_all) {
+    if (decltype(whole_c)::value || (kt + 1) * BK <= k_all) {
 #pragma unroll
       for (int i = h * APH; i < (h + 1) * APH; ++i) buffer_to_lds16(base, to(i), aoff[i], soff);
     } else {
@@ -257,11 +271,11 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
       for (int i = h * APH; i < (h + 1) * APH; ++i) buffer_to_lds16(base, to(i), a_off(i, kt, ln), soff);
     }
   };
-  auto issue_b = [&](int kt, int stage) {
+  auto issue_b = [&](int kt, int stage, auto whole_c) {
     const unsigned char* const base = B_ACROSS ? bbase + static_cast<int64_t>(kt) * (BK * EB) * ldb : bbase;
     const uint32_t soff = B_ACROSS ? 0u : static_cast<uint32_t>(kt) * 128;
     unsigned char* const to = smem + stage * STAGE + A_BYTES + wave * BPW * 1024;
-    if ((kt + 1) * BK <= k_all) {
+    if (decltype(whole_c)::value || (kt + 1) * BK <= k_all) {
 #pragma unroll
       for (int i = 0; i < BPW; ++i) buffer_to_lds16(base, to + i * 1024, boff[i], soff);
     } else {
@@ -270,19 +284,19 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
       for (int i = 0; i < BPW; ++i) buffer_to_lds16(base, to + i * 1024, b_off(i, kt, ln), soff);
     }
   };
-  auto issue_ba0 = [&](int kt, int stage) {
-    issue_b(kt, stage);
-    issue_a(kt, stage, std::integral_constant<int, 0>{});
+  auto issue_ba0 = [&](int kt, int stage, auto whole_c) {
+    issue_b(kt, stage, whole_c);
+    issue_a(kt, stage, std::integral_constant<int, 0>{}, whole_c);
   };
-  auto issue_a1 = [&](int kt, int stage) {
-    if constexpr (NH > 1) issue_a(kt, stage, std::integral_constant<int, 1>{});
+  auto issue_a1 = [&](int kt, int stage, auto whole_c) {
+    if constexpr (NH > 1) issue_a(kt, stage, std::integral_constant<int, 1>{}, whole_c);
   };
   auto issue_prologue = [&]() {
 #pragma unroll
     for (int t = 0; t < NS; ++t)
       if (t < nk) {
-        issue_ba0(t, t);
-        issue_a1(t, t);
+        issue_ba0(t, t, std::false_type{});
+        issue_a1(t, t, std::false_type{});
       }
   };
   auto wait_vm = [&](auto n_c) {
@@ -400,7 +414,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     // is refilled ahead of the last step, when its fragments are in registers.
     auto k_tile = [&](auto stage_c, auto steady_c, int kt) {
       constexpr int stage = decltype(stage_c)::value;
-      constexpr bool steady = decltype(steady_c)::value;
+      constexpr bool steady = decltype(steady_c)::value;      // k-tiles kt + 1 .. kt + NS all exist, and are whole
       constexpr int next = stage + 1 == NS ? 0 : stage + 1;
       static_for<0, HS>([&](auto hs_c) {
         constexpr int hs = decltype(hs_c)::value;
@@ -409,7 +423,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
           if constexpr (steady) wait_tiles(NS - 1, X0{});
           else wait_tiles(nk - 1 - kt < NS - 1 ? nk - 1 - kt : NS - 1, X0{});
           lds_barrier();
-          if (steady || kt + NS < nk) issue_ba0(kt + NS, stage);
+          if (steady || kt + NS < nk) issue_ba0(kt + NS, stage, steady_c);
           __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (hs == HS - 1) {
@@ -424,8 +438,8 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
             }
             lds_barrier();
             if (steady || kt + NS < nk) {
-              if constexpr (NH > 1) issue_a1(kt + NS, stage);
-              else issue_ba0(kt + NS, stage);
+              if constexpr (NH > 1) issue_a1(kt + NS, stage, steady_c);
+              else issue_ba0(kt + NS, stage, steady_c);
             }
             __builtin_amdgcn_sched_barrier(0);
             load_frags(next, 0);
@@ -444,7 +458,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     if (nk > 0) {
       load_frags(0, 0);
       int kt = 0;
-      for (; kt + 2 * NS <= nk; kt += NS) static_for<0, NS>([&](auto s) { k_tile(s, bool_constant<true>{}, kt + decltype(s)::value); });
+      for (; kt + 2 * NS <= k_all / BK; kt += NS) static_for<0, NS>([&](auto s) { k_tile(s, bool_constant<true>{}, kt + decltype(s)::value); });
       for (; kt < nk; kt += NS)
         static_for<0, NS>([&](auto s) {
           if (kt + decltype(s)::value < nk) k_tile(s, bool_constant<false>{}, kt + decltype(s)::value);
@@ -495,7 +509,12 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     // bf16: rows are put together in the wave's patch of LDS, a subtile of 16 rows at a time, and leave it as whole lines.
     unsigned char* const patch = smem + NS * STAGE + wave * CFG::PATCH;
     if constexpr (!F32) {
-      auto out16 = [&](unsigned char* at, g_u32x4 v) { *reinterpret_cast<g_u32x4*>(at) = v; };
+      // offsets from the tile's first row: they fit 32 bits (GATED_MOST_LD)
+      unsigned char* const obase = cC + (MODE == G_DW ? static_cast<int64_t>(ce) * jc.M + crow0 : static_cast<int64_t>(crow0)) * cldc * 2;
+      unsigned char* const kbase = p.pre + static_cast<int64_t>(crow0) * (KEEP == KEEP_8BIT ? 2 * p.ldpre : p.ldpre * 2);
+      unsigned char* const dbase = p.dpre + static_cast<int64_t>(crow0) * p.lddpre * 2;
+      const uint32_t ostep = static_cast<uint32_t>(cldc) * 2, kstep = static_cast<uint32_t>(KEEP == KEEP_8BIT ? p.ldpre : p.ldpre * 2), dstep = static_cast<uint32_t>(p.lddpre) * 2;
+      const uint32_t ubytes = static_cast<uint32_t>(cN) * 2;   // from g to u of a row
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
         const int rbase = crow0 + wave_m * TM + i * 16;
@@ -537,19 +556,18 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
               float a, s;
-              gated_act_slope<F32>(g[q], p.act, a, s);
+              gated_act_slope<F32, ACT>(g[q], a, s);
               h[q] = a * u[q];
               g[q] = dh[q] * u[q] * s;
               u[q] = dh[q] * a;
             }
             auto pack8 = [&](const float* v) { return g_u32x4{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])}; };
             const g_u32x4 oh = pack8(h), og = pack8(g), ou = pack8(u);
-            if (r < crow_end && pn < cN) {
-              out16(cC + (static_cast<int64_t>(r) * cldc + pn) * 2, oh);
-              unsigned char* const to = p.dpre + (static_cast<int64_t>(r) * p.lddpre + pn) * 2;
-              out16(to, og);
-              out16(to + static_cast<int64_t>(cN) * 2, ou);
-            }
+            const bool in = r < crow_end && pn < cN;
+            buffer_put(obase, in ? static_cast<uint32_t>(r - crow0) * ostep + pn * 2 : BUFFER_NOWHERE, oh);
+            const uint32_t to = static_cast<uint32_t>(r - crow0) * dstep + pn * 2;
+            buffer_put(dbase, in ? to : BUFFER_NOWHERE, og);
+            buffer_put(dbase, in ? to + ubytes : BUFFER_NOWHERE, ou);
           }
         } else if constexpr (MODE == G_GATE) {
           // 32 columns a wave: hidden, g, u in 16 rows of 64 bytes each (in 8 bits: of 32), one behind the other
@@ -576,7 +594,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
             float h[4];
             const f32x4_t g = acc[i][j], u = acc[i][J2 + j];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) h[q] = gated_act<F32>(g[q], p.act) * u[q];
+            for (int q = 0; q < 4; ++q) h[q] = gated_act<F32, ACT>(g[q]) * u[q];
             const int at = l16 * 64 + (((j * 2 + (lq >> 1)) ^ sw) << 4) + (lq & 1) * 8;
             *reinterpret_cast<uint2*>(patch + at) = make_uint2(cvt_pk_bf16(h[0], h[1]), cvt_pk_bf16(h[2], h[3]));
             if constexpr (KEEP == KEEP_FULL) {
@@ -591,26 +609,24 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
           {
             const int rr = le >> 2, c = le & 3, r = rbase + rr, f = f0 + c * 8;
             const int at = rr * 64 + ((c ^ ((rr >> 1) & 3)) << 4);
-            if (r < crow_end && f < cN) {
-              out16(cC + (static_cast<int64_t>(r) * cldc + f) * 2, *reinterpret_cast<const g_u32x4*>(patch + at));
-              if constexpr (KEEP == KEEP_FULL) {
-                unsigned char* const to = p.pre + (static_cast<int64_t>(r) * p.ldpre + f) * 2;
-                out16(to, *reinterpret_cast<const g_u32x4*>(patch + 1024 + at));
-                out16(to + static_cast<int64_t>(cN) * 2, *reinterpret_cast<const g_u32x4*>(patch + 2048 + at));
-              }
+            const bool in = r < crow_end && f < cN;
+            buffer_put(obase, in ? static_cast<uint32_t>(r - crow0) * ostep + f * 2 : BUFFER_NOWHERE, *reinterpret_cast<const g_u32x4*>(patch + at));
+            if constexpr (KEEP == KEEP_FULL) {
+              const uint32_t to = static_cast<uint32_t>(r - crow0) * kstep + f * 2;
+              buffer_put(kbase, in ? to : BUFFER_NOWHERE, *reinterpret_cast<const g_u32x4*>(patch + 1024 + at));
+              buffer_put(kbase, in ? to + ubytes : BUFFER_NOWHERE, *reinterpret_cast<const g_u32x4*>(patch + 2048 + at));
             }
           }
           if constexpr (KEEP == KEEP_8BIT) {
-            // lane l: 16 codes, half l % 2 of row l / 2 % 16 of g (lanes 0 .. 31) or u
+            // lane l: 16 codes, half l % 2 of row l / 2 % 16 of g (lanes 0 .. 31) or u; the width is a multiple of 8
             const int t = le >> 5, rr = (le >> 1) & 15, c = le & 1, r = rbase + rr, f = f0 + c * 16;
-            unsigned char* const row = p.pre + (2 * static_cast<int64_t>(r) + t) * p.ldpre;
-            if (r < crow_end && f < cN) {
-              const unsigned char* const from = patch + 1024 + t * 512 + rr * 32 + c * 16;
-              if (f + 16 <= cN) *reinterpret_cast<g_u32x4*>(row + f) = *reinterpret_cast<const g_u32x4*>(from);
-              else *reinterpret_cast<uint2*>(row + f) = *reinterpret_cast<const uint2*>(from);      // (the width is a multiple of 8)
-            }
-            if (lq < 2 && rbase + l16 < crow_end && f0 < cN)
-              p.pre[(2 * static_cast<int64_t>(rbase + l16) + lq) * p.ldpre + cN + f0 / CKPT_BLOCK] = static_cast<unsigned char>(lq == 0 ? byte[0] : byte[1]);
+            const unsigned char* const from = patch + 1024 + t * 512 + rr * 32 + c * 16;
+            const g_u32x4 codes = *reinterpret_cast<const g_u32x4*>(from);
+            const uint32_t to = (2 * static_cast<uint32_t>(r - crow0) + t) * kstep + f;
+            buffer_put(kbase, r < crow_end && f + 16 <= cN ? to : BUFFER_NOWHERE, codes);
+            buffer_put(kbase, r < crow_end && f + 8 == cN ? to : BUFFER_NOWHERE, g_u32x2{codes[0], codes[1]});
+            const uint32_t ts = (2 * static_cast<uint32_t>(rbase + l16 - crow0) + lq) * kstep + cN + f0 / CKPT_BLOCK;
+            buffer_put(kbase, lq < 2 && rbase + l16 < crow_end && f0 < cN ? ts : BUFFER_NOWHERE, static_cast<unsigned char>(lq == 0 ? byte[0] : byte[1]));
           }
         } else {
           unsigned char* const half = patch + (i & 1) * 2048;   // 16 rows of 128 bytes
@@ -623,8 +639,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
           for (int t = 0; t < 2; ++t) {
             const int rr = t * 8 + pr, r = rbase + rr;
             const g_u32x4 v = *reinterpret_cast<const g_u32x4*>(half + rr * 128 + ((pc ^ swz<8>(rr)) << 4));
-            const int64_t row = MODE == G_DW ? static_cast<int64_t>(ce) * jc.M + r : r;
-            if (r < crow_end && pn < cN) out16(cC + (row * cldc + pn) * 2, v);
+            buffer_put(obase, r < crow_end && pn < cN ? static_cast<uint32_t>(r - crow0) * ostep + pn * 2 : BUFFER_NOWHERE, v);
           }
         }
       }
@@ -645,7 +660,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
           for (int q = 0; q < 4; ++q) {
             g[q] = acc[i][j][q];
             u[q] = acc[i][J2 + j][q];
-            h[q] = gated_act<F32>(g[q], p.act) * u[q];
+            h[q] = gated_act<F32, ACT>(g[q]) * u[q];
           }
           if (in && f < cN) {
             store4<F32>(cC + (static_cast<int64_t>(r) * cldc + f) * EB, h);
@@ -698,7 +713,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               float a, s;
-              gated_act_slope<F32>(g[q], p.act, a, s);
+              gated_act_slope<F32, ACT>(g[q], a, s);
               h[q] = a * u[q];
               du[q] = v[q] * a;
               dg[q] = v[q] * u[q] * s;
@@ -721,13 +736,13 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
 
 // ---- host side ----------------------------------------------------------------------------------------------
 
-template <class CFG, int MODE, int KEEP>
+template <class CFG, int MODE, int KEEP, int ACT>
 static int launch_gated_cfg(GatedArgs a, int64_t max_rows, hipStream_t stream) {
   static std::atomic<bool> attr_set[64];
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = -1;
   if (dev < 0 || !attr_set[dev].load(std::memory_order_acquire)) {
-    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(&gated_kernel<CFG, MODE, KEEP>), hipFuncAttributeMaxDynamicSharedMemorySize, CFG::LDS);
+    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(&gated_kernel<CFG, MODE, KEEP, ACT>), hipFuncAttributeMaxDynamicSharedMemorySize, CFG::LDS);
     if (err != hipSuccess) return hip_fail(err);
     if (dev >= 0) attr_set[dev].store(true, std::memory_order_release);
   }
@@ -749,7 +764,7 @@ static int launch_gated_cfg(GatedArgs a, int64_t max_rows, hipStream_t stream) {
   const int resident = (num_cus() / 8) * CFG::WG_PER_CU;
   if (slots > resident) slots = resident;
   if (slots < 1) slots = 1;
-  hipLaunchKernelGGL((gated_kernel<CFG, MODE, KEEP>), dim3(static_cast<unsigned>(8 * slots)), dim3(CFG::THREADS), CFG::LDS, stream, a);
+  hipLaunchKernelGGL((gated_kernel<CFG, MODE, KEEP, ACT>), dim3(static_cast<unsigned>(8 * slots)), dim3(CFG::THREADS), CFG::LDS, stream, a);
   return launch_status();
 }
 
@@ -757,18 +772,27 @@ static int launch_gated_cfg(GatedArgs a, int64_t max_rows, hipStream_t stream) {
 int launch_gated_bf16(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream);
 int launch_gated_f32(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream);
 
+template <class CFG, int MODE, int KEEP>
+static int launch_gated_act(const GatedArgs& a, int64_t max_rows, hipStream_t stream) {
+  switch (a.act) {
+    case SCMOE_SILU: return launch_gated_cfg<CFG, MODE, KEEP, SCMOE_SILU>(a, max_rows, stream);
+    case SCMOE_GELU_TANH: return launch_gated_cfg<CFG, MODE, KEEP, SCMOE_GELU_TANH>(a, max_rows, stream);
+    default: return launch_gated_cfg<CFG, MODE, KEEP, SCMOE_GELU_ERF>(a, max_rows, stream);
+  }
+}
+
 template <class CFG>
 static int launch_gated_mode(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream) {
   switch (mode) {
     case G_GATE:
-      return keep == KEEP_NONE ? launch_gated_cfg<CFG, G_GATE, KEEP_NONE>(a, max_rows, stream)
-             : keep == KEEP_FULL ? launch_gated_cfg<CFG, G_GATE, KEEP_FULL>(a, max_rows, stream)
-                                 : launch_gated_cfg<CFG, G_GATE, KEEP_8BIT>(a, max_rows, stream);
+      return keep == KEEP_NONE ? launch_gated_act<CFG, G_GATE, KEEP_NONE>(a, max_rows, stream)
+             : keep == KEEP_FULL ? launch_gated_act<CFG, G_GATE, KEEP_FULL>(a, max_rows, stream)
+                                 : launch_gated_act<CFG, G_GATE, KEEP_8BIT>(a, max_rows, stream);
     case G_DH:
-      return keep == KEEP_FULL ? launch_gated_cfg<CFG, G_DH, KEEP_FULL>(a, max_rows, stream) : launch_gated_cfg<CFG, G_DH, KEEP_8BIT>(a, max_rows, stream);
-    case G_DOWN: return launch_gated_cfg<CFG, G_DOWN, KEEP_NONE>(a, max_rows, stream);
-    case G_DX: return launch_gated_cfg<CFG, G_DX, KEEP_NONE>(a, max_rows, stream);
-    default: return launch_gated_cfg<CFG, G_DW, KEEP_NONE>(a, max_rows, stream);
+      return keep == KEEP_FULL ? launch_gated_act<CFG, G_DH, KEEP_FULL>(a, max_rows, stream) : launch_gated_act<CFG, G_DH, KEEP_8BIT>(a, max_rows, stream);
+    case G_DOWN: return launch_gated_cfg<CFG, G_DOWN, KEEP_NONE, 0>(a, max_rows, stream);
+    case G_DX: return launch_gated_cfg<CFG, G_DX, KEEP_NONE, 0>(a, max_rows, stream);
+    default: return launch_gated_cfg<CFG, G_DW, KEEP_NONE, 0>(a, max_rows, stream);
   }
 }
 
