@@ -77,7 +77,7 @@ enum { SCMOE_CG_NONE = 0, SCMOE_CG_1 = 1, SCMOE_CG_2 = 2 };
 /* Upper limit on the width of a normed row. */
 #define SCMOE_MAX_NORM_WIDTH 16384
 /* Upper limit on the model and the hidden width of a gated feed-forward block. */
-#define SCMOE_MAX_GATED_WIDTH (1 << 20)
+#define SCMOE_MAX_GATED_WIDTH (1 << 17)
 /* Upper limit on its packed rows. */
 #define SCMOE_MAX_GATED_ROWS (1 << 30)
 
@@ -614,7 +614,7 @@ int scmoe_gated_ffn_workspace_bytes(int32_t dtype, int32_t d, int32_t F, size_t*
  * touched; E = 1 and offsets = {0, T} is a dense block).  W1: [E, 2 F, d] with row stride ldw1, W2:
  * [E, d, F] with row stride ldw2.  act: SCMOE_SILU, SCMOE_GELU_ERF or SCMOE_GELU_TANH.  d and F are
  * multiples of 8, up to SCMOE_MAX_GATED_WIDTH, max_rows up to SCMOE_MAX_GATED_ROWS; row strides of up to
- * 2^21 elements, an expert's W1 and W2 of less than 3.75 GiB each, and no product of more than 2^30 tiles
+ * 2^18 elements (checkpoint rows: bytes), an expert's W1 and W2 of less than 3.75 GiB each, and no product of more than 2^30 tiles
  * of 128 x 64 outputs, else SCMOE_ERR_SHAPE.
  * pre_keep: what stays of g and u for scmoe_gated_ffn_backward.
  *   SCMOE_KEEP_NOTHING  nothing (serving); pre is not looked at

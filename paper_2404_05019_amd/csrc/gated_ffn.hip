@@ -6,8 +6,11 @@
 
 namespace scmoe {
 
-// An operand's row stride that keeps 32-bit offsets inside a tile (at most 256 rows of it) inside the buffer.
-constexpr int64_t GATED_MOST_LD = 1 << 21;
+// A row stride with which 32-bit offsets inside a tile (at most 256 rows) stay inside the buffer, and BUFFER_NOWHERE and the offset of a
+// wave tile's row (at most 127 rows, of two checkpoint rows each) below 2^32.
+constexpr int64_t GATED_MOST_LD = 1 << 18;
+static_assert(BUFFER_NOWHERE + 127ull * 2 * GATED_MOST_LD < (1ull << 32) && 256ll * 4 * GATED_MOST_LD < BUFFER_SPAN);
+static_assert(BUFFER_NOWHERE + 127ull * 2 * (2 * SCMOE_MAX_GATED_WIDTH + 64) < (1ull << 32));   // (the workspace's padded rows)
 static bool gated_view_ok(const void* p, int64_t ld, int64_t cols, int dtype) { return view_ok(p, ld, cols, dtype) && ld <= GATED_MOST_LD; }
 
 static int launch_gated(const GatedArgs& a, int mode, int keep, int64_t max_rows, int dtype, hipStream_t stream) {

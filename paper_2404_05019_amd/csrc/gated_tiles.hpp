@@ -94,16 +94,30 @@ __device__ __forceinline__ g_u32x2 lds_read_transposed(uint32_t at) {
   return lds_read_transposed(reinterpret_cast<lds8_ptr>(static_cast<uintptr_t>(at)), reinterpret_cast<lds8_ptr>(static_cast<uintptr_t>(at + 64)));
 }
 
-// Stores of 16, 8, 4 and 1 bytes to base + off; an offset of BUFFER_NOWHERE stores nothing.  No branch: behind stores under a condition,
-// which it cannot count, the compiler would make every later load's wait one for these stores as well.
+// Stores of 16, 8 and 1 bytes to base + off; loads from base + off + step.  base and step are the same for the wave; an offset of
+// BUFFER_NOWHERE stores nothing and reads zeros.  No branch: behind stores under a condition, which it cannot count, the compiler would
+// make every later load's wait one for these stores as well.  (BUFFER_NOWHERE + step does not wrap: GATED_MOST_LD.)
+// The stores take no step in a scalar register: a store of more than 8 bytes a lane still reads its data when the next instruction
+// issues, and the compiler keeps that instruction from writing the data's registers only where the scalar offset is a constant (with a
+// register, now and then the first four bytes of a lane's sixteen were others).
 template <class V>
 __device__ __forceinline__ void buffer_put(unsigned char* base, uint32_t off, V v) {
 #if defined(__HIP_DEVICE_COMPILE__)
   const auto r = __builtin_amdgcn_make_buffer_rsrc(base, 0, static_cast<uint32_t>(BUFFER_SPAN), 0x00020000);
   if constexpr (sizeof(V) == 16) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(g_u32x4, v), r, off, 0, 0);
   else if constexpr (sizeof(V) == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(g_u32x2, v), r, off, 0, 0);
-  else if constexpr (sizeof(V) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), r, off, 0, 0);
   else __builtin_amdgcn_raw_buffer_store_b8(v, r, off, 0, 0);
+#endif
+}
+template <class V>
+__device__ __forceinline__ V buffer_get(const unsigned char* base, uint32_t off, uint32_t step) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, static_cast<uint32_t>(BUFFER_SPAN), 0x00020000);
+  if constexpr (sizeof(V) == 16) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(r, off, step, 0));
+  else if constexpr (sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(r, off, step, 0));
+  else return __builtin_amdgcn_raw_buffer_load_b8(r, off, step, 0);
+#else
+  return V{};
 #endif
 }
 
@@ -474,27 +488,37 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     const int itn = MODE == G_DW ? it + nslots : sched.next(it);
     const bool more = itn < items;
     // bf16: an output row's 16-byte pieces as a wave stores them, 8 rows at a time: lane l has piece l % 8 of row l / 8, and of row
-    // 8 + l / 8, of a subtile of 16 rows
+    // 8 + l / 8, of a subtile of 16 rows.  Offsets are from the wave tile's first row.
     const int le = lane_here(), pr = le >> 3, pc = le & 7;
     const int l16 = le & 15, lq = le >> 4;
     const int pn = cn0 + wave_n * TN + pc * 8;                 // its first column
-    // DH: g and u of a subtile's pieces (8 bits: codes, and the block's scale), a subtile ahead of their use
+    const int wrow0 = crow0 + wave_m * TM, left = crow_end - wrow0;           // rows that the wave tile has
+    unsigned char* const obase = cC + (MODE == G_DW ? static_cast<int64_t>(ce) * jc.M + wrow0 : static_cast<int64_t>(wrow0)) * cldc * EB;
+    unsigned char* const kbase = p.pre + static_cast<int64_t>(wrow0) * (KEEP == KEEP_8BIT ? 2 * p.ldpre : p.ldpre * EB);
+    unsigned char* const dbase = p.dpre + static_cast<int64_t>(wrow0) * p.lddpre * EB;
+    const uint32_t ostep = static_cast<uint32_t>(cldc) * EB, dstep = static_cast<uint32_t>(p.lddpre) * EB;
+    const uint32_t kstep = KEEP == KEEP_8BIT ? static_cast<uint32_t>(p.ldpre) * 2 : static_cast<uint32_t>(p.ldpre) * EB;   // of a row: two checkpoint rows
+    const uint32_t ubytes = KEEP == KEEP_8BIT ? static_cast<uint32_t>(p.ldpre) : static_cast<uint32_t>(cN) * EB;         // from g to u
+    const uint32_t dubytes = static_cast<uint32_t>(cN) * EB;
+    auto if_in = [&](bool in, uint32_t off) { return in ? off : BUFFER_NOWHERE; };
+    // DH: g and u of a subtile's pieces (8 bits: codes, and the blocks' scales), a subtile ahead of their use
     g_u32x4 kg[2][2], ku[2][2];
     auto load_kept = [&](int i) {
       if constexpr (MODE == G_DH && !F32) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          // (rows past the segment and columns past the matrix: the last ones again, for no store)
-          const int rk = crow0 + wave_m * TM + i * 16 + t * 8 + pr, r = rk < crow_end ? rk : crow_end - 1, n = pn < cN ? pn : cN - 8;
+          const int rr = i * 16 + t * 8;
+          const bool in = rr + pr < left && pn < cN;
           if constexpr (KEEP == KEEP_8BIT) {
-            const unsigned char* row = p.pre + 2 * static_cast<int64_t>(r) * p.ldpre;
-            const uint2 a = *reinterpret_cast<const uint2*>(row + n), b = *reinterpret_cast<const uint2*>(row + p.ldpre + n);
-            kg[i & 1][t] = g_u32x4{a.x, a.y, row[cN + n / CKPT_BLOCK], row[p.ldpre + cN + n / CKPT_BLOCK]};
-            ku[i & 1][t] = g_u32x4{b.x, b.y, 0, 0};
+            const uint32_t row = static_cast<uint32_t>(pr) * kstep, step = static_cast<uint32_t>(rr) * kstep;
+            const uint32_t codes = if_in(in, row + pn), scale = if_in(in, row + cN + pn / CKPT_BLOCK);
+            const g_u32x2 a = buffer_get<g_u32x2>(kbase, codes, step), b = buffer_get<g_u32x2>(kbase + ubytes, codes, step);
+            kg[i & 1][t] = g_u32x4{a[0], a[1], buffer_get<unsigned char>(kbase, scale, step), buffer_get<unsigned char>(kbase + ubytes, scale, step)};
+            ku[i & 1][t] = g_u32x4{b[0], b[1], 0, 0};
           } else {
-            const unsigned char* row = p.pre + (static_cast<int64_t>(r) * p.ldpre + n) * 2;
-            kg[i & 1][t] = *reinterpret_cast<const g_u32x4*>(row);
-            ku[i & 1][t] = *reinterpret_cast<const g_u32x4*>(row + static_cast<int64_t>(cN) * 2);
+            const uint32_t off = if_in(in, static_cast<uint32_t>(pr) * kstep + pn * EB), step = static_cast<uint32_t>(rr) * kstep;
+            kg[i & 1][t] = buffer_get<g_u32x4>(kbase, off, step);
+            ku[i & 1][t] = buffer_get<g_u32x4>(kbase + ubytes, off, step);
           }
         }
       }
@@ -509,16 +533,9 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     // bf16: rows are put together in the wave's patch of LDS, a subtile of 16 rows at a time, and leave it as whole lines.
     unsigned char* const patch = smem + NS * STAGE + wave * CFG::PATCH;
     if constexpr (!F32) {
-      // offsets from the tile's first row: they fit 32 bits (GATED_MOST_LD)
-      unsigned char* const obase = cC + (MODE == G_DW ? static_cast<int64_t>(ce) * jc.M + crow0 : static_cast<int64_t>(crow0)) * cldc * 2;
-      unsigned char* const kbase = p.pre + static_cast<int64_t>(crow0) * (KEEP == KEEP_8BIT ? 2 * p.ldpre : p.ldpre * 2);
-      unsigned char* const dbase = p.dpre + static_cast<int64_t>(crow0) * p.lddpre * 2;
-      const uint32_t ostep = static_cast<uint32_t>(cldc) * 2, kstep = static_cast<uint32_t>(KEEP == KEEP_8BIT ? p.ldpre : p.ldpre * 2), dstep = static_cast<uint32_t>(p.lddpre) * 2;
-      const uint32_t ubytes = static_cast<uint32_t>(cN) * 2;   // from g to u of a row
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
-        const int rbase = crow0 + wave_m * TM + i * 16;
-        if (rbase >= crow_end) break;                          // (wave-uniform)
+        if (i * 16 >= left) break;                             // (wave-uniform)
         wave_lds_order();                                      // (the patch has been read)
         __builtin_amdgcn_sched_barrier(0);                     // (a subtile at a time: several take registers that are not there)
         if constexpr (MODE == G_DH) {
@@ -529,7 +546,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
           wave_lds_order();
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            const int rr = t * 8 + pr, r = rbase + rr;
+            const int rr = t * 8 + pr;
             float dh[8], g[8], u[8], h[8];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
@@ -563,11 +580,11 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
             }
             auto pack8 = [&](const float* v) { return g_u32x4{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])}; };
             const g_u32x4 oh = pack8(h), og = pack8(g), ou = pack8(u);
-            const bool in = r < crow_end && pn < cN;
-            buffer_put(obase, in ? static_cast<uint32_t>(r - crow0) * ostep + pn * 2 : BUFFER_NOWHERE, oh);
-            const uint32_t to = static_cast<uint32_t>(r - crow0) * dstep + pn * 2;
-            buffer_put(dbase, in ? to : BUFFER_NOWHERE, og);
-            buffer_put(dbase, in ? to + ubytes : BUFFER_NOWHERE, ou);
+            const bool in = i * 16 + rr < left && pn < cN;
+            buffer_put(obase + static_cast<int64_t>(i * 16 + t * 8) * ostep, if_in(in, static_cast<uint32_t>(pr) * ostep + pn * 2), oh);
+            const uint32_t to = if_in(in, static_cast<uint32_t>(pr) * dstep + pn * 2);
+            buffer_put(dbase + static_cast<int64_t>(i * 16 + t * 8) * dstep, to, og);
+            buffer_put(dbase + dubytes + static_cast<int64_t>(i * 16 + t * 8) * dstep, to, ou);
           }
         } else if constexpr (MODE == G_GATE) {
           // 32 columns a wave: hidden, g, u in 16 rows of 64 bytes each (in 8 bits: of 32), one behind the other
@@ -607,26 +624,26 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
           }
           wave_lds_order();
           {
-            const int rr = le >> 2, c = le & 3, r = rbase + rr, f = f0 + c * 8;
+            const int rr = le >> 2, c = le & 3, f = f0 + c * 8;
             const int at = rr * 64 + ((c ^ ((rr >> 1) & 3)) << 4);
-            const bool in = r < crow_end && f < cN;
-            buffer_put(obase, in ? static_cast<uint32_t>(r - crow0) * ostep + f * 2 : BUFFER_NOWHERE, *reinterpret_cast<const g_u32x4*>(patch + at));
+            const bool in = i * 16 + rr < left && f < cN;
+            buffer_put(obase + static_cast<int64_t>(i * 16) * ostep, if_in(in, static_cast<uint32_t>(rr) * ostep + f * 2), *reinterpret_cast<const g_u32x4*>(patch + at));
             if constexpr (KEEP == KEEP_FULL) {
-              const uint32_t to = static_cast<uint32_t>(r - crow0) * kstep + f * 2;
-              buffer_put(kbase, in ? to : BUFFER_NOWHERE, *reinterpret_cast<const g_u32x4*>(patch + 1024 + at));
-              buffer_put(kbase, in ? to + ubytes : BUFFER_NOWHERE, *reinterpret_cast<const g_u32x4*>(patch + 2048 + at));
+              const uint32_t to = if_in(in, static_cast<uint32_t>(rr) * kstep + f * 2);
+              buffer_put(kbase + static_cast<int64_t>(i * 16) * kstep, to, *reinterpret_cast<const g_u32x4*>(patch + 1024 + at));
+              buffer_put(kbase + ubytes + static_cast<int64_t>(i * 16) * kstep, to, *reinterpret_cast<const g_u32x4*>(patch + 2048 + at));
             }
           }
           if constexpr (KEEP == KEEP_8BIT) {
             // lane l: 16 codes, half l % 2 of row l / 2 % 16 of g (lanes 0 .. 31) or u; the width is a multiple of 8
-            const int t = le >> 5, rr = (le >> 1) & 15, c = le & 1, r = rbase + rr, f = f0 + c * 16;
-            const unsigned char* const from = patch + 1024 + t * 512 + rr * 32 + c * 16;
-            const g_u32x4 codes = *reinterpret_cast<const g_u32x4*>(from);
-            const uint32_t to = (2 * static_cast<uint32_t>(r - crow0) + t) * kstep + f;
-            buffer_put(kbase, r < crow_end && f + 16 <= cN ? to : BUFFER_NOWHERE, codes);
-            buffer_put(kbase, r < crow_end && f + 8 == cN ? to : BUFFER_NOWHERE, g_u32x2{codes[0], codes[1]});
-            const uint32_t ts = (2 * static_cast<uint32_t>(rbase + l16 - crow0) + lq) * kstep + cN + f0 / CKPT_BLOCK;
-            buffer_put(kbase, lq < 2 && rbase + l16 < crow_end && f0 < cN ? ts : BUFFER_NOWHERE, static_cast<unsigned char>(lq == 0 ? byte[0] : byte[1]));
+            const int t = le >> 5, rr = (le >> 1) & 15, c = le & 1, f = f0 + c * 16;
+            const g_u32x4 codes = *reinterpret_cast<const g_u32x4*>(patch + 1024 + t * 512 + rr * 32 + c * 16);
+            const uint32_t to = static_cast<uint32_t>(rr) * kstep + t * ubytes + f;
+            const bool row = i * 16 + rr < left;
+            buffer_put(kbase + static_cast<int64_t>(i * 16) * kstep, if_in(row && f + 16 <= cN, to), codes);
+            buffer_put(kbase + static_cast<int64_t>(i * 16) * kstep, if_in(row && f + 8 == cN, to), g_u32x2{codes[0], codes[1]});
+            const uint32_t ts = static_cast<uint32_t>(l16) * kstep + lq * ubytes + cN + f0 / CKPT_BLOCK;
+            buffer_put(kbase + static_cast<int64_t>(i * 16) * kstep, if_in(lq < 2 && i * 16 + l16 < left && f0 < cN, ts), static_cast<unsigned char>(lq == 0 ? byte[0] : byte[1]));
           }
         } else {
           unsigned char* const half = patch + (i & 1) * 2048;   // 16 rows of 128 bytes
@@ -637,9 +654,9 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
           wave_lds_order();
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            const int rr = t * 8 + pr, r = rbase + rr;
+            const int rr = t * 8 + pr;
             const g_u32x4 v = *reinterpret_cast<const g_u32x4*>(half + rr * 128 + ((pc ^ swz<8>(rr)) << 4));
-            buffer_put(obase, r < crow_end && pn < cN ? static_cast<uint32_t>(r - crow0) * ostep + pn * 2 : BUFFER_NOWHERE, v);
+            buffer_put(obase + static_cast<int64_t>(i * 16 + t * 8) * ostep, if_in(i * 16 + rr < left && pn < cN, static_cast<uint32_t>(pr) * ostep + pn * 2), v);
           }
         }
       }

@@ -70,9 +70,9 @@ def test_checkpoints_refuse(lib, call, want, bad):
 @pytest.mark.parametrize("want,bad", [
     (NULL, dict(x=None)), (NULL, dict(offs=None)), (NULL, dict(W1=None)), (NULL, dict(W2=None)), (NULL, dict(hid=None)), (NULL, dict(y=None)),
     (NULL, dict(keep=FULL)), (NULL, dict(keep=EIGHT)), (SHAPE, dict(rows=-1)), (SHAPE, dict(E=0)), (SHAPE, dict(d=0)), (SHAPE, dict(d=60)), (SHAPE, dict(F=100)),
-    (SHAPE, dict(F=-8)), (SHAPE, dict(d=(1 << 20) + 8)), (SHAPE, dict(F=(1 << 20) + 8)), (SHAPE, dict(ldx=56)), (SHAPE, dict(ldx=66)),
+    (SHAPE, dict(F=-8)), (SHAPE, dict(d=(1 << 17) + 8)), (SHAPE, dict(F=(1 << 17) + 8)), (SHAPE, dict(ldx=56)), (SHAPE, dict(ldx=66)),
     (SHAPE, dict(dtype=BF16, ldx=68)), (SHAPE, dict(ldw1=62)), (SHAPE, dict(ldw2=64)), (SHAPE, dict(ldh=8)), (SHAPE, dict(ldy=8)), (SHAPE, dict(x=P + 8)),
-    (SHAPE, dict(W1=P + 4)), (SHAPE, dict(W2=P + 2)), (SHAPE, dict(hid=P + 1)), (SHAPE, dict(y=P + 8)), (SHAPE, dict(ldx=(1 << 21) + 8)),
+    (SHAPE, dict(W1=P + 4)), (SHAPE, dict(W2=P + 2)), (SHAPE, dict(hid=P + 1)), (SHAPE, dict(y=P + 8)), (SHAPE, dict(ldx=(1 << 18) + 8)),
     (SHAPE, dict(F=1 << 15, ldw1=1 << 15)), (SHAPE, dict(d=1 << 15, ldw2=1 << 16)), (SHAPE, dict(keep=FULL, pre=P, ldpre=96)),
     (SHAPE, dict(keep=EIGHT, pre=P, ldpre=96)), (SHAPE, dict(keep=EIGHT, pre=P, ldpre=104)), (SHAPE, dict(keep=EIGHT, pre=P + 8)), (SHAPE, dict(ws=P + 8, nb=64)),
     (SHAPE, dict(rows=(1 << 30) + 1)), (SHAPE, dict(rows=1 << 30, F=8192)), (SHAPE, dict(E=1 << 30)), (SHAPE, dict(E=1 << 20, d=2048, F=8192)),
@@ -87,7 +87,7 @@ def test_forward_refuses(lib, want, bad):
     (NULL, dict(ws=None)), (NULL, dict(dx=None, dW1=None, dW2=None)), (NULL, dict(rows=0, offs=None)), (SHAPE, dict(rows=-1)), (SHAPE, dict(E=0)),
     (SHAPE, dict(d=4)), (SHAPE, dict(F=4)), (SHAPE, dict(lddy=56)), (SHAPE, dict(ldx=56)), (SHAPE, dict(ldpre=96)), (SHAPE, dict(pk=EIGHT, ldpre=96)),
     (SHAPE, dict(xk=EIGHT, ldx=64)), (SHAPE, dict(lddx=8)), (SHAPE, dict(ldw1=8)), (SHAPE, dict(ldw2=8)), (SHAPE, dict(dy=P + 8)), (SHAPE, dict(dx=P + 8)),
-    (SHAPE, dict(dW1=P + 8)), (SHAPE, dict(dW2=P + 4)), (SHAPE, dict(ws=P + 8)), (SHAPE, dict(lddy=(1 << 21) + 8)), (SHAPE, dict(F=1 << 15, ldw1=1 << 15)),
+    (SHAPE, dict(dW1=P + 8)), (SHAPE, dict(dW2=P + 4)), (SHAPE, dict(ws=P + 8)), (SHAPE, dict(lddy=(1 << 18) + 8)), (SHAPE, dict(F=1 << 15, ldw1=1 << 15)),
     (DTYPE, dict(dtype=5)), (ARG, dict(act=9)), (ARG, dict(pk=NOTHING)), (ARG, dict(xk=NOTHING)), (ARG, dict(pk=3)), (WORKSPACE, dict(nb=0)),
     (WORKSPACE, dict(nb=4 * 10 * (192 + 96 + 64) - 1)),
 ])
