@@ -1,7 +1,9 @@
 // Activation checkpoints in 8 bits (checkpoint.hpp): rows packed and restored.
 //
-// Bound by HBM: a value is read and a little over a byte written, or the other way round.  A lane has 8 columns, four lanes a block,
-// whose largest magnitude they find by two permutes inside the quad; a workgroup walks over the pieces of as many rows as there are.
+// Bound by HBM: a value is read and a little over a byte written, or the other way round.  A lane has pieces of 16 bytes of x (four
+// lanes a block in bf16, eight in fp32), so that every load and store of a wave is of whole lines (pieces of 32 bytes, stored in halves:
+// unpack 144 us -> 318); the block's largest magnitude comes by lane moves.  A workgroup walks over the pieces of as many rows as there are, four a turn, whose loads are in flight together;
+// where a piece lies is counted on, not divided out.  32768 x 8192 in bf16, pack and unpack: TODO.
 #include "checkpoint.hpp"
 #include "rows.hpp"
 
@@ -11,64 +13,122 @@ struct CkptArgs {
   unsigned char* x; int64_t ldx;          // strides in bytes
   unsigned char* q; int64_t ldq;
   const int32_t* n_rows; int64_t max_rows;
-  int width, pieces;                      // pieces of 8 columns, a whole number of blocks
+  int width, pieces;                      // pieces of a row, of whole blocks
+  int64_t row_step; int col_step;         // from a lane's piece to its next one
 };
 
-constexpr int CKPT_THREADS = 256;
+constexpr int CKPT_THREADS = 256, CKPT_TURN = 4;
 
-template <bool BF16, bool PACK>
+template <bool ST>
+__device__ __forceinline__ void store8(unsigned char* p, uint2 q) {
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  if (ST) __builtin_nontemporal_store(u32x2_t{q.x, q.y}, reinterpret_cast<u32x2_t*>(p));
+  else *reinterpret_cast<u32x2_t*>(p) = u32x2_t{q.x, q.y};
+}
+
+template <bool BF16, bool PACK, bool ST>
 __global__ __launch_bounds__(CKPT_THREADS) void checkpoint_kernel(const CkptArgs a) {
   int64_t rows = a.max_rows;
   if (a.n_rows != nullptr) {
     const int64_t n = *a.n_rows;
     rows = n < rows ? n : rows;
   }
-  constexpr int EB = BF16 ? 2 : 4, NV = BF16 ? 1 : 2;                // 16-byte vectors of a piece
-  const int64_t total = rows * a.pieces, step = static_cast<int64_t>(gridDim.x) * CKPT_THREADS;
-  // (whole quads: total and step are multiples of four)
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * CKPT_THREADS + threadIdx.x; i < total; i += step) {
-    const int64_t r = i / a.pieces;
-    const int c = static_cast<int>(i - r * a.pieces) * 8;
-    const bool in = c < a.width;
-    unsigned char* const xp = a.x + r * a.ldx + static_cast<int64_t>(c) * EB;
-    unsigned char* const qp = a.q + r * a.ldq;
-    float v[8];
+  constexpr int COLS = BF16 ? 8 : 4, WORDS = COLS / 4;               // columns of a piece, words of its codes
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * CKPT_THREADS + threadIdx.x;
+  int64_t r = first / a.pieces;
+  int col = static_cast<int>(first - r * a.pieces);
+  while (r < rows) {
+    // (the lanes of a block are at the same place: pieces and steps are whole blocks)
+    unsigned char* xp[CKPT_TURN];
+    unsigned char* qp[CKPT_TURN];
+    int cc[CKPT_TURN];
+    bool in[CKPT_TURN];
+#pragma unroll
+    for (int u = 0; u < CKPT_TURN; ++u) {
+      cc[u] = col * COLS;
+      in[u] = r < rows && cc[u] < a.width;
+      xp[u] = a.x + r * a.ldx + col * 16;
+      qp[u] = a.q + r * a.ldq;
+      r += a.row_step;
+      col += a.col_step;
+      if (col >= a.pieces) {
+        col -= a.pieces;
+        ++r;
+      }
+    }
     if constexpr (PACK) {
+      uint4 w[CKPT_TURN];
 #pragma unroll
-      for (int t = 0; t < NV; ++t) {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (in) w = *reinterpret_cast<const uint4*>(xp + t * 16);
-        unpack16<BF16>(w, v + t * (8 / NV));
+      for (int u = 0; u < CKPT_TURN; ++u) {
+        w[u] = make_uint4(0, 0, 0, 0);
+        if (in[u]) w[u] = load16<ST>(xp[u]);
       }
-      uint32_t most = 0;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) most = max(most, magnitude(v[t]));
-      most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 1)));
-      most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 2)));
-      const uint32_t byte = ckpt_scale_byte(most);
-      const float inv = ckpt_inverse(byte);
-      if (in) {
-        *reinterpret_cast<uint2*>(qp + c) = make_uint2(ckpt_encode4(v[0], v[1], v[2], v[3], inv), ckpt_encode4(v[4], v[5], v[6], v[7], inv));
-        if ((c & (CKPT_BLOCK - 1)) == 0) qp[a.width + c / CKPT_BLOCK] = static_cast<unsigned char>(byte);
+      for (int u = 0; u < CKPT_TURN; ++u) {
+        float v[COLS];
+        unpack16<BF16>(w[u], v);
+        uint32_t most = 0;
+#pragma unroll
+        for (int t = 0; t < COLS; ++t) most = max(most, magnitude(v[t]));
+        most = max(most, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(most), 0xB1, 0xf, 0xf, true)));   // neighbour
+        most = max(most, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(most), 0x4E, 0xf, 0xf, true)));   // pair
+        if (!BF16) most = max(most, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(most), 0x141, 0xf, 0xf, true)));   // mirrored 8
+        const uint32_t byte = ckpt_scale_byte(most);
+        const float inv = ckpt_inverse(byte);
+        if (in[u]) {
+          const uint32_t codes = ckpt_encode4(v[0], v[1], v[2], v[3], inv);
+          if constexpr (BF16) store8<ST>(qp[u] + cc[u], make_uint2(codes, ckpt_encode4(v[COLS - 4], v[COLS - 3], v[COLS - 2], v[COLS - 1], inv)));
+          else *reinterpret_cast<uint32_t*>(qp[u] + cc[u]) = codes;
+          if ((cc[u] & (CKPT_BLOCK - 1)) == 0) qp[u][a.width + cc[u] / CKPT_BLOCK] = static_cast<unsigned char>(byte);
+        }
       }
-    } else if (in) {
-      const uint2 w = *reinterpret_cast<const uint2*>(qp + c);
-      const float s = ckpt_scale(qp[a.width + c / CKPT_BLOCK]);
-      ckpt_decode4(w.x, s, v);
-      ckpt_decode4(w.y, s, v + 4);
+    } else {
+      uint32_t codes[CKPT_TURN][WORDS], byte[CKPT_TURN];
 #pragma unroll
-      for (int t = 0; t < NV; ++t) *reinterpret_cast<uint4*>(xp + t * 16) = pack16<BF16>(v + t * (8 / NV));
+      for (int u = 0; u < CKPT_TURN; ++u) {
+        byte[u] = 0;
+#pragma unroll
+        for (int t = 0; t < WORDS; ++t) codes[u][t] = 0;
+        if (in[u]) {
+          byte[u] = qp[u][a.width + cc[u] / CKPT_BLOCK];
+#pragma unroll
+          for (int t = 0; t < WORDS; ++t) codes[u][t] = reinterpret_cast<const uint32_t*>(qp[u] + cc[u])[t];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < CKPT_TURN; ++u) {
+        float v[COLS];
+#pragma unroll
+        for (int t = 0; t < WORDS; ++t) ckpt_decode4(codes[u][t], ckpt_scale(byte[u]), v + 4 * t);
+        if (in[u]) store16<ST>(xp[u], pack16<BF16>(v));
+      }
     }
   }
 }
 
 template <bool PACK>
 static int launch_checkpoint(CkptArgs a, int dtype, hipStream_t stream) {
-  a.pieces = (a.width + CKPT_BLOCK - 1) / CKPT_BLOCK * (CKPT_BLOCK / 8);
-  const int64_t blocks = (a.max_rows * a.pieces + CKPT_THREADS - 1) / CKPT_THREADS, most = int64_t(num_cus()) * 32;
-  const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most)), block(CKPT_THREADS);
-  if (dtype == SCMOE_BF16) hipLaunchKernelGGL((checkpoint_kernel<true, PACK>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((checkpoint_kernel<false, PACK>), grid, block, 0, stream, a);
+  const int cols = 16 / elem_bytes(dtype);
+  a.pieces = (a.width + CKPT_BLOCK - 1) / CKPT_BLOCK * (CKPT_BLOCK / cols);
+  // Workgroups of one turn each, and where that leaves compute units less than eight of them, of fewer pieces a lane (16384 x 1024: 11.7 us
+  // so, 15.7 with a piece a lane; 32768 x 8192, pack: 143 us with two turns, 158 with sixteen).
+  const int64_t blocks = (a.max_rows * a.pieces + CKPT_THREADS - 1) / CKPT_THREADS, turns = (blocks + CKPT_TURN - 1) / CKPT_TURN, few = int64_t(num_cus()) * 8;
+  int64_t n = turns > few ? turns : blocks < few ? blocks : few;
+  if (n > (1 << 23)) n = 1 << 23;                                     // (under 2^32 threads)
+  const int64_t step = n * CKPT_THREADS;
+  a.row_step = step / a.pieces;
+  a.col_step = static_cast<int>(step - a.row_step * a.pieces);
+  const dim3 grid(static_cast<unsigned>(n)), block(CKPT_THREADS);
+  const bool st = streams_past_caches(a.max_rows * a.width * (elem_bytes(dtype) + 1));
+#define SCMOE_CHECKPOINT(BF16, ST) hipLaunchKernelGGL((checkpoint_kernel<BF16, PACK, ST>), grid, block, 0, stream, a)
+  if (dtype == SCMOE_BF16) {
+    if (st) SCMOE_CHECKPOINT(true, true);
+    else SCMOE_CHECKPOINT(true, false);
+  } else {
+    if (st) SCMOE_CHECKPOINT(false, true);
+    else SCMOE_CHECKPOINT(false, false);
+  }
+#undef SCMOE_CHECKPOINT
   return launch_status();
 }
 
