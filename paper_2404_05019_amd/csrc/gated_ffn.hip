@@ -97,13 +97,18 @@ extern "C" int scmoe_gated_ffn(const void* x_perm, int64_t ld_perm, int32_t dtyp
   a.offsets = offsets; a.E = E; a.act = act;
   a.pre = static_cast<unsigned char*>(pre); a.ldpre = ldpre;
   a.j[0] = gated_job(x_perm, ld_perm, W1, ldw1, hidden, ldh, 0, F, d);
+  const bool experts = second_is_the_experts(dtype, max_rows, E, d, F);
+  if (experts && dtype == SCMOE_BF16 && workspace != nullptr && ws_bytes >= ffn_mfma_scratch_bytes()) {
+    a.zero = static_cast<int*>(workspace);                  // (the counters of tiles that the second product cuts along K)
+    a.zeros = ffn_mfma_counter_ints();
+  }
   st = launch_gated(a, G_GATE, pre_keep, max_rows, dtype, s);
   if (st != SCMOE_OK) return st;
-  if (second_is_the_experts(dtype, max_rows, E, d, F)) {
+  if (experts) {
     FfnArgs f{};
     f.offsets = offsets; f.max_rows = max_rows; f.E = E; f.d = d; f.F = F;
     f.W2 = W2; f.ldw2 = ldw2; f.hidden = hidden; f.ldh = ldh; f.y = y_perm; f.ldy = ldy;
-    f.scratch = workspace; f.scratch_bytes = ws_bytes;
+    f.scratch = workspace; f.scratch_bytes = ws_bytes; f.scratch_zeroed = a.zero != nullptr;
     return ffn_second(f, dtype, s);
   }
   a.j[0] = gated_job(hidden, ldh, W2, ldw2, y_perm, ldy, 0, d, F);

@@ -44,10 +44,11 @@ struct GatedArgs {
   int E, act;
   unsigned char* pre; int64_t ldpre;   // GATE: written, DH: read: [rows, 2 F], or checkpoint rows 2 r, 2 r + 1 (strides in bytes)
   unsigned char* dpre; int64_t lddpre; // DH: gradients of g and u, [rows, 2 F]
+  int* zero; int zeros;                // GATE: ints to clear for the launch that follows (nullptr: none)
 };
 
-template <bool F32_, int BM_, int BN_, int WM_, int WN_, int NS_>
-struct GatedCfg {                      // NS_: stages
+template <bool F32_, int BM_, int BN_, int WM_, int WN_, int NS_, int PATCH_ = F32_ ? 0 : 4096>
+struct GatedCfg {                      // NS_: stages; PATCH_: bytes of LDS that a wave has for the epilogue (2048: of DOWN, DX and DW alone)
   static constexpr bool F32 = F32_;
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NS = NS_;
   static constexpr int EB = F32 ? 4 : 2, VE = 16 / EB, BK = 128 / EB, KS = 2;      // KS: k steps of 64 bytes in a stage
@@ -56,7 +57,7 @@ struct GatedCfg {                      // NS_: stages
   static constexpr int NH = MI > 1 ? 2 : 1;                                          // halves of a wave's rows that a stage is refilled by
   static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
   static constexpr int APW = A_BYTES / 1024 / WAVES, BPW = B_BYTES / 1024 / WAVES;  // copies of a wave and k-tile
-  static constexpr int PATCH = F32 ? 0 : 4096;                                       // of a wave, for the epilogue
+  static constexpr int PATCH = PATCH_;
   static constexpr int LDS = NS * STAGE + WAVES * PATCH;
   static_assert(LDS <= 160 * 1024, "LDS budget");
   static constexpr int MOST_WG = (MI > 1 ? 8 : 16) / WAVES;                          // by registers: two waves a SIMD, small tiles four
@@ -413,6 +414,8 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
   if (it >= items) return;
   setup(it);
   issue_prologue();
+  if (MODE == G_GATE && p.zero != nullptr && blockIdx.x == 0)
+    for (int i = threadIdx.x; i < p.zeros; i += CFG::THREADS) p.zero[i] = 0;
   for (;;) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -646,7 +649,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
             buffer_put(kbase + static_cast<int64_t>(i * 16) * kstep, if_in(lq < 2 && i * 16 + l16 < left && f0 < cN, ts), static_cast<unsigned char>(lq == 0 ? byte[0] : byte[1]));
           }
         } else {
-          unsigned char* const half = patch + (i & 1) * 2048;   // 16 rows of 128 bytes
+          unsigned char* const half = patch + (CFG::PATCH > 2048 ? (i & 1) * 2048 : 0);   // 16 rows of 128 bytes
 #pragma unroll
           for (int j = 0; j < NJ; ++j)
             *reinterpret_cast<uint2*>(half + l16 * 128 + (((2 * j + (lq >> 1)) ^ swz<8>(l16)) << 4) + (lq & 1) * 8) =
