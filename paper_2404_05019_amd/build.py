@@ -10,7 +10,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libscmoe.so")
 SOURCES = ["gate.hip", "dispatch.hip", "combine.hip", "ffn_mfma.hip", "ffn_direct.hip", "layer.hip",
            "norm.hip", "balance_loss.hip", "gate_backward.hip", "combine_backward.hip", "sum_parts.hip",
-           "checkpoint.hip", "gated_ffn.hip", "gated_bf16.hip", "gated_f32.hip"]
+           "checkpoint.hip", "gated_ffn.hip", "gated_bf16.hip", "gated_f32.hip", "gated_few.hip"]
 # Packed-fp32 instruction selection is switched off for all device code.
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

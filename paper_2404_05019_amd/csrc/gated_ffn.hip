@@ -13,7 +13,20 @@ static_assert(BUFFER_NOWHERE + 127ull * 2 * GATED_MOST_LD < (1ull << 32) && 256l
 static_assert(BUFFER_NOWHERE + 127ull * 2 * (2 * SCMOE_MAX_GATED_WIDTH + 64) < (1ull << 32));   // (the workspace's padded rows)
 static bool gated_view_ok(const void* p, int64_t ld, int64_t cols, int dtype) { return view_ok(p, ld, cols, dtype) && ld <= GATED_MOST_LD; }
 
+// Which calls take the kernel for few rows (gated_few.hip): where experts average at most two rows (DOWN: one, above which the experts'
+// second product does better), or there are no more than it takes at a time; in fp32, whose matrix instructions have less to gain, five.
+// us of a forward call, other kernels / few rows in GATE alone / in both:
+//   bf16, d = 2048, F = 8192, E = 16    1 row 36.1 / 28.8 / 22.7, 8 rows 160 / 139 / 138, 16 rows 202 / 182 / 178, 32 rows 298 / 259 / 267, 64 rows 312 / 330 / 385
+//   bf16, 4 rows of one expert 34.4 / 30.9 / 25.9, 16 rows 36.5 / 60.7 / 68.5;   30 rows, d = 1000, F = 2728, E = 8 39.8 / 44.4 / 48.1
+//   fp32, d = 1024, F = 4096, E = 8     1 row 35.0 / 21.6 / 16.8, 16 rows 123 / 107 / 64, 40 rows 138 / 130 / 106;   64 rows, d = 64, F = 256, E = 4 17.5 / 17.9 / 16.8
+static bool few_rows(int mode, int dtype, int64_t rows, int E) {
+  if (rows > 4096) return false;                         // (tiles of rows are the grid's y)
+  const int64_t per = dtype == SCMOE_F32 ? 5 : mode == G_GATE ? 2 : 1;
+  return rows <= 4 || rows <= per * E;
+}
+
 static int launch_gated(const GatedArgs& a, int mode, int keep, int64_t max_rows, int dtype, hipStream_t stream) {
+  if (((mode == G_GATE && keep != KEEP_8BIT) || mode == G_DOWN) && few_rows(mode, dtype, max_rows, a.E)) return launch_gated_few(a, mode, keep, max_rows, dtype, stream);
   return dtype == SCMOE_BF16 ? launch_gated_bf16(a, mode, keep, max_rows, stream) : launch_gated_f32(a, mode, keep, max_rows, stream);
 }
 
@@ -45,12 +58,12 @@ static bool kept_ok(const void* p, int64_t ld, int64_t width, int keep, int dtyp
   return keep == SCMOE_KEEP_8BIT ? ckpt_view_ok(p, ld, width) && ld <= GATED_MOST_LD : gated_view_ok(p, ld, width, dtype);
 }
 
-// Where y = W2 h is the second product of the experts without a gate (ffn_mfma.hip, ffn_direct.hip): in bf16 where its tiled kernel takes
-// the widths, and for few rows, when its other kernel streams the weights; else this block's own.  us of a forward call, so / with DOWN:
-// bf16, 16384 rows, d = 1024, F = 4096, E = 8 372 / 394; 1 row, d = 2048, F = 8192, E = 16 41 / 73; 1 row, d = 1000, F = 2728, E = 8 21 / 26; 30 rows
-// 45 / 52; but 500 rows 73 / 64, 5003 rows, E = 32 272 / 208.  fp32, 1 row, d = 1024, F = 4096, E = 8 84 / 95; but 40 rows 161 / 148, 4096, F = 2048 417 / 381.
+// Where y = W2 h is the second product of the experts without a gate (ffn_mfma.hip, ffn_direct.hip): in bf16, where its tiled kernel takes
+// the widths, and for up to 16 rows an expert, when its other kernel streams the weights; else this block's own.  us of a forward call,
+// so / with DOWN: 16384 rows, d = 1024, F = 4096, E = 8 372 / 394; 30 rows, d = 1000, F = 2728 45 / 52; but 500 rows 73 / 64, 5003 rows, E = 32
+// 272 / 208.  In fp32 DOWN does better from 40 rows on (d = 1024, F = 4096, E = 8 148 / 161; 4096 rows, F = 2048 381 / 417).
 static bool second_is_the_experts(int dtype, int64_t rows, int E, int d, int F) {
-  if (dtype == SCMOE_F32) return rows <= E;
+  if (dtype == SCMOE_F32 || few_rows(G_DOWN, dtype, rows, E)) return false;
   return ffn_mfma_supported(d, F) || rows <= 64 || (rows <= 16 * static_cast<int64_t>(E) && rows <= 1024);
 }
 

@@ -792,6 +792,9 @@ static int launch_gated_cfg(GatedArgs a, int64_t max_rows, hipStream_t stream) {
 int launch_gated_bf16(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream);
 int launch_gated_f32(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream);
 
+// GATE (kept in full or not at all) and DOWN of a few rows.
+int launch_gated_few(const GatedArgs& a, int mode, int keep, int64_t max_rows, int dtype, hipStream_t stream);
+
 template <class CFG, int MODE, int KEEP>
 static int launch_gated_act(const GatedArgs& a, int64_t max_rows, hipStream_t stream) {
   switch (a.act) {
