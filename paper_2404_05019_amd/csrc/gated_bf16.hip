@@ -63,7 +63,7 @@ int launch_gated_bf16(const GatedArgs& a, int mode, int keep, int64_t max_rows, 
     case TILES_256_128: return mode == G_DOWN ? launch_gated_cfg<GatedV, G_DOWN, KEEP_NONE, 0>(a, max_rows, stream) : launch_gated_cfg<GatedV, G_DX, KEEP_NONE, 0>(a, max_rows, stream);
     case TILES_256: return launch_gated_mode<GatedA>(a, mode, keep, max_rows, stream);
     case TILES_128: return launch_gated_mode<GatedU>(a, mode, keep, max_rows, stream);
-    default: return launch_gated_mode<GatedS>(a, mode, keep, max_rows, stream);
+    default: return launch_gated_rows<GatedS>(a, mode, keep, max_rows, stream);
   }
 }
 

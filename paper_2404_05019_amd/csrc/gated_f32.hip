@@ -4,7 +4,8 @@
 namespace scmoe {
 
 using GatedF = GatedCfg<true, 128, 128, 2, 2, 2>;    // 4 waves of 64 x 64, 64 KiB LDS, two workgroups per CU
-using GatedG = GatedCfg<true, 64, 64, 4, 1, 3>;      // 4 waves of 16 x 64, 48 KiB LDS, three workgroups per CU
+using GatedD = GatedCfg<true, 64, 64, 4, 1, 2>;      // the same with 32 KiB, four workgroups per CU: for DW, whose k is a segment's rows
+using GatedG = GatedCfg<true, 64, 64, 4, 1, 3>;
 
 // The larger tiles, which read less per product, where they come to eight rounds (of two a compute unit) and more, or to two with a long K;
 // else the smaller ones, of which more are under way at a time.  us of a forward call / a gradient, all products on larger | smaller tiles:
@@ -20,7 +21,8 @@ int launch_gated_f32(const GatedArgs& a, int mode, int keep, int64_t max_rows, h
   }
   const double rounds = tiles / (2.0 * num_cus());
   if (rounds >= 8.0 || (mode != G_DW && rounds >= 2.0 && a.j[0].Kd >= 4096)) return launch_gated_mode<GatedF>(a, mode, keep, max_rows, stream);
-  return launch_gated_mode<GatedG>(a, mode, keep, max_rows, stream);
+  if (mode == G_DW) return launch_gated_cfg<GatedD, G_DW, KEEP_NONE, 0>(a, max_rows, stream);   // (777 rows 165 / 160, 2000, d = 512, F = 1024, E = 16 180 / 175)
+  return launch_gated_rows<GatedG>(a, mode, keep, max_rows, stream);
 }
 
 }  // namespace scmoe

@@ -805,7 +805,7 @@ static int launch_gated_act(const GatedArgs& a, int64_t max_rows, hipStream_t st
 }
 
 template <class CFG>
-static int launch_gated_mode(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream) {
+static int launch_gated_rows(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream) {
   switch (mode) {
     case G_GATE:
       return keep == KEEP_NONE ? launch_gated_act<CFG, G_GATE, KEEP_NONE>(a, max_rows, stream)
@@ -814,9 +814,13 @@ static int launch_gated_mode(const GatedArgs& a, int mode, int keep, int64_t max
     case G_DH:
       return keep == KEEP_FULL ? launch_gated_act<CFG, G_DH, KEEP_FULL>(a, max_rows, stream) : launch_gated_act<CFG, G_DH, KEEP_8BIT>(a, max_rows, stream);
     case G_DOWN: return launch_gated_cfg<CFG, G_DOWN, KEEP_NONE, 0>(a, max_rows, stream);
-    case G_DX: return launch_gated_cfg<CFG, G_DX, KEEP_NONE, 0>(a, max_rows, stream);
-    default: return launch_gated_cfg<CFG, G_DW, KEEP_NONE, 0>(a, max_rows, stream);
+    default: return launch_gated_cfg<CFG, G_DX, KEEP_NONE, 0>(a, max_rows, stream);
   }
+}
+template <class CFG>
+static int launch_gated_mode(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream) {
+  if (mode == G_DW) return launch_gated_cfg<CFG, G_DW, KEEP_NONE, 0>(a, max_rows, stream);
+  return launch_gated_rows<CFG>(a, mode, keep, max_rows, stream);
 }
 
 }  // namespace scmoe
