@@ -650,9 +650,10 @@ int scmoe_gated_ffn_backward_workspace_bytes(int32_t dtype, int32_t max_rows, in
  * W1 for dx_perm alone.  dx_perm, dW1, dW2: each may be NULL, not all of them.  dW1: [E, 2 F, d], dW2:
  * [E, d, F], in dtype, without gaps, overwritten (an expert without rows: zeros; max_rows 0: all zeros,
  * and only offsets is looked at).  Rows of dx_perm past offsets[E] are not touched, and what lies past
- * offsets[E] in dy_perm, x and pre reaches nothing.  dx_perm may be the buffer of dy_perm only where dW2
- * is NULL.  fp32 accumulation in an order that does not depend on scheduling; bf16: dg, du and act(g) u
- * are rounded on their way to the second products.
+ * offsets[E] in dy_perm, x and pre reaches nothing.  dx_perm may be the buffer of dy_perm, or of x kept in
+ * full (same pointer and stride); no other output may overlap an input.  fp32 accumulation in an order
+ * that does not depend on scheduling; bf16: dg, du and act(g) u are rounded on their way to the second
+ * products.
  */
 int scmoe_gated_ffn_backward(const void* dy_perm, int64_t lddy, int32_t dtype, const void* x, int64_t ldx,
                              int32_t x_keep, const void* pre, int64_t ldpre, int32_t pre_keep,

@@ -1,7 +1,7 @@
 // The gated feed-forward block over packed expert segments and its gradient: which launches a call makes, and the checks of its arguments.
 //
 //   forward    GATE (hidden rows, and g and u where they are kept), DOWN
-//   backward   DH (gradients of g and u, h again), DX, DW (both weights' gradients in one launch)
+//   backward   DH (gradients of g and u, h again), DW (both weights' gradients in one launch), DX
 #include "gated_tiles.hpp"
 
 namespace scmoe {
@@ -169,11 +169,6 @@ extern "C" int scmoe_gated_ffn_backward(const void* dy_perm, int64_t lddy, int32
     a.j[0] = gated_job(dy_perm, lddy, W2, ldw2, hid, w.ldh, 0, F, d);
     st = launch_gated(a, G_DH, pre_keep, max_rows, dtype, s);
     if (st != SCMOE_OK) return st;
-    if (dx_perm) {
-      a.j[0] = gated_job(dpre, w.ldp, W1, ldw1, dx_perm, lddx, 0, d, 2 * F);
-      st = launch_gated(a, G_DX, KEEP_NONE, max_rows, dtype, s);
-      if (st != SCMOE_OK) return st;
-    }
     if (dW1 && x_keep == SCMOE_KEEP_8BIT) {
       st = checkpoint_unpack(x, ldx, offsets + E, max_rows, d, ws + w.x, d, dtype, s);
       if (st != SCMOE_OK) return st;
@@ -181,10 +176,15 @@ extern "C" int scmoe_gated_ffn_backward(const void* dy_perm, int64_t lddy, int32
       ldx = d;
     }
   }
-  if (!dW1 && !dW2) return SCMOE_OK;
-  int n = 0;
-  if (dW1) a.j[n++] = gated_job(dpre, w.ldp, x, ldx, dW1, d, 2 * F, d, 0);
-  if (dW2) a.j[n++] = gated_job(dy_perm, lddy, hid, w.ldh, dW2, F, d, F, 0);
-  if (n == 1) a.j[1] = GatedJob{};
-  return launch_gated(a, G_DW, KEEP_NONE, max_rows, dtype, s);
+  if (dW1 || dW2) {
+    int n = 0;
+    if (dW1) a.j[n++] = gated_job(dpre, w.ldp, x, ldx, dW1, d, 2 * F, d, 0);
+    if (dW2) a.j[n++] = gated_job(dy_perm, lddy, hid, w.ldh, dW2, F, d, F, 0);
+    st = launch_gated(a, G_DW, KEEP_NONE, max_rows, dtype, s);
+    if (st != SCMOE_OK || !dx_perm || max_rows == 0) return st;
+  }
+  // (the last launch, so that dx may take the place of dy or x)
+  a.j[0] = gated_job(dpre, w.ldp, W1, ldw1, dx_perm, lddx, 0, d, 2 * F);
+  a.j[1] = GatedJob{};
+  return launch_gated(a, G_DX, KEEP_NONE, max_rows, dtype, s);
 }

@@ -170,6 +170,13 @@ def test_launches_stay_within_the_runtime_s_limits(record):
             assert int(w[9]) <= 160 << 10
 
 
+def test_what_is_not_asked_for_is_not_needed(record):
+    for kw, launches in ((dict(dx=None, W1=None), 2), (dict(dx=None, W1=None, dW1=None, x=None, xk=NOTHING), 2), (dict(dW1=None, dW2=None, x=None, xk=NOTHING), 2),
+                         (dict(dW1=None, x=None, xk=NOTHING), 3), (dict(), 3), (dict(xk=EIGHT), 4)):
+        (st, lines), = record([("grad", kw)])
+        assert st == 0 and len(lines) == launches, kw
+
+
 def test_gradients_of_no_rows_are_written(record):
     none = dict(rows=0, dy=None, x=None, pre=None, W1=None, W2=None, ws=None, nb=0)
     for kw in (none, dict(none, dW1=None), dict(none, dW2=None), dict(none, dx=None)):

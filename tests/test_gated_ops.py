@@ -256,6 +256,108 @@ def test_backward_activations(counts, d, F, dtype, act):
     check_backward(b, b.x, b.pre)
 
 
+# Calls of the sizes that take each form of the kernels (which ones: tests/test_gated_forms.py), with ragged segments, some of them
+# empty, and widths that end inside a tile: (rows of the segments, model width, hidden width, type)
+FORMS = {
+    "wide_bf16": ([700, 0, 1300, 1, 998, 2048, 515, 600], 1000, 2728, "bf16"),
+    "wide_lines_bf16": ([1024, 1500, 0, 2047, 900, 1, 1300, 700], 1024, 2048, "bf16"),
+    "middle_bf16": ([500, 0, 731, 257, 1, 128], 392, 1544, "bf16"),
+    "middle_long_bf16": ([600, 1, 700, 0, 515, 600, 900, 887], 392, 2056, "bf16"),
+    "many_rows_bf16": ([4000, 3001, 5000, 2900], 1000, 264, "bf16"),
+    "rows_of_one_tile_bf16": ([156] * 20 + [0, 190, 1, 195] + [130] * 8, 1000, 1376, "bf16"),
+    "narrow_bf16": ([100, 3, 0, 77], 200, 264, "bf16"),
+    "wide_f32": ([2300, 0, 1999, 2601, 1, 3100, 3200, 3300], 1000, 4104, "f32"),
+    "narrow_f32": ([100, 3, 0, 77], 200, 264, "f32"),
+}
+
+
+@pytest.mark.parametrize("keep", ["full", "8bit"])
+@pytest.mark.parametrize("form", FORMS)
+def test_forms_of_the_kernels(form, keep):
+    counts, d, F, dtype = FORMS[form]
+    b = Block(counts, d, F, dtype, "silu", seed=20)
+    if keep == "full":
+        b.forward(pre=b.pre)
+        check_forward(b)
+        b.untouched(b.pre)
+        b.backward(b.x, b.pre)
+        check_backward(b, b.x, b.pre)
+    else:
+        b.forward(pre=b.pre8)
+        check_forward(b, keep="8bit")
+        assert bool((b.pre8[2 * b.K:] == 0x5A).all())
+        B.scmoe_checkpoint_pack(b.x, b.x8, n_rows=b.offsets[-1:])
+        b.backward(b.x8, b.pre8)
+        check_backward(b, restored(b.x8[:b.K], b.K, d), restored(b.pre8[:2 * b.K], 2 * b.K, F).reshape(b.K, 2 * F))
+    b.forward()                                     # (nothing kept)
+    check_forward(b, keep="")
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts", [[1], [4], [0, 0, 3, 0], [9, 0, 0, 1, 0, 0, 2, 0, 0, 0, 0, 0, 0, 0, 0, 0], [0] * 70 + [2, 0, 5] + [0] * 60 + [1] * 7, [1] * 150])
+def test_few_rows_of_many_experts(counts, dtype, act):
+    """One row to a few, in segments that lie anywhere among up to 150."""
+    b = Block(counts, 264, 72, dtype, act, spare=0 if len(counts) < 8 else 3, seed=21)
+    b.forward(pre=b.pre)
+    check_forward(b)
+    b.untouched(b.pre)
+    b.y.fill_(NAN)
+    b.forward()
+    check_forward(b)
+    b.backward(b.x, b.pre)
+    check_backward(b, b.x, b.pre)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_dx_in_the_place_of_dy_or_x(dtype):
+    b = Block([33, 0, 140, 7], 136, 200, dtype, "silu", seed=22)
+    b.forward(pre=b.pre)
+    b.backward(b.x, b.pre)
+    want = [t.clone() for t in (b.dx[:b.K], b.dW1, b.dW2)]
+    for n in ("x", "dy"):
+        kept = getattr(b, n).clone()
+        b.dW1.fill_(NAN)
+        b.dW2.fill_(NAN)
+        b.backward(b.x, b.pre, dx_perm=getattr(b, n))
+        assert all(torch.equal(p, q) for p, q in zip(want, (getattr(b, n)[:b.K], b.dW1, b.dW2)))
+        getattr(b, n).copy_(kept)
+
+
+def test_offsets_beyond_32_bits():
+    """Pre-activations, their gradients and checkpoints of more than 2^32 bytes: the last segment's rows lie behind that."""
+    far, n, d, F = 140000, 40, 8, 16384
+    counts = [far, n]
+    g = gen(23)
+    offsets, rows = offsets_of(counts), far + n
+    new = lambda *s, dtype=torch.bfloat16: torch.zeros(s, dtype=dtype, device=DEV)  # noqa: E731
+    x, dy = normal(g, rows, d, dtype="bf16"), normal(g, rows, d, dtype="bf16")
+    W1, W2 = normal(g, 2, 2 * F, d, scale=d ** -0.5, dtype="bf16"), normal(g, 2, d, F, scale=F ** -0.5, dtype="bf16")
+    hidden, y, dx, pre = new(rows, F), new(rows, d), new(rows, d), new(rows, 2 * F)
+    pre8 = new(2 * rows, B.scmoe_checkpoint_ld(F), dtype=torch.uint8)
+    dW1, dW2 = torch.empty_like(W1), torch.empty_like(W2)
+    need = B.scmoe_gated_ffn_backward_workspace_bytes(B.BF16, rows, 2, d, F)
+    assert min(pre.nbytes, pre8.nbytes, need) > 1 << 32
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    at = slice(far, rows)
+    B.scmoe_gated_ffn(x, offsets, rows, W1, W2, hidden, y, B.SILU, pre=pre)
+    B.scmoe_gated_ffn(x, offsets, rows, W1, W2, hidden, y, B.SILU, pre=pre8)
+    want_y, want_pre, _, sy, spre = forward64(x[at], W1[1], W2[1], "silu", "bf16")
+    close(y[at], want_y, sy, "bf16")
+    close(pre[at], want_pre, spre, "bf16")
+    for kept, values in ((pre, pre[at]), (pre8, restored(pre8[2 * far:], 2 * n, F).reshape(n, 2 * F))):
+        B.scmoe_gated_ffn_backward(dy, x, kept, offsets, rows, W1, W2, B.SILU, dx, dW1, dW2, workspace=ws)
+        wx, w1, w2, ex, e1, e2 = backward64(dy[at], x[at], values, W1[1], W2[1], "silu", "bf16")
+        close(dx[at], wx, ex, "bf16")
+        close(dW1[1], w1, e1, "bf16")
+        close(dW2[1], w2, e2, "bf16")
+    B.scmoe_checkpoint_pack(pre.view(2 * rows, F), pre8)
+    assert torch.equal(pre8[2 * far:], ckpt(pre.view(2 * rows, F)[2 * far:]))
+    values = restored(pre8[2 * far:], 2 * n, F, "bf16")
+    B.scmoe_checkpoint_unpack(pre8, pre.view(2 * rows, F))
+    assert torch.equal(pre.view(2 * rows, F)[2 * far:], values)
+
+
 # ---- checkpoints ------------------------------------------------------------------------------------
 
 
