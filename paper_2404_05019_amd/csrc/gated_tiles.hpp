@@ -150,6 +150,56 @@ __device__ __forceinline__ void load4(const unsigned char* p, float* v) {
   }
 }
 
+// The schedule's constructor, and its search for a tile's segment, read the segments' bounds one after the other; here a wave reads 64 at
+// a time (2000 rows of 64 experts, forward 139.7 us / 131.5, gradient 322.9 / 314.6); the search so from 17 experts on: with 8 it is 1 % slower.
+struct SegmentTiles {
+  int tiles, incl, all;                            // row tiles of segment e0 + lane, of those up to it, of the 64
+  template <int BM>
+  __device__ __forceinline__ static SegmentTiles of(const int32_t* offsets, int E, int e0, int lane) {
+    SegmentTiles m;
+    const int q = e0 + lane;
+    const int s = offsets[q < E ? q : E], t = offsets[q + 1 < E ? q + 1 : E];
+    m.tiles = (t - s + BM - 1) / BM;               // (0 past the last segment)
+    m.incl = m.tiles;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int up = __shfl_up(m.incl, off, 64);
+      if (lane >= off) m.incl += up;
+    }
+    m.all = __builtin_amdgcn_readlane(m.incl, 63);
+    return m;
+  }
+};
+// The segment of the XCD's tile `item`, from which the schedule's search then starts.
+template <int BM, class S>
+__device__ __forceinline__ void gated_find(S& sched, int item, int lane) {
+  const int tile = item < sched.rr ? ((item / S::RR) * 8 + sched.xcd) * S::RR + item % S::RR : sched.b0 + item - sched.rr;
+  int before = 0;                                  // row tiles of the segments ahead of e0
+  for (int e0 = 0; e0 < sched.E; e0 += 64) {
+    const SegmentTiles m = SegmentTiles::of<BM>(sched.offsets, sched.E, e0, lane);
+    const unsigned long long hit = __ballot((before + m.incl) * sched.nt > tile);
+    if (hit != 0) {
+      const int at = __builtin_ctzll(hit);
+      sched.cur_e = e0 + at;
+      sched.cur_base = (before + __builtin_amdgcn_readlane(m.incl, at) - __builtin_amdgcn_readlane(m.tiles, at)) * sched.nt;
+      return;
+    }
+    before += m.all;
+  }
+}
+// The share of an XCD of the row tiles of E segments.
+template <int BM, class S>
+__device__ __forceinline__ void gated_share(S& sched, int E, int lane) {
+  int all = 0;
+  for (int e0 = 0; e0 < E; e0 += 64) all += SegmentTiles::of<BM>(sched.offsets, E, e0, lane).all;
+  const int routed = all * sched.nt;
+  sched.E = E;
+  sched.rr = routed / (8 * S::RR) * S::RR;
+  const int rest = routed - 8 * sched.rr, chunk = (rest + 7) >> 3, mine = rest - sched.xcd * chunk;
+  sched.b0 = 8 * sched.rr + sched.xcd * chunk;
+  sched.ngemm = sched.rr + (mine < 0 ? 0 : mine > chunk ? chunk : mine);
+}
+
 template <class CFG, int MODE, int KEEP, int ACT>
 __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void gated_kernel(const GatedArgs p) {
   constexpr bool F32 = CFG::F32;
@@ -169,10 +219,13 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
   const int xcd = blockIdx.x & 7, nslots = gridDim.x >> 3;
   int it = blockIdx.x >> 3;
   constexpr int GM = MODE == G_GATE || MODE == G_DH ? 6 : 4;
-  TileSchedule<BM, BNF, GM> sched(MODE == G_DW ? 0 : p.j[0].nt, MODE == G_DW ? 0 : p.E, p.offsets, 0, 1, false, 1, xcd, nslots);
+  using Schedule = TileSchedule<BM, BNF, GM>;
+  constexpr int RR = Schedule::RR;
+  // (constructed without segments: gated_share counts them)
+  Schedule sched(MODE == G_DW ? 0 : p.j[0].nt, 0, p.offsets, 0, 1, false, 1, xcd, nslots);
+  if constexpr (MODE != G_DW) gated_share<BM>(sched, p.E, lane);
   // DW: as many tiles for every expert; dealt like the schedule's
   const int dw_all = p.j[0].tiles + p.j[1].tiles;
-  constexpr int RR = decltype(sched)::RR;
   const int dw_dealt = dw_all / (8 * RR) * RR, dw_rest = dw_all - 8 * dw_dealt, dw_share = (dw_rest + 7) >> 3;
   int items = sched.ngemm;
   if (MODE == G_DW) {
@@ -220,9 +273,8 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
       abase = jb->A + static_cast<int64_t>(s) * jb->lda * EB;
       bbase = jb->B + static_cast<int64_t>(s) * jb->ldb * EB;
     } else {
-      int l, part;
-      sched.item(item, l, part);
-      sched.locate(l, e, row0, row_end, n0);
+      if (p.E > 16) gated_find<BM>(sched, item, lane_here());
+      sched.locate(item, e, row0, row_end, n0);
       k_all = jb->Kd;
       abase = jb->A + static_cast<int64_t>(row0) * jb->lda * EB;
       bbase = jb->B + static_cast<int64_t>(e) * (MODE == G_GATE ? 2 * jb->N : MODE == G_DOWN ? jb->N : jb->Kd) * jb->ldb * EB;
