@@ -524,14 +524,44 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
     };
     using std::bool_constant;
     using std::integral_constant;
+    // fp32: a sum is made of parts of some 16 k-tiles (512 products), whose chains are short: dx of 200 rows, d = 2048, F = 8192
+    // (16384 products) is 6.0e-7 off so, in the 2-norm, 2.4e-6 in one chain; the time is 1 % more.
+    constexpr int PART = 16;
+    f32x4_t sum[F32 ? MI : 1][F32 ? NJ : 1];
+    auto next_part = [&](auto first_c) {
+#pragma unroll
+      for (int i = 0; i < (F32 ? MI : 0); ++i)
+#pragma unroll
+        for (int j = 0; j < (F32 ? NJ : 0); ++j) {
+          sum[i][j] = decltype(first_c)::value ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : sum[i][j] + acc[i][j];
+          acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    };
+    next_part(std::true_type{});
     if (nk > 0) {
       load_frags(0, 0);
       int kt = 0;
-      for (; kt + 2 * NS <= k_all / BK; kt += NS) static_for<0, NS>([&](auto s) { k_tile(s, bool_constant<true>{}, kt + decltype(s)::value); });
+      const int whole = k_all / BK;
+      auto turn = [&]() { static_for<0, NS>([&](auto s) { k_tile(s, bool_constant<true>{}, kt + decltype(s)::value); }); };
+      if constexpr (F32) {
+        while (kt + 2 * NS <= whole) {
+          const int end = kt + PART < whole ? kt + PART : whole;
+          for (; kt < end && kt + 2 * NS <= whole; kt += NS) turn();
+          next_part(std::false_type{});
+        }
+      } else {
+        for (; kt + 2 * NS <= whole; kt += NS) turn();
+      }
       for (; kt < nk; kt += NS)
         static_for<0, NS>([&](auto s) {
           if (kt + decltype(s)::value < nk) k_tile(s, bool_constant<false>{}, kt + decltype(s)::value);
         });
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] += sum[i][j];
+      }
     }
     lds_barrier();                                  // every wave holds its last fragments: LDS is free
 
