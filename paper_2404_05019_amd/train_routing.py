@@ -7,7 +7,7 @@ the step learns to find them:
   mean squared error and balance loss                     scmoe_balance_loss
   combine -> experts -> gate, dispatch -> norm, backwards scmoe_combine_backward, _gate_backward, _layer_norm_backward
 
-The gradient through the frozen experts is the only step in torch (the library has the forward pass of the experts alone).
+The gradient through the frozen experts is the only step in torch (of the two-layer experts the library has the forward pass alone).
 `python -m paper_2404_05019_amd.train_routing --steps 200` prints the losses and how often router and hidden router agree.
 """
 import argparse
