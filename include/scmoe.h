@@ -80,6 +80,8 @@ enum { SCMOE_CG_NONE = 0, SCMOE_CG_1 = 1, SCMOE_CG_2 = 2 };
 #define SCMOE_MAX_GATED_WIDTH (1 << 17)
 /* Upper limit on its packed rows. */
 #define SCMOE_MAX_GATED_ROWS (1 << 30)
+/* Upper limit on the width of a row that scmoe_checkpoint_pack takes. */
+#define SCMOE_MAX_CHECKPOINT_WIDTH (1 << 28)
 
 /* Shape and options of one layer.  Plain data, host memory, read during the call only. */
 typedef struct scmoe_desc {
@@ -590,7 +592,7 @@ int scmoe_combine_backward(const void* dy, int64_t lddy, int32_t dtype, const vo
  * 2^-126: rounded).
  * x: [max_rows, width], q: max_rows checkpoint rows of ldq bytes (a multiple of 16, at least width +
  * ceil(width / 32); scmoe_checkpoint_ld gives the least; bytes behind the scales are left alone).
- * width: a multiple of 8.  n_rows: one int32 on the DEVICE, the rows to be treated (offsets + E of a
+ * width: a multiple of 8, up to SCMOE_MAX_CHECKPOINT_WIDTH.  n_rows: one int32 on the DEVICE, the rows to be treated (offsets + E of a
  * dispatch; at most max_rows are), or NULL: all.  Rows past it are neither read nor written.
  */
 int scmoe_checkpoint_ld(int32_t width, int64_t* ld);      /* host only; `ld` is a host pointer */

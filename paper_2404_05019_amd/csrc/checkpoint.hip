@@ -151,7 +151,7 @@ int checkpoint_unpack(const void* q, int64_t ldq, const int32_t* n_rows, int64_t
 
 static int check_checkpoint(const void* x, int64_t ldx, int dtype, int32_t max_rows, int32_t width, const void* q, int64_t ldq) {
   if (!dtype_ok(dtype)) return SCMOE_ERR_DTYPE;
-  if (max_rows < 0 || width <= 0 || width % 8 != 0) return SCMOE_ERR_SHAPE;
+  if (max_rows < 0 || width <= 0 || width % 8 != 0 || width > SCMOE_MAX_CHECKPOINT_WIDTH) return SCMOE_ERR_SHAPE;   // (columns and their bytes: 32 bits)
   if (max_rows == 0) return SCMOE_OK;
   if (!x || !q) return SCMOE_ERR_NULL;
   return view_ok(x, ldx, width, dtype) && ckpt_view_ok(q, ldq, width) ? SCMOE_OK : SCMOE_ERR_SHAPE;
@@ -162,7 +162,7 @@ static int check_checkpoint(const void* x, int64_t ldx, int dtype, int32_t max_r
 extern "C" int scmoe_checkpoint_ld(int32_t width, int64_t* ld) {
   using namespace scmoe;
   if (!ld) return SCMOE_ERR_NULL;
-  if (width <= 0 || width % 8 != 0) return SCMOE_ERR_SHAPE;
+  if (width <= 0 || width % 8 != 0 || width > SCMOE_MAX_CHECKPOINT_WIDTH) return SCMOE_ERR_SHAPE;
   *ld = (ckpt_bytes(width) + 15) / 16 * 16;
   return SCMOE_OK;
 }

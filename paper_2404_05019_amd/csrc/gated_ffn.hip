@@ -25,8 +25,12 @@ static bool few_rows(int mode, int dtype, int64_t rows, int E) {
   return rows <= 4 || rows <= per * E;
 }
 
+static bool takes_few(int mode, int keep, int dtype, int64_t rows, int E) {
+  return ((mode == G_GATE && keep != KEEP_8BIT) || mode == G_DOWN) && few_rows(mode, dtype, rows, E);
+}
+
 static int launch_gated(const GatedArgs& a, int mode, int keep, int64_t max_rows, int dtype, hipStream_t stream) {
-  if (((mode == G_GATE && keep != KEEP_8BIT) || mode == G_DOWN) && few_rows(mode, dtype, max_rows, a.E)) return launch_gated_few(a, mode, keep, max_rows, dtype, stream);
+  if (takes_few(mode, keep, dtype, max_rows, a.E)) return launch_gated_few(a, mode, keep, max_rows, dtype, stream);
   return dtype == SCMOE_BF16 ? launch_gated_bf16(a, mode, keep, max_rows, stream) : launch_gated_f32(a, mode, keep, max_rows, stream);
 }
 
@@ -111,8 +115,8 @@ extern "C" int scmoe_gated_ffn(const void* x_perm, int64_t ld_perm, int32_t dtyp
   a.pre = static_cast<unsigned char*>(pre); a.ldpre = ldpre;
   a.j[0] = gated_job(x_perm, ld_perm, W1, ldw1, hidden, ldh, 0, F, d);
   const bool experts = second_is_the_experts(dtype, max_rows, E, d, F);
-  if (experts && dtype == SCMOE_BF16 && workspace != nullptr && ws_bytes >= ffn_mfma_scratch_bytes()) {
-    a.zero = static_cast<int*>(workspace);                  // (the counters of tiles that the second product cuts along K)
+  if (experts && dtype == SCMOE_BF16 && workspace != nullptr && ws_bytes >= ffn_mfma_scratch_bytes() && !takes_few(G_GATE, pre_keep, dtype, max_rows, E)) {
+    a.zero = static_cast<int*>(workspace);                  // (the counters of tiles that the second product cuts along K; the kernel for few rows clears none)
     a.zeros = ffn_mfma_counter_ints();
   }
   st = launch_gated(a, G_GATE, pre_keep, max_rows, dtype, s);

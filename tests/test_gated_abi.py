@@ -62,6 +62,7 @@ def lib():
     (NULL, dict(x=None)), (NULL, dict(q=None)), (SHAPE, dict(rows=-1)), (SHAPE, dict(w=0)), (SHAPE, dict(w=60)), (SHAPE, dict(x=P + 4)),
     (SHAPE, dict(q=P + 8)), (SHAPE, dict(ldx=56)), (SHAPE, dict(ldx=66)), (SHAPE, dict(ldq=64)), (SHAPE, dict(ldq=72)), (SHAPE, dict(dtype=BF16, ldx=68)),
     (SHAPE, dict(w=104, ldx=104, ldq=104)), (DTYPE, dict(dtype=2)), (DTYPE, dict(dtype=-1)),
+    (SHAPE, dict(w=(1 << 28) + 8, ldx=1 << 30, ldq=1 << 30)), (SHAPE, dict(w=(1 << 31) - 8, ldx=1 << 31, ldq=1 << 33, dtype=BF16)),
 ])
 def test_checkpoints_refuse(lib, call, want, bad):
     assert call(lib, **bad) == want
@@ -98,7 +99,8 @@ def test_backward_refuses(lib, want, bad):
 def test_sizes(lib):
     from paper_2404_05019_amd import binding as B
     assert [B.scmoe_checkpoint_ld(w) for w in (8, 32, 40, 480, 1000, 8192)] == [16, 48, 48, 496, 1040, 8448]
-    for w in (0, -8, 12):
+    assert B.scmoe_checkpoint_ld(1 << 28) == (1 << 28) + (1 << 23)
+    for w in (0, -8, 12, (1 << 28) + 8, (1 << 31) - 8):
         with pytest.raises(B.ScmoeError):
             B.scmoe_checkpoint_ld(w)
     assert lib.scmoe_checkpoint_ld(8, None) == NULL
@@ -175,6 +177,17 @@ def test_what_is_not_asked_for_is_not_needed(record):
                          (dict(dW1=None, x=None, xk=NOTHING), 3), (dict(), 3), (dict(xk=EIGHT), 4)):
         (st, lines), = record([("grad", kw)])
         assert st == 0 and len(lines) == launches, kw
+
+
+@pytest.mark.parametrize("keep", [NOTHING, FULL, EIGHT])
+def test_the_counters_of_a_cut_product_are_cleared(record, keep):
+    """By the first product's launch, or by one of their own where that is the kernel for few rows, which clears nothing."""
+    kw = dict(E=600, rows=1100, d=64, F=2048, dtype=BF16, ws=P, nb=BIG, keep=keep, pre=P if keep else None)
+    (st, lines), = record([("ffn", kw)])
+    names = [w[2] for w in lines]
+    assert st == 0 and "gemm_bf16_kernel" in names[-1]
+    assert ("zero_ints" in names[1]) == ("gated_few_kernel" in names[0]), names
+    assert ("gated_few_kernel" in names[0]) == (keep != EIGHT)
 
 
 def test_gradients_of_no_rows_are_written(record):

@@ -309,6 +309,14 @@ def test_few_rows_of_many_experts(counts, dtype, act):
     check_backward(b, b.x, b.pre)
 
 
+@pytest.mark.parametrize("counts", [[0] * 300 + [500] + [0] * 297 + [1, 599], [2] * 500 + [1] * 100])
+def test_few_rows_of_hundreds_of_experts(counts):
+    """The first product by the kernel for few rows, the second one's tiles cut along F, their counters in a workspace that holds anything."""
+    b = Block(counts, 64, 2048, "bf16", "silu", spare=0, seed=23)
+    b.forward(pre=b.pre)
+    check_forward(b)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_dx_in_the_place_of_dy_or_x(dtype):
     b = Block([33, 0, 140, 7], 136, 200, dtype, "silu", seed=22)
