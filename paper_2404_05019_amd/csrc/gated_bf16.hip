@@ -31,21 +31,8 @@ using GatedS = GatedCfg<false, 64, 64, 4, 1, 3>;     // 4 waves of 16 x 64, 64 K
 //   2000 rows, d = 512, F = 1024, E = 8        GATE 35 / 29 / 28, DH 72 / 57 / 49, DX 80 / 57 / 49, DW 57 / 57 / 65
 enum { TILES_256, TILES_256_128, TILES_128, TILES_64 };
 static int tiles_for(const GatedArgs& a, int mode, int64_t max_rows) {
-  const double cus = num_cus(), segs = static_cast<double>(a.E < max_rows ? a.E : max_rows);
-  // an expert's row tiles of that many rows: its last one half full, unless the average leaves room in one
-  auto row_tiles = [&](double rows) {
-    const double mean = static_cast<double>(max_rows) / segs;
-    return segs * (mean <= 0.75 * rows ? 1.0 : mean / rows + 0.5);
-  };
-  auto tiles = [&](int rows, int cols) {
-    double n = 0;
-    for (const GatedJob& j : a.j) {
-      if (j.C == nullptr) continue;
-      const double across = (j.N + cols - 1) / cols;
-      n += across * (mode == G_DW ? static_cast<double>((j.M + rows - 1) / rows) * a.E : row_tiles(rows));
-    }
-    return n;
-  };
+  const double cus = num_cus();
+  auto tiles = [&](int rows, int cols) { return likely_tiles(a, mode, max_rows, rows, cols); };
   auto rounds = [](double t) {
     const double whole = floor(t), rest = t - whole;
     return whole < 1.0 ? 1.0 : rest > 0.0 ? whole + 0.5 + 0.5 * rest : whole;
@@ -65,6 +52,28 @@ int launch_gated_bf16(const GatedArgs& a, int mode, int keep, int64_t max_rows, 
     case TILES_128: return launch_gated_mode<GatedU>(a, mode, keep, max_rows, stream);
     default: return launch_gated_rows<GatedS>(a, mode, keep, max_rows, stream);
   }
+}
+
+// DX and DW in one launch (which of the two forms, and when), us of a gradient, two launches / one:
+//  * On 128 x 128 tiles (DX on 64 x 64 ones where it has under a quarter as many tiles as compute units), where both together are at most 3.5 rounds:
+//    8192 rows, d = 384, F = 1536, E = 8 112 / 101; 4096, 768, 2048, 4 142 / 122; 2048, 1024, 4096, 1 164 / 147; 16384, 256, 1024, 4 126 / 108;
+//    1000, 512, 2048, 2 44 / 34; 300, 512, 4096, 1 51 / 44 (DX on 128 x 128 tiles: 67); 64, 768, 2048, 1 33 / 28; also where DX fills 3/8 to 5/8 of the units
+//    and DW is up to twelve rounds: 1000, 768, 2048, 16 120 / 108; 1500, 1024, 2048, 16 150 / 141; 300, 768, 2048, 16 91 / 89; but 64 tiles of DX
+//    (300, 1024, 4096, 8) 134 / 145.
+//  * On 256 x 256 tiles, where DX has a quarter to one of them a compute unit and DW twice as many, up to 24 a unit: 2000, 768, 2048, 64 315 / 283; 8192, 768,
+//    1536, 8 158 / 136; 1000, 1024, 2048, 32 217 / 187; 4096, 1536, 4096, 2 369 / 318; 8192, 768, 2048, 16 242 / 239; 6000, 512, 2048, 24 171 / 171; 5003, 1000, 2728,
+//    32 443 / 460; 8192, 1024, 2048, 8 240 / 242.  Beyond that two launches fill the chip for as long, and share the caches better: 16384, 1024, 4096, 8
+//    752 / 792; 32768, 2048, 8192, 16 5227 / 5834; 2000, 2048, 8192, 16 896 / 962; 16384, 512, 1024, 8 152 / 162.
+int launch_gated_gradients_bf16(const GatedArgs& x, const GatedArgs& w, int64_t max_rows, hipStream_t stream) {
+  const double cus = num_cus();
+  const double xu = likely_tiles(x, G_DX, max_rows, 128, 128), wu = likely_tiles(w, G_DW, max_rows, 128, 128);
+  const double xa = likely_tiles(x, G_DX, max_rows, 256, 256), wa = likely_tiles(w, G_DW, max_rows, 256, 256);
+  if (xu <= 1.5 * cus && xu + wu <= 3.5 * 2.0 * cus)
+    return xu < 0.25 * cus ? launch_gated_pair<GatedS, GatedU>(x, w, max_rows, stream) : launch_gated_pair<GatedU, GatedU>(x, w, max_rows, stream);
+  if (xu > 0.625 * cus && xa >= 0.25 * cus && xa <= cus && wa >= 2.0 * xa && wa <= 24.0 * cus) return launch_gated_pair<GatedA, GatedA>(x, w, max_rows, stream);
+  if (xu >= 0.375 * cus && xu <= 0.625 * cus && wu <= 12.0 * 2.0 * cus) return launch_gated_pair<GatedU, GatedU>(x, w, max_rows, stream);
+  const int st = launch_gated_bf16(w, G_DW, KEEP_NONE, max_rows, stream);
+  return st == SCMOE_OK ? launch_gated_bf16(x, G_DX, KEEP_NONE, max_rows, stream) : st;
 }
 
 }  // namespace scmoe

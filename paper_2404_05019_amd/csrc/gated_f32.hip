@@ -25,4 +25,17 @@ int launch_gated_f32(const GatedArgs& a, int mode, int keep, int64_t max_rows, h
   return launch_gated_rows<GatedG>(a, mode, keep, max_rows, stream);
 }
 
+// DX and DW in one launch, where DX has up to two tiles of 64 x 64 a compute unit (its own launch has three), and DW up to 24 rounds.  DX's tiles with three
+// stages, three workgroups a unit, up to 0.6 tiles a unit, where a tile's time counts; else two stages and four workgroups.  us of a
+// gradient, two launches / so with three stages / with two: 100 rows, d = 512, F = 2048, E = 8 125 / 111 / 136; 500, 384, 1536, 8 110 / 95 / 108; 16, 1024, 4096, 8
+// 280 / 266 / 310; 777, 1000, 1360, 5 164 / 158 / 152; 1000, 1024, 2048, 8 315 / 287 / 282; 5000, 256, 1024, 4 176 / 163 / 160; 300, 1024, 2048, 16 240 / 264 /
+// 242; more tiles: 2000, 1024, 2048, 8 429 / 453 / 432; 16384, 384, 1536, 8 933 / 966 / 946.
+int launch_gated_gradients_f32(const GatedArgs& x, const GatedArgs& w, int64_t max_rows, hipStream_t stream) {
+  const double cus = num_cus(), tx = likely_tiles(x, G_DX, max_rows, 64, 64);
+  if (tx <= 2.0 * cus && likely_tiles(w, G_DW, max_rows, 64, 64) <= 24.0 * 4.0 * cus)
+    return tx <= 0.6 * cus ? launch_gated_pair<GatedG, GatedD>(x, w, max_rows, stream) : launch_gated_pair<GatedD, GatedD>(x, w, max_rows, stream);
+  const int st = launch_gated_f32(w, G_DW, KEEP_NONE, max_rows, stream);
+  return st == SCMOE_OK ? launch_gated_f32(x, G_DX, KEEP_NONE, max_rows, stream) : st;
+}
+
 }  // namespace scmoe

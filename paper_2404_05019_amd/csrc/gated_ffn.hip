@@ -180,15 +180,19 @@ extern "C" int scmoe_gated_ffn_backward(const void* dy_perm, int64_t lddy, int32
       ldx = d;
     }
   }
+  GatedArgs b = a;
   if (dW1 || dW2) {
     int n = 0;
     if (dW1) a.j[n++] = gated_job(dpre, w.ldp, x, ldx, dW1, d, 2 * F, d, 0);
     if (dW2) a.j[n++] = gated_job(dy_perm, lddy, hid, w.ldh, dW2, F, d, F, 0);
-    st = launch_gated(a, G_DW, KEEP_NONE, max_rows, dtype, s);
-    if (st != SCMOE_OK || !dx_perm || max_rows == 0) return st;
+    if (!dx_perm || max_rows == 0) return launch_gated(a, G_DW, KEEP_NONE, max_rows, dtype, s);
   }
-  // (the last launch, so that dx may take the place of dy or x)
-  a.j[0] = gated_job(dpre, w.ldp, W1, ldw1, dx_perm, lddx, 0, d, 2 * F);
-  a.j[1] = GatedJob{};
-  return launch_gated(a, G_DX, KEEP_NONE, max_rows, dtype, s);
+  b.j[0] = gated_job(dpre, w.ldp, W1, ldw1, dx_perm, lddx, 0, d, 2 * F);
+  if (!dW1 && !dW2) return launch_gated(b, G_DX, KEEP_NONE, max_rows, dtype, s);
+  // dx may take the place of dy or of x, which dW1 and dW2 are made of: then it is made after them.
+  if (dx_perm == dy_perm || dx_perm == x) {
+    st = launch_gated(a, G_DW, KEEP_NONE, max_rows, dtype, s);
+    return st == SCMOE_OK ? launch_gated(b, G_DX, KEEP_NONE, max_rows, dtype, s) : st;
+  }
+  return dtype == SCMOE_BF16 ? launch_gated_gradients_bf16(b, a, max_rows, s) : launch_gated_gradients_f32(b, a, max_rows, s);
 }

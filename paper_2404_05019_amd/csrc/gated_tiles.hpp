@@ -23,6 +23,7 @@
 #include "gated_act.hpp"
 #include "rows.hpp"
 #include <atomic>
+#include <math.h>
 
 namespace scmoe {
 
@@ -200,8 +201,9 @@ __device__ __forceinline__ void gated_share(S& sched, int E, int lane) {
   sched.ngemm = sched.rr + (mine < 0 ? 0 : mine > chunk ? chunk : mine);
 }
 
+// What workgroup `block` of `blocks` does of a product.
 template <class CFG, int MODE, int KEEP, int ACT>
-__global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void gated_kernel(const GatedArgs p) {
+__device__ __forceinline__ void gated_product(const GatedArgs& p, const int block, const int blocks) {
   constexpr bool F32 = CFG::F32;
   constexpr int BM = CFG::BM, BN = CFG::BN, EB = CFG::EB, VE = CFG::VE, BK = CFG::BK, KS = CFG::KS, NS = CFG::NS;
   constexpr int MI = CFG::MI, NJ = CFG::NJ, TM = CFG::TM, TN = CFG::TN, STAGE = CFG::STAGE, A_BYTES = CFG::A_BYTES;
@@ -216,8 +218,8 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
   const int wave_m = wave / CFG::WN, wave_n = wave % CFG::WN;
 
   // ---- what this workgroup does: tiles slot, slot + nslots, ... of its XCD's share ---------------------------
-  const int xcd = blockIdx.x & 7, nslots = gridDim.x >> 3;
-  int it = blockIdx.x >> 3;
+  const int xcd = block & 7, nslots = blocks >> 3;
+  int it = block >> 3;
   constexpr int GM = MODE == G_GATE || MODE == G_DH ? 6 : 4;
   using Schedule = TileSchedule<BM, BNF, GM>;
   constexpr int RR = Schedule::RR;
@@ -466,7 +468,7 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
   if (it >= items) return;
   setup(it);
   issue_prologue();
-  if (MODE == G_GATE && p.zero != nullptr && blockIdx.x == 0)
+  if (MODE == G_GATE && p.zero != nullptr && block == 0)
     for (int i = threadIdx.x; i < p.zeros; i += CFG::THREADS) p.zero[i] = 0;
   for (;;) {
 #pragma unroll
@@ -836,18 +838,58 @@ __global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void
   }
 }
 
+template <class CFG, int MODE, int KEEP, int ACT>
+__global__ __launch_bounds__(CFG::THREADS, CFG::WG_PER_CU * CFG::WAVES / 4) void gated_kernel(const GatedArgs p) {
+  gated_product<CFG, MODE, KEEP, ACT>(p, blockIdx.x, gridDim.x);
+}
+
+// DX and DW, which both wait for DH alone, in one launch: the first xblocks workgroups have DX, the others DW.  By itself DX, one to two rounds
+// of long tiles, often leaves a good part of the compute units without work, and both have a start and an end.
+template <class X_, class W_>
+struct GatedPair {
+  using X = X_;
+  using W = W_;
+  static constexpr int LDS = X::LDS > W::LDS ? X::LDS : W::LDS;
+  static constexpr int WG_PER_CU = X::WG_PER_CU < W::WG_PER_CU ? X::WG_PER_CU : W::WG_PER_CU;
+  static_assert(X::THREADS == W::THREADS, "one launch");
+};
+template <class P>
+__global__ __launch_bounds__(P::X::THREADS, P::WG_PER_CU * P::X::WAVES / 4) void gated_pair_kernel(const GatedArgs x, const GatedArgs w, const int xblocks) {
+  const int block = blockIdx.x;
+  if (block < xblocks) gated_product<typename P::X, G_DX, KEEP_NONE, 0>(x, block, xblocks);
+  else gated_product<typename P::W, G_DW, KEEP_NONE, 0>(w, block - xblocks, gridDim.x - xblocks);
+}
+
 // ---- host side ----------------------------------------------------------------------------------------------
 
-template <class CFG, int MODE, int KEEP, int ACT>
-static int launch_gated_cfg(GatedArgs a, int64_t max_rows, hipStream_t stream) {
-  static std::atomic<bool> attr_set[64];
+// LDS of a kernel's launches, said once a device.
+template <class KERNEL>
+static int allow_lds(KERNEL* kernel, int bytes, std::atomic<bool>* said) {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = -1;
-  if (dev < 0 || !attr_set[dev].load(std::memory_order_acquire)) {
-    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(&gated_kernel<CFG, MODE, KEEP, ACT>), hipFuncAttributeMaxDynamicSharedMemorySize, CFG::LDS);
+  if (dev < 0 || !said[dev].load(std::memory_order_acquire)) {
+    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (err != hipSuccess) return hip_fail(err);
-    if (dev >= 0) attr_set[dev].store(true, std::memory_order_release);
+    if (dev >= 0) said[dev].store(true, std::memory_order_release);
   }
+  return SCMOE_OK;
+}
+
+// Tiles of a launch's products as the host expects them: an expert's last row tile half full, unless the average leaves room in one.
+inline double likely_tiles(const GatedArgs& a, int mode, int64_t max_rows, int rows, int cols) {
+  const double segs = static_cast<double>(a.E < max_rows ? a.E : max_rows), mean = max_rows > 0 ? static_cast<double>(max_rows) / segs : 0.0;
+  double n = 0;
+  for (const GatedJob& j : a.j) {
+    if (j.C == nullptr) continue;
+    const double across = (j.N + cols - 1) / cols;
+    n += across * (mode == G_DW ? static_cast<double>((j.M + rows - 1) / rows) * a.E : segs * (mean <= 0.75 * rows ? 1.0 : mean / rows + 0.5));
+  }
+  return n;
+}
+
+// Fills in the tiles of a launch's products; returns how many there are at most.
+template <class CFG, int MODE>
+static int64_t count_tiles(GatedArgs& a, int64_t max_rows) {
   constexpr int BNF = MODE == G_GATE ? CFG::BN / 2 : CFG::BN;
   int64_t tiles = 0;
   for (GatedJob& j : a.j) {
@@ -862,7 +904,15 @@ static int launch_gated_cfg(GatedArgs a, int64_t max_rows, hipStream_t stream) {
       tiles += (max_rows / CFG::BM + (a.E < max_rows ? a.E : max_rows)) * j.nt;
     }
   }
-  int64_t slots = (tiles + 7) / 8;
+  return tiles;
+}
+
+template <class CFG, int MODE, int KEEP, int ACT>
+static int launch_gated_cfg(GatedArgs a, int64_t max_rows, hipStream_t stream) {
+  static std::atomic<bool> said[64];
+  const int st = allow_lds(&gated_kernel<CFG, MODE, KEEP, ACT>, CFG::LDS, said);
+  if (st != SCMOE_OK) return st;
+  int64_t slots = (count_tiles<CFG, MODE>(a, max_rows) + 7) / 8;
   const int resident = (num_cus() / 8) * CFG::WG_PER_CU;
   if (slots > resident) slots = resident;
   if (slots < 1) slots = 1;
@@ -870,9 +920,36 @@ static int launch_gated_cfg(GatedArgs a, int64_t max_rows, hipStream_t stream) {
   return launch_status();
 }
 
+// The workgroups are shared out so that both products are likely to end at the same time: DX has one to a few long tiles a workgroup, DW many
+// short ones (with DX's tiles counted at most instead of as expected, 4000 rows, d = 512, F = 2048, E = 64, gradient 264 us, so 226).
+template <class X, class W>
+static int launch_gated_pair(GatedArgs x, GatedArgs w, int64_t max_rows, hipStream_t stream) {
+  using P = GatedPair<X, W>;
+  static std::atomic<bool> said[64];
+  const int st = allow_lds(&gated_pair_kernel<P>, P::LDS, said);
+  if (st != SCMOE_OK) return st;
+  count_tiles<X, G_DX>(x, max_rows);
+  count_tiles<W, G_DW>(w, max_rows);
+  const double tx = likely_tiles(x, G_DX, max_rows, X::BM, X::BN), tw = likely_tiles(w, G_DW, max_rows, W::BM, W::BN);
+  // a tile's time: its k-tiles, and three for its start and end
+  const double cx = (x.j[0].Kd / X::BK + 3.0) * X::BM * X::BN, cw = (static_cast<double>(max_rows) / w.E / W::BK + 0.5 + 3.0) * W::BM * W::BN;
+  const int resident = (num_cus() / 8) * P::WG_PER_CU;
+  int best = 1;
+  double least = 1e300;
+  for (int s = 1; s < resident; ++s) {
+    const double rx = ceil(tx / (8.0 * s)) * cx, rw = ceil(tw / (8.0 * (resident - s))) * cw, t = rx > rw ? rx : rw;
+    if (t < least) { least = t; best = s; }
+  }
+  hipLaunchKernelGGL((gated_pair_kernel<P>), dim3(static_cast<unsigned>(8 * resident)), dim3(X::THREADS), P::LDS, stream, x, w, 8 * best);
+  return launch_status();
+}
+
 // One launch of a product (DW: of one or two), of either type.
 int launch_gated_bf16(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream);
 int launch_gated_f32(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream);
+// DX and DW, in one launch where that is better.
+int launch_gated_gradients_bf16(const GatedArgs& x, const GatedArgs& w, int64_t max_rows, hipStream_t stream);
+int launch_gated_gradients_f32(const GatedArgs& x, const GatedArgs& w, int64_t max_rows, hipStream_t stream);
 
 // GATE (kept in full or not at all) and DOWN of a few rows.
 int launch_gated_few(const GatedArgs& a, int mode, int keep, int64_t max_rows, int dtype, hipStream_t stream);

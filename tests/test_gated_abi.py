@@ -190,6 +190,13 @@ def test_the_counters_of_a_cut_product_are_cleared(record, keep):
     assert ("gated_few_kernel" in names[0]) == (keep != EIGHT)
 
 
+def test_dx_that_takes_the_place_of_an_input_is_made_last(record):
+    """Else its launch may have the weights' gradients beside it."""
+    for kw, launches in ((dict(dx=2 * P), 2), (dict(dx=2 * P, x=2 * P), 3), (dict(dx=2 * P, dy=2 * P), 3), (dict(dx=2 * P, xk=EIGHT), 3)):
+        (st, lines), = record([("grad", kw)])
+        assert st == 0 and len(lines) == launches, kw
+
+
 def test_gradients_of_no_rows_are_written(record):
     none = dict(rows=0, dy=None, x=None, pre=None, W1=None, W2=None, ws=None, nb=0)
     for kw in (none, dict(none, dW1=None), dict(none, dW2=None), dict(none, dx=None)):

@@ -12,9 +12,15 @@ GATE, DOWN, DH, DX, DW = range(5)
 
 
 def kernels(lines):
-    """(mode, how it is kept, type, tile) of the block's own kernels; the others by name."""
+    """(mode, how it is kept, type, tile) of the block's own kernels, (type, tiles of DX and of DW with their stages) of those that have both
+    gradients; the others by name."""
     got = []
     for w in lines:
+        m = re.search(r"gated_pair_kernelINS_9GatedPairINS_8GatedCfgILb(\d)ELi(\d+)ELi\d+ELi\dELi\dELi(\d).*?EE(S3_|NS2_ILb\dELi(\d+)ELi\d+ELi\dELi\dELi(\d))", w[2])
+        if m:
+            x = (int(m[2]), int(m[3]))
+            got.append(("f32" if m[1] == "1" else "bf16", x, x if m[4] == "S3_" else (int(m[5]), int(m[6]))))
+            continue
         m = re.search(r"gated_kernel.*GatedCfgILb(\d)ELi(\d+)ELi(\d+)E.*?EELi(\d)ELi(\d)ELi\d", w[2])
         got.append((int(m[4]), int(m[5]), "f32" if m[1] == "1" else "bf16", (int(m[2]), int(m[3]))) if m else re.search(r"[a-z_0-9]+_kernel|gemm_bf16_kernel|zero_ints", w[2])[0])
     return got
@@ -25,7 +31,9 @@ def calls(rows, E, d, F, dtype):
     for keep in (NOTHING, FULL, EIGHT):
         yield "ffn", dict(kw, keep=keep, pre=P if keep else None)
     for keep in (FULL, EIGHT):
-        yield "grad", dict(kw, xk=keep, pk=keep)
+        yield "grad", dict(kw, xk=keep, pk=keep, dx=2 * P)
+    yield "grad", dict(kw, dx=None)
+    yield "grad", dict(kw, dW1=None, dW2=None)
 
 
 def test_every_form_is_run(record):  # noqa: F811
@@ -43,11 +51,12 @@ def test_every_form_is_run(record):  # noqa: F811
     want += [(GATE, k, "bf16", t) for k in (NOTHING, FULL, EIGHT) for t in (T256, T128, T64)] + [(DH, k, "bf16", t) for k in (FULL, EIGHT) for t in (T256, T128, T64)]
     for t in (T128, T64):
         want += [(m, NOTHING, "f32", t) for m in (DOWN, DX, DW)] + [(GATE, k, "f32", t) for k in (NOTHING, FULL, EIGHT)] + [(DH, k, "f32", t) for k in (FULL, EIGHT)]
-    assert not [k for k in want if k not in taken], sorted(taken.items())
-    assert sorted(taken) == sorted(want)
+    want += [("bf16", t, w) for t, w in (((256, 2), (256, 2)), ((128, 2), (128, 2)), ((64, 3), (128, 2)))] + [("f32", (64, n), (64, 2)) for n in (2, 3)]
+    assert not [k for k in want if k not in taken], sorted(map(str, taken.items()))
+    assert set(taken) == set(want)
 
 
-@pytest.mark.parametrize("kernel", ["gated_kernel", "gated_few_kernel", "checkpoint_kernel"])
+@pytest.mark.parametrize("kernel", ["gated_kernel", "gated_pair_kernel", "gated_few_kernel", "checkpoint_kernel"])
 def test_the_kernels_fit_their_registers(scratch, kernel):  # noqa: F811
     """A register that goes to memory and back waits for the copies that are kept in flight."""
     of = {k: v for k, v in scratch.items() if kernel in k}

@@ -268,6 +268,9 @@ FORMS = {
     "narrow_bf16": ([100, 3, 0, 77], 200, 264, "bf16"),
     "wide_f32": ([2300, 0, 1999, 2601, 1, 3100, 3200, 3300], 1000, 4104, "f32"),
     "narrow_f32": ([100, 3, 0, 77], 200, 264, "f32"),
+    "middle_f32": ([300, 0, 215, 1, 270], 776, 520, "f32"),
+    "long_f32": ([0, 39, 1], 136, 2056, "f32"),
+    "short_bf16": ([1024, 700, 1, 0, 1003, 1299], 392, 1032, "bf16"),
 }
 
 
@@ -289,6 +292,12 @@ def test_forms_of_the_kernels(form, keep):
         B.scmoe_checkpoint_pack(b.x, b.x8, n_rows=b.offsets[-1:])
         b.backward(b.x8, b.pre8)
         check_backward(b, restored(b.x8[:b.K], b.K, d), restored(b.pre8[:2 * b.K], 2 * b.K, F).reshape(b.K, 2 * F))
+    for n in (("dx_perm",), ("dW1", "dW2")):        # (not both: a launch of its own)
+        b.dx.fill_(NAN)
+        b.dW1.fill_(NAN)
+        b.dW2.fill_(NAN)
+        b.backward(b.x, b.pre if keep == "full" else b.pre8, **{k: None for k in ("dx_perm", "dW1", "dW2") if k not in n})
+        check_backward(b, b.x, b.pre if keep == "full" else restored(b.pre8[:2 * b.K], 2 * b.K, F).reshape(b.K, 2 * F), [k[:2] if k == "dx_perm" else k for k in n])
     b.forward()                                     # (nothing kept)
     check_forward(b, keep="")
 
