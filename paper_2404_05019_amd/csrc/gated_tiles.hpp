@@ -423,7 +423,9 @@ __device__ __forceinline__ void gated_product(const GatedArgs& p, const int bloc
   f32x4_t acc[MI][NJ];
   g_u32x4 wf[2][NJ], xf[2][H];
   static_assert((NS * KS) % 2 == 0, "the weight-fragment buffers alternate over the unrolled k loop");
-  auto load_frags = [&](int R, int hs) {                  // half-step hs: step hs % KS, row-subtile half hs / KS
+  // halves_c: how many halves of its rows the wave has (those past the segment are not read or multiplied)
+  auto load_frags = [&](int R, int hs, auto halves_c) {   // half-step hs: step hs % KS, row-subtile half hs / KS
+    if (hs / KS >= decltype(halves_c)::value) return;
     const int s = hs % KS, half = hs / KS, st = R * STAGE, wbuf = (R * KS + s) & 1, xbuf = hs & 1;
 #pragma unroll
     for (int t = 0; t < (H > NJ ? H : NJ); ++t) {
@@ -437,7 +439,8 @@ __device__ __forceinline__ void gated_product(const GatedArgs& p, const int bloc
       }
     }
   };
-  auto mfma_step = [&](int R, int hs) {
+  auto mfma_step = [&](int R, int hs, auto halves_c) {
+    if (hs / KS >= decltype(halves_c)::value) return;
     const int s = hs % KS, half = hs / KS, wbuf = (R * KS + s) & 1, xbuf = hs & 1;
 #pragma unroll
     for (int c = 0; c < (F32 ? 4 : 1); ++c)
@@ -452,10 +455,12 @@ __device__ __forceinline__ void gated_product(const GatedArgs& p, const int bloc
         }
   };
   // issue order of a half-step: a matrix instruction, then reads for the next half-step
-  auto interleave = [&](auto next_hs_c) {
+  auto interleave = [&](auto hs_c, auto next_hs_c, auto halves_c) {
+    constexpr int halves = decltype(halves_c)::value, next = decltype(next_hs_c)::value / KS;
+    if constexpr (decltype(hs_c)::value / KS >= halves) return;
     constexpr int RA = A_ACROSS ? (F32 ? 4 : 2) : 1, RB = B_ACROSS ? (F32 ? 4 : 2) : 1;
-    constexpr int reads = H * RA + (decltype(next_hs_c)::value / KS ? 0 : NJ * RB);
-    constexpr int mfmas = H * NJ * (F32 ? 4 : 1), per = (reads + mfmas - 1) / mfmas, groups = reads / per;
+    constexpr int reads = next >= halves ? 0 : H * RA + (next ? 0 : NJ * RB);
+    constexpr int mfmas = H * NJ * (F32 ? 4 : 1), per = reads > mfmas ? (reads + mfmas - 1) / mfmas : 1, groups = reads / per;
 #pragma unroll
     for (int q = 0; q < groups; ++q) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -483,7 +488,7 @@ __device__ __forceinline__ void gated_product(const GatedArgs& p, const int bloc
     // One k-tile (the order of its half-steps, copies and barriers is gemm_bf16_kernel's): B and the first halves of the rows are
     // refilled with k-tile kt + NS while the second halves are multiplied, these behind a second barrier.  Without halves the whole stage
     // is refilled ahead of the last step, when its fragments are in registers.
-    auto k_tile = [&](auto stage_c, auto steady_c, int kt) {
+    auto k_tile = [&](auto stage_c, auto steady_c, auto halves_c, int kt) {
       constexpr int stage = decltype(stage_c)::value;
       constexpr bool steady = decltype(steady_c)::value;      // k-tiles kt + 1 .. kt + NS all exist, and are whole
       constexpr int next = stage + 1 == NS ? 0 : stage + 1;
@@ -513,14 +518,14 @@ __device__ __forceinline__ void gated_product(const GatedArgs& p, const int bloc
               else issue_ba0(kt + NS, stage, steady_c);
             }
             __builtin_amdgcn_sched_barrier(0);
-            load_frags(next, 0);
+            load_frags(next, 0, halves_c);
           }
-          mfma_step(stage, hs);
-          if constexpr (steady) interleave(std::integral_constant<int, 0>{});
+          mfma_step(stage, hs, halves_c);
+          if constexpr (steady) interleave(hs_c, std::integral_constant<int, 0>{}, halves_c);
         } else {
-          load_frags(stage, hs + 1);
-          mfma_step(stage, hs);
-          interleave(std::integral_constant<int, hs + 1>{});
+          load_frags(stage, hs + 1, halves_c);
+          mfma_step(stage, hs, halves_c);
+          interleave(hs_c, std::integral_constant<int, hs + 1>{}, halves_c);
         }
       });
     };
@@ -540,11 +545,11 @@ __device__ __forceinline__ void gated_product(const GatedArgs& p, const int bloc
         }
     };
     next_part(std::true_type{});
-    if (nk > 0) {
-      load_frags(0, 0);
+    auto multiply = [&](auto halves_c) {
+      load_frags(0, 0, halves_c);
       int kt = 0;
       const int whole = k_all / BK;
-      auto turn = [&]() { static_for<0, NS>([&](auto s) { k_tile(s, bool_constant<true>{}, kt + decltype(s)::value); }); };
+      auto turn = [&]() { static_for<0, NS>([&](auto s) { k_tile(s, bool_constant<true>{}, halves_c, kt + decltype(s)::value); }); };
       if constexpr (F32) {
         while (kt + 2 * NS <= whole) {
           const int end = kt + PART < whole ? kt + PART : whole;
@@ -556,8 +561,17 @@ __device__ __forceinline__ void gated_product(const GatedArgs& p, const int bloc
       }
       for (; kt < nk; kt += NS)
         static_for<0, NS>([&](auto s) {
-          if (kt + decltype(s)::value < nk) k_tile(s, bool_constant<false>{}, kt + decltype(s)::value);
+          if (kt + decltype(s)::value < nk) k_tile(s, bool_constant<false>{}, halves_c, kt + decltype(s)::value);
         });
+    };
+    if (nk > 0) {
+      // DX, whose tiles stay with few rows for a long k where it shares a launch with DW: a wave without rows, or with a half of them, leaves
+      // out the products of the others (gradient of 2000 rows, d = 768, F = 2048, E = 64 283 us, so 270; 4000, 1024, 1024, 64 216, so 199).  The
+      // other products gain nothing (their time is the weights').
+      const int rows_here = row_end - row0 - wave_m * TM;
+      if (MODE == G_DX && NH > 1 && rows_here <= 0) multiply(integral_constant<int, 0>{});
+      else if (MODE == G_DX && NH > 1 && rows_here <= H * 16) multiply(integral_constant<int, 1>{});
+      else multiply(integral_constant<int, NH>{});
       if constexpr (F32) {
 #pragma unroll
         for (int i = 0; i < MI; ++i)
