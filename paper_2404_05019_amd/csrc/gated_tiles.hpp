@@ -18,6 +18,8 @@
 //  * Rows past a segment, columns past a matrix and k past its end read zeros (offsets outside the buffer), in both operands, so that what
 //    lies there (another expert's rows, NaN) reaches nothing.
 //  * Persistent workgroups, as in ffn_mfma.hip, whose schedule, barrier and two-group refill of a stage these kernels share.
+// Bound by the matrix rate at the power limit where the segments are long (32768 rows, d = 2048, F = 8192, E = 16: DW 1378 TFLOP/s, DX 1402, DH
+// 976, whose epilogue has 26 vector operations an element), by streaming the weights where they are short (64 rows: GATE 4.9 TB/s).
 #pragma once
 #include "checkpoint.hpp"
 #include "gated_act.hpp"
@@ -947,7 +949,7 @@ static int launch_gated_pair(GatedArgs x, GatedArgs w, int64_t max_rows, hipStre
   const double tx = likely_tiles(x, G_DX, max_rows, X::BM, X::BN), tw = likely_tiles(w, G_DW, max_rows, W::BM, W::BN);
   // a tile's time: its k-tiles, and three for its start and end
   const double cx = (x.j[0].Kd / X::BK + 3.0) * X::BM * X::BN, cw = (static_cast<double>(max_rows) / w.E / W::BK + 0.5 + 3.0) * W::BM * W::BN;
-  const int resident = (num_cus() / 8) * P::WG_PER_CU;
+  const int each = (num_cus() / 8) * P::WG_PER_CU, resident = each < 2 ? 2 : each;     // (both have some)
   int best = 1;
   double least = 1e300;
   for (int s = 1; s < resident; ++s) {
