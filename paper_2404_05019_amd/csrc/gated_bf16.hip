@@ -22,13 +22,17 @@ using GatedS = GatedCfg<false, 64, 64, 4, 1, 3>;     // 4 waves of 16 x 64, 64 K
 // 256 x 128 tiles against those that would be taken else:
 //   5003 rows, d = 1000, F = 2728, E = 32      DOWN 186 / 199, DX 446 / 465;   6000, d = 1024, F = 4096, E = 8  DX 374 / 391
 //   but 3001, d = 768, F = 2048, E = 12        DX 155 / 139;   8192, d = 384, F = 1536, E = 8  DX 124 / 117
-// 64 x 64 tiles where the 128 x 128 ones would leave half of the compute units without work, or are fewer than 1.5 of them with a short K; their rows of an
-// operand across k are 128 bytes long, which streams weights worse, and a gradient of weights (all tiles are written, whatever the rows)
+// 64 x 64 tiles where the 128 x 128 ones would leave half of the compute units without work, or, with a short K, are fewer than 1.5 of them (GATE 0.6, DH 0.7,
+// where the segments are not short as well); their rows of an operand across k are 128 bytes long, which streams weights worse, and a gradient of weights (all tiles are written, whatever the rows)
 // always has tiles enough:
 //   1 row, d = 2048, F = 8192, E = 16          GATE 60 / 38 / 33, DH 447 / 426 / 421, DX 581 / 427 / 388
 //   30 rows, d = 1000, F = 2728, E = 8         GATE 47 / 41 / 38
 //   500 rows, d = 1000, F = 2728, E = 8        GATE 74 / 70 / 71, DH 148 / 134 / 133, DX 198 / 133 / 122
 //   2000 rows, d = 512, F = 1024, E = 8        GATE 35 / 29 / 28, DH 72 / 57 / 49, DX 80 / 57 / 49, DW 57 / 57 / 65
+// 128 x 128 / 64 x 64 with a short K, and their number of the larger tiles:
+//   GATE  3000 rows, d = 512, F = 512, E = 12 (235) 21.8 / 25.6; 1500, 768, 1024, 8 (251) 25.5 / 29.2; 1000, 512, 2048, 2 (282) 24.8 / 27.2; 300, 512, 4096, 1
+//         (182) 23.8 / 25.0; but 500, 512, 1024, 8 (128) 19.4 / 18.8; short segments: 200, 1024, 4096, 4 (256) 35.8 / 34.6; 30, 1000, 2728, 8 (344) 41 / 38
+//   DH    1000, 1024, 2048, 8 (189) 98 / 104; 4096, 128, 1024, 4 (272) 34.7 / 36.6; but 2000, 512, 1024, 8 (157) 36.2 / 33.8; 1200, 1024, 2048, 20 (320) 166 / 160
 enum { TILES_256, TILES_256_128, TILES_128, TILES_64 };
 static int tiles_for(const GatedArgs& a, int mode, int64_t max_rows) {
   const double cus = num_cus();
@@ -39,7 +43,9 @@ static int tiles_for(const GatedArgs& a, int mode, int64_t max_rows) {
   };
   const bool gate = mode == G_GATE;                            // (half as many columns: a tile has those of g and of u)
   const double small = tiles(128, gate ? 64 : 128);
-  if (mode != G_DW && small < (a.j[0].Kd < 2048 ? 1.5 : 0.5) * cus) return TILES_64;
+  const bool short_segments = static_cast<double>(max_rows) <= 56.0 * (a.E < max_rows ? a.E : static_cast<double>(max_rows));
+  const double limit = a.j[0].Kd >= 2048 ? 0.5 : short_segments || mode == G_DOWN || mode == G_DX ? 1.5 : gate ? 0.6 : 0.7;
+  if (mode != G_DW && small < limit * cus) return TILES_64;
   const double t256 = 4.0 * rounds(tiles(256, gate ? 128 : 256) / cus), t128 = small <= cus ? 2.0 : 3.0 * rounds(small / (2.0 * cus));
   if ((mode == G_DOWN || mode == G_DX) && 2.6 * rounds(tiles(256, 128) / cus) < (t256 < t128 ? t256 : t128)) return TILES_256_128;
   return t256 <= t128 ? TILES_256 : TILES_128;
