@@ -575,6 +575,16 @@ def _experts(t, shape, dtype, device):
     return t.data_ptr(), _ldw(t)
 
 
+def _experts_grad(t, shape, dtype, device):
+    """Address of the gradient of weights [E, out, in], without gaps (None: not given).  A flat one is taken as well; any other shape,
+    whose elements may be as many, is refused."""
+    if t is None:
+        return None
+    if t.dim() != 1 and tuple(t.shape) != shape:
+        _refuse(t, "%s of %s" % (shape, dtype))
+    return _dense(t, shape[0] * shape[1] * shape[2], device, dtype)
+
+
 def scmoe_gated_ffn_workspace_bytes(dtype, d, F):
     out = C.c_size_t(0)
     _check(lib().scmoe_gated_ffn_workspace_bytes(dtype, d, F, C.byref(out)), "scmoe_gated_ffn_workspace_bytes")
@@ -601,8 +611,8 @@ def scmoe_gated_ffn_backward_workspace_bytes(dtype, max_rows, E, d, F):
 
 
 def scmoe_gated_ffn_backward(dy_perm, x, pre, offsets, max_rows, W1, W2, act=SILU, dx_perm=None, dW1=None, dW2=None, workspace=None, stream=None):
-    """dx_perm, dW1 and dW2 (each may be None) of scmoe_gated_ffn.  x: its input rows, pre: what it kept; each in the type of dy_perm
-    or in 8 bits (torch.uint8)."""
+    """dx_perm, dW1 and dW2 (each may be None; [E, 2 F, d] and [E, d, F], or flat) of scmoe_gated_ffn.  x: its input rows, pre: what it
+    kept; each in the type of dy_perm or in 8 bits (torch.uint8)."""
     E, d, F = W2.shape
     dtype, (dev, hs) = dy_perm.dtype, _place(dy_perm, stream)
     (gp, ldg), (dp, ldd) = (_packed_rows(t, max_rows, d, dtype, dev) for t in (dy_perm, dx_perm))
@@ -610,5 +620,5 @@ def scmoe_gated_ffn_backward(dy_perm, x, pre, offsets, max_rows, W1, W2, act=SIL
     (xp, ldx, xk), (pp, ldp, pk) = _kept(x, max_rows, d, 1, dtype, dev), _kept(pre, max_rows, F, 2, dtype, dev)
     wp, nb = _scratch(workspace, dev)
     _check(lib().scmoe_gated_ffn_backward(gp, ldg, dtype_code(dy_perm), xp, ldx, xk, pp, ldp, pk, _dense(offsets, E + 1, dev, torch.int32), max_rows, E, d, F,
-                                          w1, ld1, w2, ld2, act, dp, ldd, _dense(dW1, 2 * E * F * d, dev, dtype), _dense(dW2, E * d * F, dev, dtype), wp, nb,
-                                          hs), "scmoe_gated_ffn_backward")
+                                          w1, ld1, w2, ld2, act, dp, ldd, _experts_grad(dW1, (E, 2 * F, d), dtype, dev), _experts_grad(dW2, (E, d, F), dtype, dev),
+                                          wp, nb, hs), "scmoe_gated_ffn_backward")
