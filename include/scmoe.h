@@ -624,7 +624,8 @@ int scmoe_gated_ffn_workspace_bytes(int32_t dtype, int32_t d, int32_t F, size_t*
  *   SCMOE_KEEP_8BIT     pre: 2 max_rows checkpoint rows of width F (ldpre: bytes of one); g of row r is
  *                       checkpoint row 2 r, u is 2 r + 1.  The codes are made from the fp32 sums.
  * fp32 accumulation; bf16: hidden, g, u and y are rounded once each on store, hidden from the fp32 g and
- * u.  Results are the same from call to call.
+ * u.  act(g) of an fp32 g is right to 8e-5 of itself (fp32: some roundings, and what an argument of e^x that
+ * is rounded makes of it) down to where e^x underflows.  Results are the same from call to call.
  * workspace: optional device scratch (16-byte aligned) of scmoe_gated_ffn_workspace_bytes bytes; NULL or
  * less of it: slower where it would be used.
  */
