@@ -23,6 +23,7 @@
 #pragma once
 #include "checkpoint.hpp"
 #include "gated_act.hpp"
+#include "pair_share.hpp"
 #include "rows.hpp"
 #include <atomic>
 #include <math.h>
@@ -936,8 +937,25 @@ static int launch_gated_cfg(GatedArgs a, int64_t max_rows, hipStream_t stream) {
   return launch_status();
 }
 
-// The workgroups are shared out so that both products are likely to end at the same time: DX has one to a few long tiles a workgroup, DW many
-// short ones (with DX's tiles counted at most instead of as expected, 4000 rows, d = 512, F = 2048, E = 64, gradient 264 us, so 226).
+// A tile's time, in products of a k-tile's width: its k-tiles, and three for its start and end.
+template <class CFG, int MODE>
+static double tile_cost(const GatedArgs& a, int64_t max_rows) {
+  const double k = MODE == G_DW ? static_cast<double>(max_rows) / a.E / CFG::BK + 0.5 : a.j[0].Kd / CFG::BK;
+  return (k + 3.0) * CFG::BM * CFG::BN;
+}
+
+// (DX's tiles as expected, not as many as there may be: 4000 rows, d = 512, F = 2048, E = 64, gradient 226 us, the other way 264.)
+template <class X, class W>
+static int pair_resident() {
+  const int each = (num_cus() / 8) * GatedPair<X, W>::WG_PER_CU;
+  return each < 2 ? 2 : each;
+}
+template <class X, class W>
+static PairShare share_gated_pair(const GatedArgs& x, const GatedArgs& w, int64_t max_rows) {
+  return share_pair(likely_tiles(x, G_DX, max_rows, X::BM, X::BN), tile_cost<X, G_DX>(x, max_rows), likely_tiles(w, G_DW, max_rows, W::BM, W::BN),
+                    tile_cost<W, G_DW>(w, max_rows), pair_resident<X, W>(), num_cus());
+}
+
 template <class X, class W>
 static int launch_gated_pair(GatedArgs x, GatedArgs w, int64_t max_rows, hipStream_t stream) {
   using P = GatedPair<X, W>;
@@ -946,17 +964,8 @@ static int launch_gated_pair(GatedArgs x, GatedArgs w, int64_t max_rows, hipStre
   if (st != SCMOE_OK) return st;
   count_tiles<X, G_DX>(x, max_rows);
   count_tiles<W, G_DW>(w, max_rows);
-  const double tx = likely_tiles(x, G_DX, max_rows, X::BM, X::BN), tw = likely_tiles(w, G_DW, max_rows, W::BM, W::BN);
-  // a tile's time: its k-tiles, and three for its start and end
-  const double cx = (x.j[0].Kd / X::BK + 3.0) * X::BM * X::BN, cw = (static_cast<double>(max_rows) / w.E / W::BK + 0.5 + 3.0) * W::BM * W::BN;
-  const int each = (num_cus() / 8) * P::WG_PER_CU, resident = each < 2 ? 2 : each;     // (both have some)
-  int best = 1;
-  double least = 1e300;
-  for (int s = 1; s < resident; ++s) {
-    const double rx = ceil(tx / (8.0 * s)) * cx, rw = ceil(tw / (8.0 * (resident - s))) * cw, t = rx > rw ? rx : rw;
-    if (t < least) { least = t; best = s; }
-  }
-  hipLaunchKernelGGL((gated_pair_kernel<P>), dim3(static_cast<unsigned>(8 * resident)), dim3(X::THREADS), P::LDS, stream, x, w, 8 * best);
+  hipLaunchKernelGGL((gated_pair_kernel<P>), dim3(static_cast<unsigned>(8 * pair_resident<X, W>())), dim3(X::THREADS), P::LDS, stream, x, w,
+                     8 * share_gated_pair<X, W>(x, w, max_rows).first);
   return launch_status();
 }
 
