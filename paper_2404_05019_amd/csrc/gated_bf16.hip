@@ -1,5 +1,6 @@
 // The gated feed-forward block's products in bf16 (gated_tiles.hpp).
 #include "gated_tiles.hpp"
+#include <algorithm>
 #include <math.h>
 
 namespace scmoe {
@@ -34,7 +35,8 @@ using GatedS = GatedCfg<false, 64, 64, 4, 1, 3>;     // 4 waves of 16 x 64, 64 K
 //         (182) 23.8 / 25.0; but 500, 512, 1024, 8 (128) 19.4 / 18.8; short segments: 200, 1024, 4096, 4 (256) 35.8 / 34.6; 30, 1000, 2728, 8 (344) 41 / 38
 //   DH    1000, 1024, 2048, 8 (189) 98 / 104; 4096, 128, 1024, 4 (272) 34.7 / 36.6; but 2000, 512, 1024, 8 (157) 36.2 / 33.8; 1200, 1024, 2048, 20 (320) 166 / 160
 enum { TILES_256, TILES_256_128, TILES_128, TILES_64 };
-static int tiles_for(const GatedArgs& a, int mode, int64_t max_rows) {
+struct TileTimes { double small, t256, t128, t256_128; };      // how many 128 x 128 tiles; times, 4 of which are a 256 x 256 tile's
+static TileTimes tile_times(const GatedArgs& a, int mode, int64_t max_rows) {
   const double cus = num_cus();
   auto tiles = [&](int rows, int cols) { return likely_tiles(a, mode, max_rows, rows, cols); };
   auto rounds = [](double t) {
@@ -42,13 +44,20 @@ static int tiles_for(const GatedArgs& a, int mode, int64_t max_rows) {
     return whole < 1.0 ? 1.0 : rest > 0.0 ? whole + 0.5 + 0.5 * rest : whole;
   };
   const bool gate = mode == G_GATE;                            // (half as many columns: a tile has those of g and of u)
-  const double small = tiles(128, gate ? 64 : 128);
-  const bool short_segments = static_cast<double>(max_rows) <= 56.0 * (a.E < max_rows ? a.E : static_cast<double>(max_rows));
-  const double limit = a.j[0].Kd >= 2048 ? 0.5 : short_segments || mode == G_DOWN || mode == G_DX ? 1.5 : gate ? 0.6 : 0.7;
-  if (mode != G_DW && small < limit * cus) return TILES_64;
-  const double t256 = 4.0 * rounds(tiles(256, gate ? 128 : 256) / cus), t128 = small <= cus ? 2.0 : 3.0 * rounds(small / (2.0 * cus));
-  if ((mode == G_DOWN || mode == G_DX) && 2.6 * rounds(tiles(256, 128) / cus) < (t256 < t128 ? t256 : t128)) return TILES_256_128;
-  return t256 <= t128 ? TILES_256 : TILES_128;
+  TileTimes t;
+  t.small = tiles(128, gate ? 64 : 128);
+  t.t256 = 4.0 * rounds(tiles(256, gate ? 128 : 256) / cus);
+  t.t128 = t.small <= cus ? 2.0 : 3.0 * rounds(t.small / (2.0 * cus));
+  t.t256_128 = mode == G_DOWN || mode == G_DX ? 2.6 * rounds(tiles(256, 128) / cus) : 1e300;
+  return t;
+}
+static bool short_segments(const GatedArgs& a, int64_t max_rows) { return max_rows <= 56 * (a.E < max_rows ? a.E : max_rows); }
+static int tiles_for(const GatedArgs& a, int mode, int64_t max_rows) {
+  const TileTimes t = tile_times(a, mode, max_rows);
+  const double limit = a.j[0].Kd >= 2048 ? 0.5 : short_segments(a, max_rows) || mode == G_DOWN || mode == G_DX ? 1.5 : mode == G_GATE ? 0.6 : 0.7;
+  if (mode != G_DW && t.small < limit * num_cus()) return TILES_64;
+  if (t.t256_128 < (t.t256 < t.t128 ? t.t256 : t.t128)) return TILES_256_128;
+  return t.t256 <= t.t128 ? TILES_256 : TILES_128;
 }
 
 int launch_gated_bf16(const GatedArgs& a, int mode, int keep, int64_t max_rows, hipStream_t stream) {
@@ -64,20 +73,33 @@ int launch_gated_bf16(const GatedArgs& a, int mode, int keep, int64_t max_rows, 
 //  * On 128 x 128 tiles (DX on 64 x 64 ones where it has under a quarter as many tiles as compute units), where both together are at most 3.5 rounds:
 //    8192 rows, d = 384, F = 1536, E = 8 112 / 101; 4096, 768, 2048, 4 142 / 122; 2048, 1024, 4096, 1 164 / 147; 16384, 256, 1024, 4 126 / 108;
 //    1000, 512, 2048, 2 44 / 34; 300, 512, 4096, 1 51 / 44 (DX on 128 x 128 tiles: 67); 64, 768, 2048, 1 33 / 28; also where DX fills 3/8 to 5/8 of the units
-//    and DW is up to twelve rounds: 1000, 768, 2048, 16 120 / 108; 1500, 1024, 2048, 16 150 / 141; 300, 768, 2048, 16 91 / 89; but 64 tiles of DX
-//    (300, 1024, 4096, 8) 134 / 145.
-//  * On 256 x 256 tiles, where DX has a quarter to one of them a compute unit and DW twice as many, up to 24 a unit: 2000, 768, 2048, 64 315 / 283; 8192, 768,
-//    1536, 8 158 / 136; 1000, 1024, 2048, 32 217 / 187; 4096, 1536, 4096, 2 369 / 318; 8192, 768, 2048, 16 242 / 239; 6000, 512, 2048, 24 171 / 171; 5003, 1000, 2728,
-//    32 443 / 460; 8192, 1024, 2048, 8 240 / 242.  Beyond that two launches fill the chip for as long, and share the caches better: 16384, 1024, 4096, 8
+//    and DW is up to twelve rounds: 1000, 768, 2048, 16 120 / 108; 1500, 1024, 2048, 16 150 / 141; 2205, 576, 2232, 16 142 / 128; 744, 1336, 2408, 9 169 / 153; but
+//    64 tiles of DX (300, 1024, 4096, 8) 134 / 145.  With short segments, whose tiles of DW have one k-tile, up to seven rounds: 1068, 376, 760, 42 (4.4) 56 / 53; 1479,
+//    344, 784, 43 (5) 69 / 60; but 396, 720, 1384, 20 (7.7) 77 / 83; 54, 624, 1736, 22 (9) 88 / 98; 843, 480, 1816, 30 (10) 99 / 108.
+//  * On 256 x 256 tiles, where DX has a quarter to one of them a compute unit and DW twice as many, up to 24 a unit: 2000, 768, 2048, 64 314 / 270; 8192, 768,
+//    1536, 8 158 / 137; 1000, 1024, 2048, 32 217 / 190; 4096, 1536, 4096, 2 361 / 313; 8192, 768, 2048, 16 238 / 229; 6000, 512, 2048, 24 169 / 168; 8192, 1024, 2048,
+//    8 237 / 237.  Beyond that two launches fill the chip for as long, and share the caches better: 16384, 1024, 4096, 8
 //    752 / 792; 32768, 2048, 8192, 16 5227 / 5834; 2000, 2048, 8192, 16 896 / 962; 16384, 512, 1024, 8 152 / 162.
+//    Nor where the slower half of the launch, whose tiles rarely come out even, is expected to take 1.1 times as long as two launches on the tiles
+//    that suit each: 5003, 1000, 2728, 32 445 / 458; 8632, 544, 1592, 24 228 / 258; 18353, 576, 2248, 21 432 / 503; 3925, 1440, 5400, 13 666 / 753; 8660, 304, 848,
+//    57 126 / 139.  Of 107 sizes, most of them drawn, that leaves out 29, of which 18 are slower in one launch, by up to 16 %, and the others faster, by up
+//    to 7 % (6000, 1024, 2048, 32 303 / 285).  Segments of up to 128 rows stay in one launch: half of DX's waves leave out their products there (2959, 848,
+//    952, 32 134 / 119; 2008, 1216, 4320, 21 398 / 342).
+static bool pair_gains(const GatedArgs& x, const GatedArgs& w, int64_t max_rows) {
+  if (max_rows <= 128 * static_cast<int64_t>(w.E)) return true;
+  const TileTimes tx = tile_times(x, G_DX, max_rows), tw = tile_times(w, G_DW, max_rows);
+  const double dx = std::min({tx.t256, tx.t128, tx.t256_128}), dw = std::min(tw.t256, tw.t128);
+  return share_gated_pair<GatedA, GatedA>(x, w, max_rows).cost <= 1.1 * 0.25 * (dx * tile_cost<GatedA, G_DX>(x, max_rows) + dw * tile_cost<GatedA, G_DW>(w, max_rows));
+}
 int launch_gated_gradients_bf16(const GatedArgs& x, const GatedArgs& w, int64_t max_rows, hipStream_t stream) {
   const double cus = num_cus();
   const double xu = likely_tiles(x, G_DX, max_rows, 128, 128), wu = likely_tiles(w, G_DW, max_rows, 128, 128);
   const double xa = likely_tiles(x, G_DX, max_rows, 256, 256), wa = likely_tiles(w, G_DW, max_rows, 256, 256);
   if (xu <= 1.5 * cus && xu + wu <= 3.5 * 2.0 * cus)
     return xu < 0.25 * cus ? launch_gated_pair<GatedS, GatedU>(x, w, max_rows, stream) : launch_gated_pair<GatedU, GatedU>(x, w, max_rows, stream);
-  if (xu > 0.625 * cus && xa >= 0.25 * cus && xa <= cus && wa >= 2.0 * xa && wa <= 24.0 * cus) return launch_gated_pair<GatedA, GatedA>(x, w, max_rows, stream);
-  if (xu >= 0.375 * cus && xu <= 0.625 * cus && wu <= 12.0 * 2.0 * cus) return launch_gated_pair<GatedU, GatedU>(x, w, max_rows, stream);
+  if (xu > 0.625 * cus && xa >= 0.25 * cus && xa <= cus && wa >= 2.0 * xa && wa <= 24.0 * cus && pair_gains(x, w, max_rows))
+    return launch_gated_pair<GatedA, GatedA>(x, w, max_rows, stream);
+  if (xu >= 0.375 * cus && xu <= 0.625 * cus && wu <= (short_segments(x, max_rows) ? 7.0 : 12.0) * 2.0 * cus) return launch_gated_pair<GatedU, GatedU>(x, w, max_rows, stream);
   const int st = launch_gated_bf16(w, G_DW, KEEP_NONE, max_rows, stream);
   return st == SCMOE_OK ? launch_gated_bf16(x, G_DX, KEEP_NONE, max_rows, stream) : st;
 }

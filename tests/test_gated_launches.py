@@ -1,9 +1,11 @@
-"""The launch that dx and the weights' gradients of the gated experts share, without a GPU."""
+"""The launch that dx and the weights' gradients of the gated experts share, without a GPU (tests/hip_recorder.c in place of the HIP runtime)."""
 import math
 import os
 import subprocess
 
 import pytest
+
+from test_gated_abi import BF16, P, record  # noqa: F401 (a fixture)
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -55,3 +57,19 @@ def test_small_tiles_are_spread(shares):
     assert shares["few long tiles beside many small ones"] == 28
     assert shares["one expert"] == 13
     assert 8 * shares["more than a workgroup a compute unit"] + 102 <= 256
+
+
+# rows, model width, hidden width, experts, and what the gradient takes in two launches and in one (us)
+TWO = [(5003, 1000, 2728, 32, 445, 458), (8632, 544, 1592, 24, 228, 258), (18353, 576, 2248, 21, 432, 503), (3925, 1440, 5400, 13, 666, 753),
+       (8660, 304, 848, 57, 126, 139), (5028, 1032, 1448, 16, 204, 230), (32768, 2048, 8192, 16, 5227, 5834), (843, 480, 1816, 30, 99, 108), (54, 624, 1736, 22, 88, 98),
+       (396, 720, 1384, 20, 77, 83)]
+ONE = [(2000, 768, 2048, 64, 314, 270), (8192, 768, 1536, 8, 158, 137), (1000, 1024, 2048, 32, 217, 190), (4096, 1536, 4096, 2, 361, 313),
+       (2959, 848, 952, 32, 134, 119), (2008, 1216, 4320, 21, 398, 342), (8192, 384, 1536, 8, 112, 101), (1068, 376, 760, 42, 56, 53),
+       (1479, 344, 784, 43, 69, 60), (2205, 576, 2232, 16, 142, 128), (744, 1336, 2408, 9, 169, 153), (7001, 80, 208, 4, 33, 28)]
+
+
+@pytest.mark.parametrize("rows,d,F,E,two,one", TWO + ONE)
+def test_dx_shares_a_launch_with_the_weights_gradients_where_that_is_faster(record, rows, d, F, E, two, one):  # noqa: F811
+    (st, lines), = record([("grad", dict(rows=rows, d=d, F=F, E=E, dtype=BF16, dx=2 * P))])
+    assert st == 0 and len(lines) == (2 if one < two else 3)
+    assert any("gated_pair_kernel" in w[2] for w in lines) == (one < two)
