@@ -115,7 +115,7 @@ extern "C" int scmoe_gated_ffn(const void* x_perm, int64_t ld_perm, int32_t dtyp
   a.pre = static_cast<unsigned char*>(pre); a.ldpre = ldpre;
   a.j[0] = gated_job(x_perm, ld_perm, W1, ldw1, hidden, ldh, 0, F, d);
   const bool experts = second_is_the_experts(dtype, max_rows, E, d, F);
-  if (experts && dtype == SCMOE_BF16 && workspace != nullptr && ws_bytes >= ffn_mfma_scratch_bytes() && !takes_few(G_GATE, pre_keep, dtype, max_rows, E)) {
+  if (experts && workspace != nullptr && ws_bytes >= ffn_mfma_scratch_bytes() && !takes_few(G_GATE, pre_keep, dtype, max_rows, E)) {
     a.zero = static_cast<int*>(workspace);                  // (the counters of tiles that the second product cuts along K; the kernel for few rows clears none)
     a.zeros = ffn_mfma_counter_ints();
   }

@@ -134,24 +134,11 @@ __device__ __forceinline__ uint32_t max_over_lq(uint32_t v) {
   return max(b[0], b[1]);
 }
 
-template <bool F32>
-__device__ __forceinline__ void store4(unsigned char* p, const float* v) {
-  if constexpr (F32) *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
-  else *reinterpret_cast<uint2*>(p) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
-}
-template <bool F32>
+__device__ __forceinline__ void store4(unsigned char* p, const float* v) { *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]}; }
 __device__ __forceinline__ void load4(const unsigned char* p, float* v) {
-  if constexpr (F32) {
-    const f32x4_t t = *reinterpret_cast<const f32x4_t*>(p);
+  const f32x4_t t = *reinterpret_cast<const f32x4_t*>(p);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = t[q];
-  } else {
-    const uint2 t = *reinterpret_cast<const uint2*>(p);
-    v[0] = __uint_as_float(t.x << 16);
-    v[1] = __uint_as_float(t.x & 0xffff0000u);
-    v[2] = __uint_as_float(t.y << 16);
-    v[3] = __uint_as_float(t.y & 0xffff0000u);
-  }
+  for (int q = 0; q < 4; ++q) v[q] = t[q];
 }
 
 // The schedule's constructor, and its search for a tile's segment, read the segments' bounds one after the other; here a wave reads 64 at
@@ -784,10 +771,10 @@ __device__ __forceinline__ void gated_product(const GatedArgs& p, const int bloc
             h[q] = gated_act<F32, ACT>(g[q]) * u[q];
           }
           if (in && f < cN) {
-            store4<F32>(cC + (static_cast<int64_t>(r) * cldc + f) * EB, h);
+            store4(cC + (static_cast<int64_t>(r) * cldc + f) * EB, h);
             if constexpr (KEEP == KEEP_FULL) {
-              store4<F32>(p.pre + (static_cast<int64_t>(r) * p.ldpre + f) * EB, g);
-              store4<F32>(p.pre + (static_cast<int64_t>(r) * p.ldpre + cN + f) * EB, u);
+              store4(p.pre + (static_cast<int64_t>(r) * p.ldpre + f) * EB, g);
+              store4(p.pre + (static_cast<int64_t>(r) * p.ldpre + cN + f) * EB, u);
             }
           }
         }
@@ -828,8 +815,8 @@ __device__ __forceinline__ void gated_product(const GatedArgs& p, const int bloc
               row += p.ldpre;
               ckpt_decode4(*reinterpret_cast<const uint32_t*>(row + n), ckpt_scale(row[cN + n / CKPT_BLOCK]), u);
             } else {
-              load4<F32>(p.pre + (static_cast<int64_t>(r) * p.ldpre + n) * EB, g);
-              load4<F32>(p.pre + (static_cast<int64_t>(r) * p.ldpre + cN + n) * EB, u);
+              load4(p.pre + (static_cast<int64_t>(r) * p.ldpre + n) * EB, g);
+              load4(p.pre + (static_cast<int64_t>(r) * p.ldpre + cN + n) * EB, u);
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -839,12 +826,12 @@ __device__ __forceinline__ void gated_product(const GatedArgs& p, const int bloc
               du[q] = v[q] * a;
               dg[q] = v[q] * u[q] * s;
             }
-            store4<F32>(cC + (static_cast<int64_t>(r) * cldc + n) * EB, h);
-            store4<F32>(p.dpre + (static_cast<int64_t>(r) * p.lddpre + n) * EB, dg);
-            store4<F32>(p.dpre + (static_cast<int64_t>(r) * p.lddpre + cN + n) * EB, du);
+            store4(cC + (static_cast<int64_t>(r) * cldc + n) * EB, h);
+            store4(p.dpre + (static_cast<int64_t>(r) * p.lddpre + n) * EB, dg);
+            store4(p.dpre + (static_cast<int64_t>(r) * p.lddpre + cN + n) * EB, du);
           } else {
             const int64_t at = MODE == G_DW ? (static_cast<int64_t>(ce) * jc.M + r) * cldc + n : static_cast<int64_t>(r) * cldc + n;
-            store4<F32>(cC + at * EB, v);
+            store4(cC + at * EB, v);
           }
         }
       }
