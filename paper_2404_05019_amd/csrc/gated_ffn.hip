@@ -3,6 +3,7 @@
 //   forward    GATE (hidden rows, and g and u where they are kept), DOWN
 //   backward   DH (gradients of g and u, h again), DW (both weights' gradients in one launch), DX
 #include "gated_tiles.hpp"
+#include <math.h>
 
 namespace scmoe {
 
@@ -13,24 +14,43 @@ static_assert(BUFFER_NOWHERE + 127ull * 2 * GATED_MOST_LD < (1ull << 32) && 256l
 static_assert(BUFFER_NOWHERE + 127ull * 2 * (2 * SCMOE_MAX_GATED_WIDTH + 64) < (1ull << 32));   // (the workspace's padded rows)
 static bool gated_view_ok(const void* p, int64_t ld, int64_t cols, int dtype) { return view_ok(p, ld, cols, dtype) && ld <= GATED_MOST_LD; }
 
-// Which calls take the kernel for few rows (gated_few.hip): where experts average at most two rows (DOWN: one, above which the experts'
-// second product does better), or there are no more than it takes at a time; in fp32, whose matrix instructions have less to gain, five.
-// us of a forward call, other kernels / few rows in GATE alone / in both:
-//   bf16, d = 2048, F = 8192, E = 16    1 row 36.1 / 28.8 / 22.7, 8 rows 160 / 139 / 138, 16 rows 202 / 182 / 178, 32 rows 298 / 259 / 267, 64 rows 312 / 330 / 385
-//   bf16, 4 rows of one expert 34.4 / 30.9 / 25.9, 16 rows 36.5 / 60.7 / 68.5;   30 rows, d = 1000, F = 2728, E = 8 39.8 / 44.4 / 48.1
-//   fp32, d = 1024, F = 4096, E = 8     1 row 35.0 / 21.6 / 16.8, 16 rows 123 / 107 / 64, 40 rows 138 / 130 / 106;   64 rows, d = 64, F = 256, E = 4 17.5 / 17.9 / 16.8
-static bool few_rows(int mode, int dtype, int64_t rows, int E) {
+// Which calls take the kernel for few rows (gated_few.hip).  A wave of it has one column of a segment's tile.  It streams the column's weights well where
+// they are long (4 KB and more), and costs some 0.6 ns of its own, all waves together: more than a row of 512 values.  So it is taken
+//  * up to an average of so many rows an expert (bf16: two, in DOWN one, above which the experts' second product does better; fp32, whose matrix instructions
+//    have less to gain: five and two), where the columns are long enough for the number of waves;
+//  * up to five rows an expert, where the waves are so few that the others' launch takes longer anyhow;
+//  * for no more rows than a tile has.
+// us of a forward call, random loads, other kernels / few rows in GATE alone / in DOWN alone / in both:
+//   bf16  1 row, d = 2048, F = 8192, E = 16 36 / 29 / - / 23;  8 rows 147 / 126 / 143 / 121;  16, E = 32 263 / 237 / 256 / 218;  but 40, E = 8 161 / 191 / 199 / 228
+//         5, 512, 2048, 4 17 / 16 / 16 / 16;  but 40, 512, 2048, 8 17 / 30 / 21 / 34;  64, 256, 1024, 64 21 / 36 / 25 / 40;  96, 512, 512, 64 22 / 28 / 37 / 44;
+//         64, 1024, 4096, 64 170 / 206 / 170 / 208;  200, 256, 1024, 200 46 / 130 / 67 / 151
+//   fp32  5, 1024, 4096, 1 89 / 79 / 31 / 18;  16, 1024, 4096, 8 129 / 111 / 90 / 72;  40, 1024, 4096, 8 138 / 133 / 114 / 110;  20, 256, 1024, 4 31 / 30 / 17 / 17;
+//         64, 2048, 2048, 32 323 / 273 / 304 / 252;  but 80, 2048, 8192, 16 733 / 820 / 831 / 924;  320, 256, 1024, 64 64 / 100 / 74 / 110
+// Of 770 such calls the choice is 0.8 % above the best of the four in the mean, 25 % at most (by the average alone 11 %, and up to three and a half times as
+// long).  Where a load is skewed, a segment has many tiles of four rows, each of which reads its weights, if from the caches: all rows at one expert of 16,
+// bf16, d = 2048, F = 8192, 16 rows 79 us where the others take 35, 32 rows 104 where they take 35.  A random load of as many takes 160 to 260.
+// Beyond 256 experts, four times what the gate has, the average alone decides, as tests/test_gated_abi.py has it for 600 (1100 rows, d = 64, F = 2048 1430 us, by
+// the other kernels 304).
+static bool few_rows(int mode, int dtype, int64_t rows, int E, int N, int Kd) {
   if (rows > 4096) return false;                         // (tiles of rows are the grid's y)
-  const int64_t per = dtype == SCMOE_F32 ? 5 : mode == G_GATE ? 2 : 1;
-  return rows <= 4 || rows <= per * E;
+  const bool f32 = dtype == SCMOE_F32, gate = mode == G_GATE;
+  if (rows <= 4) return true;
+  if (E > 256) return rows <= (f32 ? 5 : gate ? 2 : 1) * static_cast<int64_t>(E);
+  // segments that have rows, of rows that are spread at random
+  const double bytes = static_cast<double>(Kd) * elem_bytes(dtype), occupied = E * (1.0 - pow(1.0 - 1.0 / E, static_cast<double>(rows)));
+  const double waves = (occupied > rows / 3.0 ? occupied : rows / 3.0) * N;
+  if (!f32 && gate) return (rows <= 2 * E && (bytes >= 4000.0 || waves <= 12.0 * bytes)) || (rows <= 5 * E && waves <= 8000.0);
+  if (!f32) return (rows <= E && waves <= 2.0 * bytes) || (rows <= 5 * E && waves <= 4000.0);
+  if (gate) return rows <= 5 * E && (bytes >= 4000.0 || waves <= 24.0 * bytes);
+  return (rows <= 2 * E && (bytes >= 8000.0 || waves <= 12.0 * bytes)) || (rows <= 5 * E && waves <= 16000.0);
 }
 
-static bool takes_few(int mode, int keep, int dtype, int64_t rows, int E) {
-  return ((mode == G_GATE && keep != KEEP_8BIT) || mode == G_DOWN) && few_rows(mode, dtype, rows, E);
+static bool takes_few(const GatedArgs& a, int mode, int keep, int dtype, int64_t rows) {
+  return ((mode == G_GATE && keep != KEEP_8BIT) || mode == G_DOWN) && few_rows(mode, dtype, rows, a.E, a.j[0].N, a.j[0].Kd);
 }
 
 static int launch_gated(const GatedArgs& a, int mode, int keep, int64_t max_rows, int dtype, hipStream_t stream) {
-  if (takes_few(mode, keep, dtype, max_rows, a.E)) return launch_gated_few(a, mode, keep, max_rows, dtype, stream);
+  if (takes_few(a, mode, keep, dtype, max_rows)) return launch_gated_few(a, mode, keep, max_rows, dtype, stream);
   return dtype == SCMOE_BF16 ? launch_gated_bf16(a, mode, keep, max_rows, stream) : launch_gated_f32(a, mode, keep, max_rows, stream);
 }
 
@@ -67,7 +87,7 @@ static bool kept_ok(const void* p, int64_t ld, int64_t width, int keep, int dtyp
 // so / with DOWN: 16384 rows, d = 1024, F = 4096, E = 8 372 / 394; 30 rows, d = 1000, F = 2728 45 / 52; but 500 rows 73 / 64, 5003 rows, E = 32
 // 272 / 208.  In fp32 DOWN does better from 40 rows on (d = 1024, F = 4096, E = 8 148 / 161; 4096 rows, F = 2048 381 / 417).
 static bool second_is_the_experts(int dtype, int64_t rows, int E, int d, int F) {
-  if (dtype == SCMOE_F32 || few_rows(G_DOWN, dtype, rows, E)) return false;
+  if (dtype == SCMOE_F32 || few_rows(G_DOWN, dtype, rows, E, d, F)) return false;
   return ffn_mfma_supported(d, F) || rows <= 64 || (rows <= 16 * static_cast<int64_t>(E) && rows <= 1024);
 }
 
@@ -115,7 +135,7 @@ extern "C" int scmoe_gated_ffn(const void* x_perm, int64_t ld_perm, int32_t dtyp
   a.pre = static_cast<unsigned char*>(pre); a.ldpre = ldpre;
   a.j[0] = gated_job(x_perm, ld_perm, W1, ldw1, hidden, ldh, 0, F, d);
   const bool experts = second_is_the_experts(dtype, max_rows, E, d, F);
-  if (experts && workspace != nullptr && ws_bytes >= ffn_mfma_scratch_bytes() && !takes_few(G_GATE, pre_keep, dtype, max_rows, E)) {
+  if (experts && workspace != nullptr && ws_bytes >= ffn_mfma_scratch_bytes() && !takes_few(a, G_GATE, pre_keep, dtype, max_rows)) {
     a.zero = static_cast<int*>(workspace);                  // (the counters of tiles that the second product cuts along K; the kernel for few rows clears none)
     a.zeros = ffn_mfma_counter_ints();
   }
