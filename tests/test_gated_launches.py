@@ -14,7 +14,7 @@ LAUNCHES = {
     "few long tiles beside many small ones": (224, 9.0, 24, 124.0, 64),             # 7001 rows, d = 80, F = 208, E = 4
     "one expert": (97, 7.0, 10, 100.0, 64),
     "more than a workgroup a compute unit": (193, 24.0, 102, 67.4, 64),              # 8183, 320, 680, 2
-    "one a compute unit": (128, 67.0, 3072, 4.0, 32),
+    "one a compute unit": (128, 67.0, 3000, 4.0, 32),
     "one tile of each": (1, 10.0, 1, 10.0, 32),
     "nothing": (0, 1.0, 0, 1.0, 64),
     "two workgroups": (100, 3.0, 100, 5.0, 2),
