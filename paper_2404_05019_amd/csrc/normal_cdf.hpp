@@ -13,8 +13,8 @@
 namespace scmoe {
 
 // Phi(v), and e = e^(-v^2 / 2).  Below zero Phi(v) = e M(|v|), above 1 - that, with M(z) ~ t P(t), t = 1 / (1 + a z) (Hastings' form): the
-// smallest error where v is small, a tenth of a code's step of bf16 everywhere: v Phi(v) is multiplied by other factors, so what lies
-// far below zero counts relative to itself (a polynomial in v, clamped as in gelu.hpp, is off by 1.2e-5 in Phi, a quarter of it at -4).
+// smallest error where v is small, and everywhere a fiftieth of bf16's rounding or less: v Phi(v) is multiplied by other factors, so what
+// lies far below zero counts relative to itself (a polynomial in v, clamped as in gelu.hpp, is off by 1.2e-5 in Phi, a quarter of it at -4).
 // a and P: least largest error over 0 <= z <= 13.5, allowed to grow tenfold from z = 0.5 to 3.5.
 //   relative error of Phi   v >= -1: 8.3e-6, >= -2: 2.9e-5, >= -13: 7.4e-5;  absolute: 3.5e-6;  below -13.2 e underflows
 // The exponential and the reciprocal are the hardware's (1 ulp each); +-inf and NaN come out as in the formula.
